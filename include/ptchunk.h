@@ -423,6 +423,96 @@ int pt_update_consts_read(pt_ctx* ctx, pt_update_consts* out, void* stream);
  * skips if found_inf != 0.  For kernel-isolated tests. */
 int pt_step_override(pt_ctx* ctx, float grad_mult, int32_t found_inf, void* stream);
 
+/* ---- AdamW over a list of tensors ---------------------------------------------------------
+ * The update of pt_chunk_adamw_step for tensors where they lie, without chunks: any number of them, of any sizes,
+ * in one launch, behind one launch for the norm of all their gradients.  One optimizer step is
+ *     pt_tensors_grad_sqnorm     global norm and non-finite flag of all gradients of the list; ends the step before
+ *     pt_tensors_adamw_step      clips by that norm and updates, or leaves everything as it is if a gradient is +-inf or NaN
+ * Both only enqueue.  A list has the step counter and the loss scale that a context has, and its own memory on the
+ * device that is current at pt_tensors_create; text of errors: pt_last_error(NULL) of the calling thread.  Not thread-safe.
+ * The caller owns the arrays; they stay where they are and of their size as long as the list is used (build a new
+ * list when gradients move).  No two arrays of a list may overlap, but for gradients, which are only read.
+ * Give a list's calls one stream, or order their streams by events.  A step may be captured into a graph, both calls in one. */
+typedef struct pt_tensors pt_tensors;
+
+#define PT_TENSOR_NO_DECAY 1u   /* kept out of the weight decay */
+#define PT_TENSOR_GRAD_F32 2u   /* the gradient is fp32, not of the list's 16-bit type */
+
+/* One tensor of a list; all pointers are device pointers to its first element, elements back to back.  16-bit arrays need
+ * 2-byte alignment, all others 4-byte.  elems may be 0: the pointers are then not looked at. */
+typedef struct {
+  const void* grad;  /* gradient, times the loss scale                                             */
+  float* master;     /* fp32 weights                                                               */
+  void* param16;     /* 16-bit copy of the weights, written; NULL: there is none                   */
+  void* m;           /* momentum: fp32, or OCP e4m3 codes                                          */
+  void* v;           /* variance in fp32, or its square root in e4m3 codes                         */
+  float* m_scale;    /* states in 8 bits: ceil(elems / 256) scales; code times the scale of its    */
+  float* v_scale;    /*   block of 256 elements is the value.  States in 32 bits: not looked at    */
+  uint64_t elems;
+  uint32_t flags;    /* PT_TENSOR_*                                                                */
+  uint32_t reserved;
+} pt_tensor;
+
+/* Describes n_tensors tensors to the device.  state_bits 32: m and v as in chunks, results bit-identical to theirs.
+ * state_bits 8: m and sqrt(v) in blocks of 256 consecutive elements of a tensor, OCP e4m3 codes times the block's largest
+ * magnitude / 448 (blocks whose largest is below 2^-100 become zero); all zero bytes and scales are m = v = 0.  The update computes
+ * in fp32 (each product rounded before it is added) and rounds the states up or down at random with the odds that keep their mean (rounding to nearest would
+ * hold an average in place that moves by less than half a code a step); a variance that is not zero keeps one code at least.
+ * The random numbers are a function of `seed`, the step counter and the element's place in the list: the same calls give the same
+ * bits.  scaler as for pt_ctx_create.  Allocates and synchronises; not a hot call.
+ * At most 2^31 blocks of 256 elements (each tensor's last one counted whole). */
+int pt_tensors_create(pt_tensors** out, int dtype, const pt_tensor* list, uint32_t n_tensors, int state_bits,
+                      const pt_scaler_cfg* scaler, uint64_t seed);
+int pt_tensors_destroy(pt_tensors* list);
+
+/* Overwrites step counter and loss-scale state (resume).  Enqueued on stream; a norm taken before is void. */
+int pt_tensors_set_state(pt_tensors* list, int32_t step, double loss_scale, int32_t good_steps, void* stream);
+
+/* Norm of all gradients / loss scale, fp64 in a fixed order, and whether one of them is +-inf or NaN.  Ends the step of an update
+ * enqueued before: counter and loss scale as by pt_step_end. */
+int pt_tensors_grad_sqnorm(pt_tensors* list, void* stream);
+
+/* One update of every tensor.  PT_ERR_STATE without a norm since the last one.  Betas other than the last call's cost a tiny
+ * launch more. */
+int pt_tensors_adamw_step(pt_tensors* list, const pt_hparams* hp, void* stream);
+
+/* Scalars of the last norm and update; step, good_steps and loss_scale as they are behind the update.  Synchronises `stream`. */
+int pt_tensors_report_read(pt_tensors* list, pt_step_report* out, void* stream);
+
+/* ---- loss of a language model's head -------------------------------------------------------
+ * Softmax cross entropy of `rows` hidden states against a head of `vocab` rows, and its gradients, without the logits of
+ * all rows ever being held.  With h = hidden, W = weight, y = target, s = row_scale:
+ *     z_rv = sum_k h_rk W_vk      loss_r = log sum_v exp(z_rv) - z_r,y_r
+ *     G_rv = s_r (exp(z_rv) / sum_u exp(z_ru) - [v = y_r])      d_hidden = G W      d_weight = G^T h
+ * A row whose target lies outside [0, vocab) is ignored: its loss and its row of d_hidden are 0, it adds nothing to d_weight,
+ * and nothing of its hidden state is looked at.  16-bit inputs, fp32 sums of their exact products; G is rounded to the 16-bit
+ * type once, between the two products it takes part in, and so are the results.
+ * d_hidden and d_weight may each be NULL: then that gradient is not taken; with both NULL only the loss is, and nothing of the
+ * size of the logits is written at all. */
+typedef struct {
+  const void* hidden;      /* device, [rows, width] 16-bit elements                                */
+  const void* weight;      /* device, [vocab, width]                                               */
+  const int64_t* target;   /* device, [rows]                                                       */
+  const float* row_scale;  /* device, [rows]: d(total) / d(loss_r), finite; NULL: 1 for every row  */
+  float* loss;             /* device, [rows], written                                              */
+  void* d_hidden;          /* device, [rows, width], written; or NULL                              */
+  void* d_weight;          /* device, [vocab, width], written; or NULL                             */
+  uint64_t hidden_stride, weight_stride, d_hidden_stride, d_weight_stride; /* elements between rows, >= width */
+  uint32_t rows, vocab, width;
+  int32_t dtype;           /* pt_dtype                                                             */
+} pt_head;
+
+/* Bytes of workspace that pt_head_loss needs at least, and that it is fastest with (0 for an argument that is NULL is not
+ * written).  With gradients the rows are taken in pieces: fewer bytes, more pieces, each of which reads and writes the sums of
+ * d_weight once.  Host only. */
+int pt_head_workspace(const pt_head* head, uint64_t* least_bytes, uint64_t* best_bytes);
+
+/* Enqueues the whole computation on `stream`; allocates nothing, does not synchronise, may be captured into a graph.
+ * workspace: device, 256-byte aligned, of workspace_bytes >= least_bytes (else PT_ERR_NOMEM); its contents are of no use afterwards.
+ * Widths, strides and addresses that are multiples of 8 elements take the weight where it lies; others are copied into the
+ * workspace first.  rows == 0 does nothing but clear d_weight.  Errors: text in pt_last_error(NULL). */
+int pt_head_loss(const pt_head* head, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* ---- OPTIM-phase cost model (host only) -------------------------------------------------
  * The paper's runtime model restricted to the optimizer phase (Appendix A.1, Eq. 2: the part
  * that runs on the GPU and the part that does not run side by side, the longer one decides;

@@ -26,6 +26,8 @@ EXPORTS = [
     "pt_layout_grouped", "pt_chunk_size_search", "pt_layout_execution_order", "pt_chunk_host_adamw_step",
     "pt_optim_predict", "pt_optim_choose", "pt_ctx_set_no_decay", "pt_chunk_accum_grads",
     "pt_chunk_grad_sqnorm_noalloc", "pt_calib_adamw_pattern", "pt_stream_status",
+    "pt_tensors_create", "pt_tensors_destroy", "pt_tensors_set_state", "pt_tensors_grad_sqnorm", "pt_tensors_adamw_step",
+    "pt_tensors_report_read", "pt_head_workspace", "pt_head_loss",
 ]
 
 
@@ -65,6 +67,19 @@ class pt_optim_choice(C.Structure):
                 ("t_step", C.c_double), ("t_gpu", C.c_double), ("t_other", C.c_double), ("hbm_bytes", C.c_uint64)]
 
 
+class pt_tensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("master", C.c_void_p), ("param16", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("elems", C.c_uint64), ("flags", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class pt_head(C.Structure):
+    _fields_ = [("hidden", C.c_void_p), ("weight", C.c_void_p), ("target", C.c_void_p), ("row_scale", C.c_void_p), ("loss", C.c_void_p),
+                ("d_hidden", C.c_void_p), ("d_weight", C.c_void_p), ("hidden_stride", C.c_uint64), ("weight_stride", C.c_uint64),
+                ("d_hidden_stride", C.c_uint64), ("d_weight_stride", C.c_uint64), ("rows", C.c_uint32), ("vocab", C.c_uint32),
+                ("width", C.c_uint32), ("dtype", C.c_int32)]
+
+
+PT_TENSOR_NO_DECAY, PT_TENSOR_GRAD_F32 = 1, 2
 PT_OPTIM_STREAM, PT_OPTIM_HOST = 0, 1
 
 
@@ -135,6 +150,14 @@ def lib():
         L.pt_layout_execution_order.argtypes = [C.POINTER(u32), u32, u32, C.POINTER(u32)]
         L.pt_chunk_size_search.argtypes = [C.POINTER(u64), C.POINTER(u32), u32, u64, u64, u64, C.POINTER(u64),
                                            C.POINTER(u32), C.POINTER(u64)]
+        L.pt_tensors_create.argtypes = [pp, C.c_int, C.POINTER(pt_tensor), u32, C.c_int, C.POINTER(pt_scaler_cfg), u64]
+        L.pt_tensors_destroy.argtypes = [vp]
+        L.pt_tensors_set_state.argtypes = [vp, i32, C.c_double, i32, vp]
+        L.pt_tensors_grad_sqnorm.argtypes = [vp, vp]
+        L.pt_tensors_adamw_step.argtypes = [vp, C.POINTER(pt_hparams), vp]
+        L.pt_tensors_report_read.argtypes = [vp, C.POINTER(pt_step_report), vp]
+        L.pt_head_workspace.argtypes = [C.POINTER(pt_head), C.POINTER(u64), C.POINTER(u64)]
+        L.pt_head_loss.argtypes = [C.POINTER(pt_head), vp, u64, vp]
         for name in EXPORTS:
             if name not in ("pt_version", "pt_status_string", "pt_last_error"):
                 getattr(L, name).restype = C.c_int
@@ -460,3 +483,98 @@ def pt_chunk_accum_grads(ctx, plan, acc_chunks, overwrite, take_norm, stream=Non
         rc = L.pt_chunk_accum_grads(ctx, plan, _ptr_array(acc_chunks), int(bool(overwrite)), int(bool(take_norm)), _stream(stream))
     if rc:
         _check(rc, "pt_chunk_accum_grads", ctx)
+
+
+# ---- lists of tensors -------------------------------------------------------------------
+
+def tensor(grad, master, m, v, param16=None, m_scale=None, v_scale=None, no_decay: bool = False) -> pt_tensor:
+    """One tensor of a list, from torch tensors whose elements lie back to back (master: fp32; grad: fp32 or the list's 16-bit type;
+    m, v: fp32, or one byte an element with m_scale and v_scale).  The caller keeps them."""
+    import torch
+    n = master.numel()
+    for name, x in (("grad", grad), ("master", master), ("m", m), ("v", v), ("param16", param16)):
+        if x is not None and not (x.is_contiguous() and x.numel() == n):
+            raise ValueError(f"tensor: {name} is not {n} elements back to back")
+    for name, x in (("m_scale", m_scale), ("v_scale", v_scale)):
+        if x is not None and not (x.is_contiguous() and x.numel() >= -(-n // 256) and x.dtype == torch.float32):
+            raise ValueError(f"tensor: {name} is not an fp32 number for every 256 elements")
+    size = 1 if m_scale is not None else 4
+    if master.dtype != torch.float32 or m.element_size() != size or v.element_size() != size or \
+            (param16 is not None and param16.element_size() != 2) or (grad.dtype != torch.float32 and grad.element_size() != 2):
+        raise ValueError("tensor: an array is not of its element type")
+    flags = (PT_TENSOR_NO_DECAY if no_decay else 0) | (PT_TENSOR_GRAD_F32 if grad.dtype == torch.float32 else 0)
+    return pt_tensor(_addr(grad), _addr(master), _addr(param16), _addr(m), _addr(v), _addr(m_scale), _addr(v_scale), n, flags, 0)
+
+
+def pt_tensors_create(dtype: int, tensors, state_bits: int, scaler: pt_scaler_cfg | None = None, seed: int = 0):
+    """tensors: list of `tensor(...)`; state_bits: 8 or 32."""
+    arr = (pt_tensor * max(len(tensors), 1))(*tensors)
+    out = C.c_void_p()
+    _check(lib().pt_tensors_create(C.byref(out), int(dtype), arr, len(tensors), int(state_bits),
+                                   C.byref(scaler) if scaler is not None else None, int(seed)), "pt_tensors_create")
+    return out
+
+
+def pt_tensors_destroy(tensors):
+    _check(lib().pt_tensors_destroy(tensors), "pt_tensors_destroy")
+
+
+def pt_tensors_set_state(tensors, step: int, loss_scale: float, good_steps: int, stream=None):
+    _check(lib().pt_tensors_set_state(tensors, int(step), float(loss_scale), int(good_steps), _stream(stream)), "pt_tensors_set_state")
+
+
+def pt_tensors_grad_sqnorm(tensors, stream=None):
+    rc = lib().pt_tensors_grad_sqnorm(tensors, _stream(stream))
+    if rc:
+        _check(rc, "pt_tensors_grad_sqnorm")
+
+
+def pt_tensors_adamw_step(tensors, hp: pt_hparams, stream=None):
+    rc = lib().pt_tensors_adamw_step(tensors, C.byref(hp), _stream(stream))
+    if rc:
+        _check(rc, "pt_tensors_adamw_step")
+
+
+def pt_tensors_report_read(tensors, stream=None) -> pt_step_report:
+    out = pt_step_report()
+    _check(lib().pt_tensors_report_read(tensors, C.byref(out), _stream(stream)), "pt_tensors_report_read")
+    return out
+
+
+# ---- loss of a head ---------------------------------------------------------------------
+
+def head(hidden, weight, target, loss, row_scale=None, d_hidden=None, d_weight=None) -> pt_head:
+    """Describes a head's loss from torch tensors: hidden [rows, width] and weight [vocab, width] of one 16-bit type, target [rows] int64,
+    loss and row_scale [rows] fp32, gradients as what they belong to.  Rows may lie at any stride.  The caller keeps the tensors."""
+    import torch
+    rows, width = hidden.shape
+    vocab = weight.shape[0]
+    if hidden.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("head: hidden is neither bfloat16 nor float16")
+    for name, x, shape in (("weight", weight, (vocab, width)), ("d_hidden", d_hidden, (rows, width)), ("d_weight", d_weight, (vocab, width)),
+                           ("hidden", hidden, (rows, width))):
+        if x is not None and (x.dtype != hidden.dtype or tuple(x.shape) != shape or (x.stride(1) != 1 and width > 1)):
+            raise ValueError(f"head: {name} is not {shape} of {hidden.dtype} with the elements of a row back to back")
+    for name, x, dtype in (("target", target, torch.int64), ("loss", loss, torch.float32), ("row_scale", row_scale, torch.float32)):
+        if x is not None and (x.dtype != dtype or tuple(x.shape) != (rows,) or not x.is_contiguous()):
+            raise ValueError(f"head: {name} is not {rows} numbers of {dtype} back to back")
+
+    def pitch(x):
+        return 0 if x is None else max(x.stride(0), width) if x.shape[0] <= 1 else x.stride(0)
+    return pt_head(_addr(hidden), _addr(weight), _addr(target), _addr(row_scale), _addr(loss), _addr(d_hidden), _addr(d_weight), pitch(hidden),
+                   pitch(weight), pitch(d_hidden), pitch(d_weight), rows, vocab, width, PT_BF16 if hidden.dtype == torch.bfloat16 else PT_FP16)
+
+
+def pt_head_workspace(head: pt_head):
+    """-> (least, best) bytes of the workspace.  Host only."""
+    a, b = C.c_uint64(), C.c_uint64()
+    _check(lib().pt_head_workspace(C.byref(head), C.byref(a), C.byref(b)), "pt_head_workspace")
+    return int(a.value), int(b.value)
+
+
+def pt_head_loss(head: pt_head, workspace, stream=None):
+    """workspace: a device tensor of pt_head_workspace(head) bytes."""
+    rc = lib().pt_head_loss(C.byref(head), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                            _stream(stream))
+    if rc:
+        _check(rc, "pt_head_loss")

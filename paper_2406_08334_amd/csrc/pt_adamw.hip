@@ -11,8 +11,7 @@
 // sqrt and / (this file is compiled with contraction off and without fast-math).
 #include "pt_common.h"
 #include "pt_scalars.h"
-
-#include <hip/hip_fp16.h>
+#include "pt_update.h"
 
 #include <algorithm>
 
@@ -41,35 +40,6 @@ __device__ __forceinline__ void st_stream(T v, P p) {
   else *p = v;
 }
 
-template <int DT>
-__device__ __forceinline__ float decode16(uint32_t w16) {
-  if (DT == PT_BF16) {
-    return __uint_as_float(w16 << 16);
-  } else {
-    __half_raw r; r.x = (unsigned short)w16;
-    return __half2float(__half(r));
-  }
-}
-
-template <int DT>
-__device__ __forceinline__ uint32_t encode16(float x) {
-  if (DT == PT_BF16) {
-    const uint32_t u = __float_as_uint(x);
-    const uint32_t nan = (u >> 16) | 0x0040u;                          // NaN stays NaN
-    const uint32_t rne = (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;       // round to nearest, ties to even
-    return (u & 0x7fffffffu) > 0x7f800000u ? nan : rne;                // a select: a branch per element was compiled before
-  } else {
-    // The recast rounds the STORED fp32 master weight.  Without this barrier the compiler
-    // folds the producing fma and the conversion into one mixed-precision fma that rounds
-    // the exact result straight to fp16, which can differ from RNE16(RNE32(.)) by one ulp.
-    asm volatile("" : "+v"(x));
-    __half_raw r = __half_raw(__float2half_rn(x));
-    return (uint32_t)r.x;
-  }
-}
-
-struct Consts { float b1, b2, omb1, omb2, decay, step_size, rsb2, eps, gm; };
-
 // Four gradient elements as they sit in a gradient chunk: four 16-bit words, or four floats
 // when the chunk accumulates micro-batches in fp32.
 template <bool GF32> struct GradUnit { typedef u32x2 vec; };
@@ -95,19 +65,10 @@ __device__ __forceinline__ void update_unit(const Consts& k, const float (&dk)[4
   uint32_t pw[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    // one correctly rounded binary32 operation per line; contraction is off for this file
-    float g = gv[j] * k.gm;
-    float t1 = k.omb1 * g;
-    float mn = __builtin_fmaf(k.b1, m[j], t1);
-    float t2 = k.omb2 * g;
-    t2 = t2 * g;
-    float vn = __builtin_fmaf(k.b2, v[j], t2);
-    float d = __builtin_fmaf(__builtin_sqrtf(vn), k.rsb2, k.eps);
-    float u = mn / d;
-    float t3 = w[j] * dk[j];
-    float wn = __builtin_fmaf(-k.step_size, u, t3);
-    m[j] = mn; v[j] = vn; w[j] = wn;
-    pw[j] = encode16<DT>(wn);
+    float wj = w[j], mj = m[j], vj = v[j], sj;
+    update_element(k, dk[j], gv[j], wj, mj, vj, sj);
+    m[j] = mj; v[j] = vj; w[j] = wj;
+    pw[j] = encode16<DT>(wj);
   }
   p2.x = pw[0] | (pw[1] << 16);
   p2.y = pw[2] | (pw[3] << 16);

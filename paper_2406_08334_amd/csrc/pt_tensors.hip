@@ -1,0 +1,535 @@
+// AdamW over a list of tensors at once, with states in 32 or in 8 bits: one launch for the norm of all gradients, one for the update.
+//
+// The update is that of the chunks (pt_update.h), bit for bit where the states have 32 bits.  States in 8 bits are blocks of 256 consecutive
+// elements of a tensor: m and r = sqrt(v) as OCP e4m3 numbers times an fp32 scale, the block's largest magnitude / 448.  r, because its
+// range is half of v's in powers of two: e4m3 numbers reach from 448 down to 2^-9, and an r 2^-18 below its block's largest is as good as
+// the smallest code.  A wave holds a block, four elements a lane, so the largest magnitude is a tree over lanes and the state is read and
+// written once: 16.06 bytes an element (gradient 2, master 8, parameter 2, states 4, scales 0.06) instead of 28.
+//
+// States are rounded up or down at random with the odds that keep their mean.  To the nearest, an average that moves by less than half a
+// code's distance (6 %) a step, all of them with beta near 1, would stay where it is for good.  The 16 random bits of a state are a function of the
+// list's seed, the number of the update and the element's place (splitmix64 of a counter: Steele, Lea, Flood, 2014), so a run can be repeated.
+// What is not zero keeps an r of one code at least: an m beside an r of zero would be divided by eps alone.
+#include "pt_common.h"
+#include "pt_scalars.h"
+#include "pt_update.h"
+
+#include <algorithm>
+#include <memory>
+
+#pragma clang fp contract(off)
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// global memory takes these at any address of an element
+typedef f32x4 f32x4_a __attribute__((aligned(4)));
+typedef u32x2 u32x2_a __attribute__((aligned(2)));
+typedef u32x4 u32x4_a __attribute__((aligned(2)));
+
+constexpr uint32_t BLOCK = 256;              // elements of a block: a wave's, and those that share a scale
+constexpr uint32_t UNIT = 4096;              // elements a wave of the norm takes at a time
+constexpr uint32_t COARSE = 16;              // blocks / units per entry of the look-up tables
+constexpr uint32_t NORM_THREADS = 256, NORM_BLOCKS = 1024, NORM_WAVES = NORM_THREADS / 64;
+constexpr uint32_t UPDATE_WAVES = 11 * 256;
+
+// One tensor as the kernels read it.
+struct Desc {
+  uint64_t grad, master, param, m, v, ms, vs, elems;
+  uint32_t flags, pad;
+};
+
+struct ListState {
+  PtDevState s;
+  double bc1, bc2;       // 1 - beta^t of the update in flight
+  uint64_t key;          // of its random numbers
+  uint32_t applied;      // the update of the norm before has been enqueued: the next norm ends its step first
+};
+
+// Which tensor owns block or unit i: a table entry per COARSE of them says where to begin.
+struct Index { const uint32_t* first; const uint32_t* coarse; uint32_t n; };
+__device__ __forceinline__ uint32_t owner(const Index& x, uint32_t i) {
+  uint32_t t = x.coarse[i / COARSE];
+  while (i >= x.first[t + 1]) ++t;
+  return t;
+}
+
+__device__ __forceinline__ uint64_t mix64(uint64_t x) {
+  x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
+  x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
+  return x ^ (x >> 31);
+}
+constexpr uint64_t PHI = 0x9E3779B97F4A7C15ull;
+
+// ---- norm --------------------------------------------------------------------------------------------
+
+template <int DT>
+__device__ __forceinline__ void take8(const u32x4& q, double& a0, double& a1) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const double x = decode16<DT>(q[k] & 0xffffu), y = decode16<DT>(q[k] >> 16);
+    a0 = fma(x, x, a0);
+    a1 = fma(y, y, a1);
+  }
+}
+
+struct NormArgs {
+  Index units;
+  const Desc* desc;
+  ListState* st;
+  double* part;
+  double beta1, beta2;
+  uint64_t seed;
+};
+
+// Sum of squares of every gradient in a fixed order: waves take units in turn, the last workgroup to finish adds the workgroups' sums up in
+// order, ends the step before and opens this one.
+template <int DT>
+__global__ void __launch_bounds__(NORM_THREADS) k_list_norm(const NormArgs a) {
+  const uint32_t lane = threadIdx.x & 63;
+  double a0 = 0.0, a1 = 0.0;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * NORM_WAVES + (threadIdx.x >> 6));
+  for (uint32_t i = wave; i < a.units.n; i += gridDim.x * NORM_WAVES) {
+    const uint32_t u = a.units.n - 1 - i;           // from the far end: the update, which begins at the near one, finds that in the cache
+    const uint32_t t = owner(a.units, u);
+    const Desc& d = a.desc[t];
+    const uint64_t at = uint64_t(u - a.units.first[t]) * UNIT;
+    const uint32_t len = uint32_t(min(uint64_t(UNIT), d.elems - at));
+    if (d.flags & PT_TENSOR_GRAD_F32) {
+      const PT_GLOBAL float* g = (const PT_GLOBAL float*)d.grad + at;
+      const uint32_t whole = len / 4;
+#pragma unroll 8
+      for (uint32_t k = lane; k < whole; k += 64) {
+        const f32x4 q = *(const PT_GLOBAL f32x4_a*)(g + 4 * k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { const double x = q[j]; if (j & 1) a1 = fma(x, x, a1); else a0 = fma(x, x, a0); }
+      }
+      if (4 * whole + lane < len) { const double x = g[4 * whole + lane]; a0 = fma(x, x, a0); }
+    } else {
+      const PT_GLOBAL uint16_t* g = (const PT_GLOBAL uint16_t*)d.grad + at;
+      const uint32_t whole = len / 8;
+      if (len == UNIT) {
+        u32x4 q[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q[k] = *(const PT_GLOBAL u32x4_a*)(g + 8 * (lane + 64 * k));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) take8<DT>(q[k], a0, a1);
+      } else {
+        for (uint32_t k = lane; k < whole; k += 64) {
+          const u32x4 q = *(const PT_GLOBAL u32x4_a*)(g + 8 * k);
+          take8<DT>(q, a0, a1);
+        }
+        if (8 * whole + lane < len) { const double x = decode16<DT>(g[8 * whole + lane]); a0 = fma(x, x, a0); }
+      }
+    }
+  }
+  double sum = a0 + a1;
+  uint32_t none = 0;
+  __shared__ uint32_t s_last;
+  pt_block_sum(sum, none);
+  if (threadIdx.x == 0) {
+    st_agent(a.part + blockIdx.x, sum);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    s_last = __hip_atomic_fetch_add(&a.st->s.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1 ? 1u : 0u;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  PtDevState s = a.st->s;
+  if (a.st->applied) pt_advance(s, s.found_inf != 0);
+  // the powers of beta while the sums are on their way
+  const double bc = threadIdx.x < 2 ? 1.0 - pow(threadIdx.x ? a.beta2 : a.beta1, double(s.step + 1)) : 0.0;
+  sum = 0.0;
+  for (uint32_t k = threadIdx.x; k < gridDim.x; k += NORM_THREADS) sum += ld_agent(a.part + k);
+  pt_block_sum(sum, none);
+  if (threadIdx.x == 1) a.st->bc2 = bc;
+  if (threadIdx.x != 0) return;
+  uint32_t inf;
+  double sq;
+  pt_close_sum(sum, 1.0 / s.loss_scale, sq, inf);
+  s.sqnorm = sq;
+  s.norm = sqrt(sq);
+  s.found_inf = inf ? 1 : 0;
+  s.skip = s.found_inf;
+  s.ticket = 0;
+  a.st->s = s;
+  a.st->bc1 = bc;
+  a.st->key = mix64(a.seed + uint64_t(uint32_t(s.step) + 1u) * PHI);
+  a.st->applied = 0;
+}
+
+// The powers for an update whose betas are not those the norm was taken with.
+__global__ void k_list_betas(ListState* st, double beta1, double beta2) {
+  if (threadIdx.x > 1) return;
+  const double bc = 1.0 - pow(threadIdx.x ? beta2 : beta1, double(st->s.step + 1));
+  if (threadIdx.x) st->bc2 = bc; else st->bc1 = bc;
+}
+
+__global__ void k_list_set(ListState* st, int32_t step, double loss_scale, int32_t good_steps) {
+  st->s.step = step; st->s.loss_scale = loss_scale; st->s.good_steps = good_steps;
+  st->applied = 0;
+}
+
+// ---- update ------------------------------------------------------------------------------------------
+
+struct UpdateArgs {
+  Index blocks;
+  const Desc* desc;
+  ListState* st;
+  pt_hparams hp;
+};
+
+// The nine constants of the update, in every wave from the few numbers that the norm has left.
+__device__ __forceinline__ Consts list_consts(const UpdateArgs& a, double& clip) {
+  float c[9];
+  pt_step_consts(c, a.hp, a.st->bc1, a.st->bc2);
+  c[8] = pt_grad_mult(clip, a.hp.max_norm, a.st->s.norm, a.st->s.loss_scale);
+  return {c[0], c[1], c[2], c[3], c[4], c[5], c[6], c[7], c[8]};
+}
+
+// Largest value over the wave, in every lane.
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
+  return x;
+}
+
+constexpr float TOP8 = 448.0f, TINY8 = 0x1p-100f;        // largest number of the format; blocks of smaller ones are zero
+
+// One number in 8 bits: |x| / scale lies on the format's grid or between two of its codes; random (of 20 bits) decides.  In fp32 with the exponent
+// moved by 120 the format is the number's upper 12 bits, the steps below the smallest power of two included.
+__device__ __forceinline__ uint32_t encode8(float x, float inv, uint32_t random) {
+  const float y = fminf(__builtin_fabsf(x) * inv, TOP8);
+  const uint32_t bits = __float_as_uint(y * 0x1p-120f);
+  return min((bits + random) >> 20, 0x7eu);
+}
+
+// The update with states in 8 bits: as update_element, but every product is rounded before it is added.  A code is a threshold on m and r, and a
+// difference in their last bit turns over one in a million of them, each by 6 % or more; so the two averages are what any plain evaluation
+// in fp32 gives.
+__device__ __forceinline__ void update_element8(const Consts& k, float decay, float g, float& w, float& m, float& v, float& s) {
+  g = g * k.gm;
+  const float m1 = k.b1 * m, m2 = k.omb1 * g;
+  m = m1 + m2;
+  float v2 = k.omb2 * g;
+  v2 = v2 * g;
+  const float v1 = k.b2 * v;
+  v = v1 + v2;
+  s = __builtin_sqrtf(v);
+  const float d = __builtin_fmaf(s, k.rsb2, k.eps);
+  const float u = m / d;
+  w = __builtin_fmaf(-k.step_size, u, w * decay);
+}
+
+// BITS == 8: dequantises.  codes: four e4m3 numbers.
+__device__ __forceinline__ f32x4 decode8(uint32_t codes, float scale) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), true);
+  return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+}
+
+template <int DT, int BITS>
+__global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
+  const uint32_t lane = threadIdx.x;
+  double clip;
+  const Consts k = list_consts(a, clip);
+  const int32_t skip = a.st->s.skip;
+  const uint64_t key = a.st->key;
+  if (blockIdx.x == 0 && lane == 0) {          // what no other workgroup reads
+    a.st->applied = 1;
+    a.st->s.clip_coef = clip;
+    const float c[9] = {k.b1, k.b2, k.omb1, k.omb2, k.decay, k.step_size, k.rsb2, k.eps, k.gm};
+#pragma unroll
+    for (int j = 0; j < 9; ++j) a.st->s.c[j] = c[j];
+  }
+  if (skip) return;
+  for (uint32_t b = blockIdx.x; b < a.blocks.n; b += gridDim.x) {
+    const uint32_t t = owner(a.blocks, b);
+    const Desc d = a.desc[t];
+    const uint32_t nb = b - a.blocks.first[t];
+    const uint64_t at = uint64_t(nb) * BLOCK;
+    const uint32_t len = uint32_t(min(uint64_t(BLOCK), d.elems - at)), e = lane * 4;
+    const bool whole = len == BLOCK;
+    const float decay = d.flags & PT_TENSOR_NO_DECAY ? 1.0f : k.decay;
+    PT_GLOBAL float* pw = (PT_GLOBAL float*)d.master + at + e;
+    const PT_GLOBAL uint16_t* pg = (const PT_GLOBAL uint16_t*)d.grad + at + e;
+    const PT_GLOBAL float* pg32 = (const PT_GLOBAL float*)d.grad + at + e;
+    PT_GLOBAL uint16_t* pp = (PT_GLOBAL uint16_t*)d.param + at + e;
+    PT_GLOBAL float *pm = (PT_GLOBAL float*)d.m + at + e, *pv = (PT_GLOBAL float*)d.v + at + e;
+    PT_GLOBAL uint8_t *pm8 = (PT_GLOBAL uint8_t*)d.m + at + e, *pv8 = (PT_GLOBAL uint8_t*)d.v + at + e;
+    f32x4 w = {}, m = {}, v = {}, g = {};
+    uint32_t cm = 0, cv = 0;
+    float ms = 0.0f, vs = 0.0f;
+    if constexpr (BITS == 8) { ms = ((const PT_GLOBAL float*)d.ms)[nb]; vs = ((const PT_GLOBAL float*)d.vs)[nb]; }
+    if (whole) {
+      if (d.flags & PT_TENSOR_GRAD_F32) g = *(const PT_GLOBAL f32x4_a*)pg32;
+      else {
+        const u32x2 q = *(const PT_GLOBAL u32x2_a*)pg;
+        g = f32x4{decode16<DT>(q.x & 0xffffu), decode16<DT>(q.x >> 16), decode16<DT>(q.y & 0xffffu), decode16<DT>(q.y >> 16)};
+      }
+      w = *(const PT_GLOBAL f32x4_a*)pw;
+      if constexpr (BITS == 8) { cm = *(const PT_GLOBAL uint32_t*)pm8; cv = *(const PT_GLOBAL uint32_t*)pv8; }
+      else { m = *(const PT_GLOBAL f32x4_a*)pm; v = *(const PT_GLOBAL f32x4_a*)pv; }
+    } else {
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        if (e + j < len) {
+          g[j] = d.flags & PT_TENSOR_GRAD_F32 ? pg32[j] : decode16<DT>(pg[j]);
+          w[j] = pw[j];
+          if constexpr (BITS == 8) { cm |= uint32_t(pm8[j]) << (8 * j); cv |= uint32_t(pv8[j]) << (8 * j); }
+          else { m[j] = pm[j]; v[j] = pv[j]; }
+        }
+    }
+    if constexpr (BITS == 8) {
+      m = decode8(cm, ms);
+      v = decode8(cv, vs);
+      v = v * v;
+    }
+    float r[4];
+    uint32_t p[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float wj = w[j], mj = m[j], vj = v[j];
+      if constexpr (BITS == 8) update_element8(k, decay, g[j], wj, mj, vj, r[j]);
+      else update_element(k, decay, g[j], wj, mj, vj, r[j]);
+      w[j] = wj; m[j] = mj; v[j] = vj;
+      p[j] = encode16<DT>(wj);
+    }
+    if constexpr (BITS == 8) {
+      float bm = fmaxf(fmaxf(__builtin_fabsf(m[0]), __builtin_fabsf(m[1])), fmaxf(__builtin_fabsf(m[2]), __builtin_fabsf(m[3])));
+      float bv = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
+      bm = fminf(wave_max(bm), 3.402823466e38f);
+      bv = fminf(wave_max(bv), 3.402823466e38f);
+      const bool hm = bm >= TINY8, hv = bv >= TINY8;
+      const float im = hm ? TOP8 / bm : 0.0f, iv = hv ? TOP8 / bv : 0.0f;
+      cm = cv = 0;
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const uint64_t z = mix64((uint64_t(b) * (BLOCK / 2) + (e + j) / 2 + 1) * PHI + key);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t rm = uint32_t(z >> (32 * i)) & 0xffffu, rv = uint32_t(z >> (32 * i + 16)) & 0xffffu;
+          cm |= (encode8(m[j + i], im, rm * 16 + 8) | (m[j + i] < 0.0f ? 0x80u : 0u)) << (8 * (j + i));
+          cv |= max(encode8(r[j + i], iv, rv * 16 + 8), hv && r[j + i] > 0.0f ? 1u : 0u) << (8 * (j + i));
+        }
+      }
+      if (lane == 0) {
+        ((PT_GLOBAL float*)d.ms)[nb] = hm ? bm / TOP8 : 0.0f;
+        ((PT_GLOBAL float*)d.vs)[nb] = hv ? bv / TOP8 : 0.0f;
+      }
+    }
+    if (whole) {
+      *(PT_GLOBAL f32x4_a*)pw = w;
+      if (d.param) *(PT_GLOBAL u32x2_a*)pp = u32x2{p[0] | (p[1] << 16), p[2] | (p[3] << 16)};
+      if constexpr (BITS == 8) { *(PT_GLOBAL uint32_t*)pm8 = cm; *(PT_GLOBAL uint32_t*)pv8 = cv; }
+      else { *(PT_GLOBAL f32x4_a*)pm = m; *(PT_GLOBAL f32x4_a*)pv = v; }
+    } else {
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        if (e + j < len) {
+          pw[j] = w[j];
+          if (d.param) pp[j] = uint16_t(p[j]);
+          if constexpr (BITS == 8) { pm8[j] = uint8_t(cm >> (8 * j)); pv8[j] = uint8_t(cv >> (8 * j)); }
+          else { pm[j] = m[j]; pv[j] = v[j]; }
+        }
+    }
+  }
+}
+
+// Tables of an Index over `counts` pieces of every tensor.
+void build_index(const std::vector<uint64_t>& counts, std::vector<uint32_t>& first, std::vector<uint32_t>& coarse) {
+  first.assign(1, 0);
+  for (uint64_t c : counts) first.push_back(uint32_t(first.back() + c));
+  coarse.assign(size_t(first.back() / COARSE) + 1, 0);
+  uint32_t t = 0;
+  for (uint32_t i = 0; i < first.back(); i += COARSE) {
+    while (i >= first[t + 1]) ++t;
+    coarse[i / COARSE] = t;
+  }
+}
+
+}  // namespace
+
+struct pt_tensors {
+  int device = 0, dtype = PT_BF16, bits = 32;
+  bool scaler = false;
+  uint64_t seed = 0;
+  Index units{}, blocks{};
+  uint32_t norm_grid = 0, update_grid = 0;
+  bool open = false;                      // a norm has been taken that no update has used
+  double beta1 = 0.9, beta2 = 0.95;       // those the last norm was taken with
+  double next_beta1 = 0.9, next_beta2 = 0.95;
+  uint8_t* mem = nullptr;                 // everything below lies in it
+  ListState* st = nullptr;
+  double* part = nullptr;
+  const Desc* desc = nullptr;
+};
+
+namespace {
+
+int create(pt_tensors* l, const pt_tensor* list, uint32_t n, const pt_scaler_cfg* cfg) {
+  const char* who = "pt_tensors_create";
+  const bool q = l->bits == 8;
+  std::vector<Desc> desc;
+  std::vector<uint64_t> nb, nu;
+  uint64_t blocks = 0;
+  for (uint32_t i = 0; i < n; ++i) {
+    const pt_tensor& t = list[i];
+    if (t.flags & ~(PT_TENSOR_NO_DECAY | PT_TENSOR_GRAD_F32))
+      return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: tensor %u has unknown flags", who, i);
+    if (!t.elems) continue;                             // owns no block; its pointers are not looked at
+    if (!t.grad || !t.master || !t.m || !t.v || (q && (!t.m_scale || !t.v_scale)))
+      return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: NULL array of tensor %u", who, i);
+    const uintptr_t at32 = (uintptr_t)t.master | (uintptr_t)t.m | (uintptr_t)t.v |
+                           (q ? (uintptr_t)t.m_scale | (uintptr_t)t.v_scale : 0) | (t.flags & PT_TENSOR_GRAD_F32 ? (uintptr_t)t.grad : 0);
+    if (at32 % 4 != 0 || ((uintptr_t)t.grad | (uintptr_t)t.param16) % 2 != 0)
+      return pt_fail(nullptr, PT_ERR_ALIGNMENT, "%s: tensor %u: 16-bit arrays need 2-byte, all others 4-byte alignment", who, i);
+    desc.push_back({(uint64_t)t.grad, (uint64_t)t.master, (uint64_t)t.param16, (uint64_t)t.m, (uint64_t)t.v, (uint64_t)t.m_scale,
+                    (uint64_t)t.v_scale, t.elems, t.flags, 0});
+    if (t.elems > (uint64_t(1) << 40)) return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: tensor %u has more than 2^40 elements", who, i);
+    nb.push_back((t.elems + BLOCK - 1) / BLOCK);
+    nu.push_back((t.elems + UNIT - 1) / UNIT);
+    blocks += nb.back();
+    if (blocks > 0x7fffffffu) return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: more than 2^31 blocks of 256 elements", who);
+  }
+  std::vector<uint32_t> bf, bc, uf, uc;
+  build_index(nb, bf, bc);
+  build_index(nu, uf, uc);
+  l->blocks.n = bf.back();
+  l->units.n = uf.back();
+  l->norm_grid = std::min(NORM_BLOCKS, std::max(1u, (l->units.n + NORM_WAVES - 1) / NORM_WAVES));
+  l->update_grid = std::min(UPDATE_WAVES, std::max(1u, l->blocks.n));
+  // one allocation: state, partial sums, descriptions, tables
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  const size_t o_part = up(sizeof(ListState)), o_desc = o_part + up(NORM_BLOCKS * sizeof(double)), o_bf = o_desc + up(desc.size() * sizeof(Desc)),
+               o_bc = o_bf + up(bf.size() * 4), o_uf = o_bc + up(bc.size() * 4), o_uc = o_uf + up(uf.size() * 4), total = o_uc + up(uc.size() * 4);
+  std::vector<uint8_t> host(total, 0);
+  ListState st{};
+  st.s.clip_coef = 1.0;
+  st.s.loss_scale = cfg ? cfg->init_scale : 1.0;
+  st.s.growth = cfg ? cfg->growth : 1.0;
+  st.s.backoff = cfg ? cfg->backoff : 1.0;
+  st.s.growth_interval = cfg ? cfg->growth_interval : 1;
+  st.s.scaler_enabled = cfg ? 1 : 0;
+  std::memcpy(host.data(), &st, sizeof st);
+  if (!desc.empty()) std::memcpy(host.data() + o_desc, desc.data(), desc.size() * sizeof(Desc));
+  std::memcpy(host.data() + o_bf, bf.data(), bf.size() * 4);
+  std::memcpy(host.data() + o_bc, bc.data(), bc.size() * 4);
+  std::memcpy(host.data() + o_uf, uf.data(), uf.size() * 4);
+  std::memcpy(host.data() + o_uc, uc.data(), uc.size() * 4);
+  PT_HIP(nullptr, hipGetDevice(&l->device));
+  PT_HIP(nullptr, hipMalloc((void**)&l->mem, total));
+  PT_HIP(nullptr, hipMemcpy(l->mem, host.data(), total, hipMemcpyHostToDevice));
+  l->st = (ListState*)l->mem;
+  l->part = (double*)(l->mem + o_part);
+  l->desc = (const Desc*)(l->mem + o_desc);
+  l->blocks.first = (const uint32_t*)(l->mem + o_bf);
+  l->blocks.coarse = (const uint32_t*)(l->mem + o_bc);
+  l->units.first = (const uint32_t*)(l->mem + o_uf);
+  l->units.coarse = (const uint32_t*)(l->mem + o_uc);
+  return PT_OK;
+}
+
+}  // namespace
+
+extern "C" int pt_tensors_create(pt_tensors** out, int dtype, const pt_tensor* list, uint32_t n_tensors, int state_bits,
+                                 const pt_scaler_cfg* scaler, uint64_t seed) {
+  if (!out) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_create: out is NULL");
+  *out = nullptr;
+  if (dtype != PT_BF16 && dtype != PT_FP16)
+    return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_create: dtype %d is neither PT_BF16 nor PT_FP16", dtype);
+  if (state_bits != 8 && state_bits != 32)
+    return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_create: states have 8 or 32 bits, not %d", state_bits);
+  if (!list && n_tensors) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_create: list is NULL");
+  if (scaler && (!(scaler->init_scale >= 1.0) || !(scaler->growth >= 1.0) || !(scaler->backoff > 0.0) || !(scaler->backoff <= 1.0) ||
+                 scaler->growth_interval < 1))
+    return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_create: scaler needs init_scale >= 1, growth >= 1, 0 < backoff <= 1, "
+                   "growth_interval >= 1");
+  return pt_guarded(nullptr, "pt_tensors_create", [&] {
+    std::unique_ptr<pt_tensors> l(new pt_tensors());
+    l->dtype = dtype;
+    l->bits = state_bits;
+    l->scaler = scaler != nullptr;
+    l->seed = seed;
+    const int rc = create(l.get(), list, n_tensors, scaler);
+    if (rc != PT_OK) {
+      if (l->mem) (void)hipFree(l->mem);
+      return rc;
+    }
+    *out = l.release();
+    return int(PT_OK);
+  });
+}
+
+extern "C" int pt_tensors_destroy(pt_tensors* l) {
+  if (!l) return PT_OK;
+  (void)hipDeviceSynchronize();
+  if (l->mem) (void)hipFree(l->mem);
+  delete l;
+  return PT_OK;
+}
+
+extern "C" int pt_tensors_set_state(pt_tensors* l, int32_t step, double loss_scale, int32_t good_steps, void* stream) {
+  if (!l) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_set_state: NULL list");
+  if (step < 0 || good_steps < 0 || !(loss_scale >= 1.0))
+    return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_set_state: step, good_steps >= 0 and loss_scale >= 1 required");
+  if (!l->scaler && loss_scale != 1.0)
+    return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_set_state: list has no scaler, loss_scale must be 1");
+  hipLaunchKernelGGL(k_list_set, dim3(1), dim3(1), 0, (hipStream_t)stream, l->st, step, loss_scale, good_steps);
+  PT_LAUNCH_CHECK(nullptr, "k_list_set");
+  l->open = false;                        // a norm was taken under the old loss scale
+  return PT_OK;
+}
+
+extern "C" int pt_tensors_grad_sqnorm(pt_tensors* l, void* stream) {
+  if (!l) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_grad_sqnorm: NULL list");
+  l->beta1 = l->next_beta1;
+  l->beta2 = l->next_beta2;
+  const NormArgs a = {l->units, l->desc, l->st, l->part, l->beta1, l->beta2, l->seed};
+  hipLaunchKernelGGL(l->dtype == PT_BF16 ? k_list_norm<PT_BF16> : k_list_norm<PT_FP16>, dim3(l->norm_grid), dim3(NORM_THREADS), 0,
+                     (hipStream_t)stream, a);
+  PT_LAUNCH_CHECK(nullptr, "k_list_norm");
+  l->open = true;
+  return PT_OK;
+}
+
+extern "C" int pt_tensors_adamw_step(pt_tensors* l, const pt_hparams* hp, void* stream) {
+  if (!l || !hp) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_adamw_step: NULL argument");
+  if (!l->open)
+    return pt_fail(nullptr, PT_ERR_STATE, "pt_tensors_adamw_step: no norm has been taken since the last update (pt_tensors_grad_sqnorm)");
+  if (hp->beta1 != l->beta1 || hp->beta2 != l->beta2) {
+    hipLaunchKernelGGL(k_list_betas, dim3(1), dim3(64), 0, (hipStream_t)stream, l->st, hp->beta1, hp->beta2);
+    PT_LAUNCH_CHECK(nullptr, "k_list_betas");
+    l->next_beta1 = hp->beta1;
+    l->next_beta2 = hp->beta2;
+  }
+  const UpdateArgs a = {l->blocks, l->desc, l->st, *hp};
+  const auto kernel = l->dtype == PT_BF16 ? (l->bits == 8 ? k_list_adamw<PT_BF16, 8> : k_list_adamw<PT_BF16, 32>)
+                                          : (l->bits == 8 ? k_list_adamw<PT_FP16, 8> : k_list_adamw<PT_FP16, 32>);
+  hipLaunchKernelGGL(kernel, dim3(l->update_grid), dim3(64), 0, (hipStream_t)stream, a);
+  PT_LAUNCH_CHECK(nullptr, "k_list_adamw");
+  l->open = false;
+  return PT_OK;
+}
+
+extern "C" int pt_tensors_report_read(pt_tensors* l, pt_step_report* out, void* stream) {
+  if (!l || !out) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_tensors_report_read: NULL argument");
+  ListState h;
+  PT_HIP(nullptr, hipMemcpyAsync(&h, l->st, sizeof h, hipMemcpyDeviceToHost, (hipStream_t)stream));
+  PT_HIP(nullptr, hipStreamSynchronize((hipStream_t)stream));
+  out->sqnorm = h.s.sqnorm; out->norm = h.s.norm; out->clip_coef = h.s.clip_coef;
+  out->loss_scale = h.s.loss_scale; out->grad_mult = h.s.c[8]; out->found_inf = h.s.found_inf;
+  out->step = h.s.step; out->good_steps = h.s.good_steps;
+  // The next norm ends the step on the device; until then these are what the update leaves behind.
+  if (h.applied) {
+    const bool inf = h.s.found_inf != 0, grown = !inf && h.s.good_steps + 1 >= h.s.growth_interval;
+    out->step += inf ? 0 : 1;
+    if (h.s.scaler_enabled) {
+      out->good_steps = inf || grown ? 0 : h.s.good_steps + 1;
+      if (inf) out->loss_scale = std::max(h.s.loss_scale * h.s.backoff, 1.0);
+      if (grown) out->loss_scale = h.s.loss_scale * h.s.growth;
+    }
+  }
+  return PT_OK;
+}
