@@ -21,6 +21,12 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int BK = 64;
+#ifdef NOPRIO
+#define PRIO(x)
+#else
+#define PRIO(x) __builtin_amdgcn_s_setprio(x)
+#endif
+
 
 template <int DT>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
@@ -121,6 +127,27 @@ struct Tile {
   __device__ __forceinline__ uint32_t wave_m() const { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WM) * TM; }
   __device__ __forceinline__ uint32_t wave_n() const { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WM) * TN; }
 
+  struct Frags { s16x8 a[FM], b[FN]; };
+  __device__ __forceinline__ void read(Frags& f, const lds_char* from, uint32_t wm, uint32_t wn, int kk) const {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) f.a[i] = SP::read(from, wm + i * 16, kk);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) f.b[j] = SQ::read(from + SP::BYTES, wn + j * 16, kk);
+  }
+  __device__ __forceinline__ void multiply(const Frags& f) {
+    __builtin_amdgcn_sched_barrier(0);
+    PRIO(1);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = mfma<DT>(f.a[i], f.b[j], acc[i][j]);
+    PRIO(0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // Two steps' operands are in LDS, half a step's in registers: what a half needs is read from LDS while the half before is multiplied, and a
+  // step is fetched while the one before it is multiplied.  The workgroup meets in the middle of a step, when every wave has read the last of
+  // one buffer: that one is fetched into then, and the other one has arrived.
   __device__ __forceinline__ void run(lds_char* lds, const Operand& p, const Operand& q, uint32_t m0, uint32_t n0, uint32_t k0, uint32_t steps) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -134,28 +161,31 @@ struct Tile {
     const uint32_t wm = wave_m(), wn = wave_n();
     sp.fetch(lds, k0);
     sq.fetch(lds + SP::BYTES, k0);
+    if (steps > 1) {
+      sp.fetch(lds + BYTES, k0 + BK);
+      sq.fetch(lds + BYTES + SP::BYTES, k0 + BK);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SP::N + SQ::N) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    Frags f0, f1;
+    read(f0, lds, wm, wn, 0);
     for (uint32_t s = 0; s < steps; ++s) {
+      lds_char* here = lds + (s & 1) * BYTES;
+      lds_char* there = lds + ((s + 1) & 1) * BYTES;
+      read(f1, here, wm, wn, 1);
+      multiply(f0);
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      lds_char* here = lds + (s & 1) * BYTES;
-      if (s + 1 < steps) {
-        lds_char* there = lds + ((s + 1) & 1) * BYTES;
-        sp.fetch(there, k0 + (s + 1) * BK);
-        sq.fetch(there + SP::BYTES, k0 + (s + 1) * BK);
+      if (s + 2 < steps) {
+        sp.fetch(here, k0 + (s + 2) * BK);
+        sq.fetch(here + SP::BYTES, k0 + (s + 2) * BK);
       }
-#pragma unroll
-      for (int kk = 0; kk < BK / 32; ++kk) {
-        s16x8 a[FM], b[FN];
-#pragma unroll
-        for (int i = 0; i < FM; ++i) a[i] = SP::read(here, wm + i * 16, kk);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) b[j] = SQ::read(here + SP::BYTES, wn + j * 16, kk);
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = mfma<DT>(a[i], b[j], acc[i][j]);
-      }
+      if (s + 1 < steps) read(f0, there, wm, wn, 0);
+      multiply(f1);
     }
   }
 };

@@ -33,7 +33,8 @@ constexpr uint32_t BLOCK = 256;              // elements of a block: a wave's, a
 constexpr uint32_t UNIT = 4096;              // elements a wave of the norm takes at a time
 constexpr uint32_t COARSE = 16;              // blocks / units per entry of the look-up tables
 constexpr uint32_t NORM_THREADS = 256, NORM_BLOCKS = 1024, NORM_WAVES = NORM_THREADS / 64;
-constexpr uint32_t UPDATE_WAVES = 11 * 256;
+
+constexpr uint32_t ALIGNED = 1u << 31;       // of Desc::flags: a block's arrays begin at multiples of what a lane stores
 
 // One tensor as the kernels read it.
 struct Desc {
@@ -43,17 +44,23 @@ struct Desc {
 
 struct ListState {
   PtDevState s;
-  double bc1, bc2;       // 1 - beta^t of the update in flight
+  // of the update in flight: 1 - beta1^t and its reciprocal, 1 / sqrt(1 - beta2^t), norm + 1e-6 and 1 / it, 1 / loss scale
+  double bc1, inv_bc1, norm_eps, inv_norm, inv_scale;
+  float rsb2;
   uint64_t key;          // of its random numbers
   uint32_t applied;      // the update of the norm before has been enqueued: the next norm ends its step first
 };
 
 // Which tensor owns block or unit i: a table entry per COARSE of them says where to begin.
-struct Index { const uint32_t* first; const uint32_t* coarse; uint32_t n; };
+// Tables and descriptions are written before the first launch: loads of the scalar cache, which no store of the update holds up.
+struct Index { const PT_SCALAR uint32_t* first; const PT_SCALAR uint32_t* coarse; uint32_t n; };
 __device__ __forceinline__ uint32_t owner(const Index& x, uint32_t i) {
   uint32_t t = x.coarse[i / COARSE];
   while (i >= x.first[t + 1]) ++t;
   return t;
+}
+__device__ __forceinline__ Desc describe(const PT_SCALAR Desc* at) {
+  return {at->grad, at->master, at->param, at->m, at->v, at->ms, at->vs, at->elems, at->flags, 0};
 }
 
 __device__ __forceinline__ uint64_t mix64(uint64_t x) {
@@ -77,7 +84,7 @@ __device__ __forceinline__ void take8(const u32x4& q, double& a0, double& a1) {
 
 struct NormArgs {
   Index units;
-  const Desc* desc;
+  const PT_SCALAR Desc* desc;
   ListState* st;
   double* part;
   double beta1, beta2;
@@ -94,7 +101,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_list_norm(const NormArgs a) {
   for (uint32_t i = wave; i < a.units.n; i += gridDim.x * NORM_WAVES) {
     const uint32_t u = a.units.n - 1 - i;           // from the far end: the update, which begins at the near one, finds that in the cache
     const uint32_t t = owner(a.units, u);
-    const Desc& d = a.desc[t];
+    const Desc d = describe(a.desc + t);
     const uint64_t at = uint64_t(u - a.units.first[t]) * UNIT;
     const uint32_t len = uint32_t(min(uint64_t(UNIT), d.elems - at));
     if (d.flags & PT_TENSOR_GRAD_F32) {
@@ -143,7 +150,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_list_norm(const NormArgs a) {
   sum = 0.0;
   for (uint32_t k = threadIdx.x; k < gridDim.x; k += NORM_THREADS) sum += ld_agent(a.part + k);
   pt_block_sum(sum, none);
-  if (threadIdx.x == 1) a.st->bc2 = bc;
+  if (threadIdx.x == 1) a.st->rsb2 = float(1.0 / sqrt(bc));
   if (threadIdx.x != 0) return;
   uint32_t inf;
   double sq;
@@ -155,6 +162,10 @@ __global__ void __launch_bounds__(NORM_THREADS) k_list_norm(const NormArgs a) {
   s.ticket = 0;
   a.st->s = s;
   a.st->bc1 = bc;
+  a.st->inv_bc1 = 1.0 / bc;
+  a.st->norm_eps = s.norm + 1e-6;
+  a.st->inv_norm = 1.0 / (s.norm + 1e-6);
+  a.st->inv_scale = 1.0 / s.loss_scale;
   a.st->key = mix64(a.seed + uint64_t(uint32_t(s.step) + 1u) * PHI);
   a.st->applied = 0;
 }
@@ -163,7 +174,8 @@ __global__ void __launch_bounds__(NORM_THREADS) k_list_norm(const NormArgs a) {
 __global__ void k_list_betas(ListState* st, double beta1, double beta2) {
   if (threadIdx.x > 1) return;
   const double bc = 1.0 - pow(threadIdx.x ? beta2 : beta1, double(st->s.step + 1));
-  if (threadIdx.x) st->bc2 = bc; else st->bc1 = bc;
+  if (threadIdx.x) st->rsb2 = float(1.0 / sqrt(bc));
+  else { st->bc1 = bc; st->inv_bc1 = 1.0 / bc; }
 }
 
 __global__ void k_list_set(ListState* st, int32_t step, double loss_scale, int32_t good_steps) {
@@ -175,39 +187,58 @@ __global__ void k_list_set(ListState* st, int32_t step, double loss_scale, int32
 
 struct UpdateArgs {
   Index blocks;
-  const Desc* desc;
+  const PT_SCALAR Desc* desc;
   ListState* st;
-  pt_hparams hp;
+  double lr, max_norm;
+  float c[8];                // the constants that neither norm nor counter enter; [5], [6]: not used
 };
 
-// The nine constants of the update, in every wave from the few numbers that the norm has left.
+// a / b, correctly rounded, from inv = 1 / b correctly rounded (Markstein: one step on the remainder).
+__device__ __forceinline__ double quotient(double a, double b, double inv) {
+  const double q = a * inv;
+  return fma(fma(-q, b, a), inv, q);
+}
+
+// The nine constants of the update, in every wave, from the few numbers that the norm has left.
 __device__ __forceinline__ Consts list_consts(const UpdateArgs& a, double& clip) {
-  float c[9];
-  pt_step_consts(c, a.hp, a.st->bc1, a.st->bc2);
-  c[8] = pt_grad_mult(clip, a.hp.max_norm, a.st->s.norm, a.st->s.loss_scale);
-  return {c[0], c[1], c[2], c[3], c[4], c[5], c[6], c[7], c[8]};
+  const PT_SCALAR ListState& st = *(const PT_SCALAR ListState*)a.st;       // the norm's launch has written all that is read here
+  clip = 1.0;
+  if (a.max_norm > 0.0) {
+    const double q = quotient(a.max_norm, st.norm_eps, st.inv_norm);
+    clip = q < 1.0 ? q : 1.0;
+  }
+  return {a.c[0], a.c[1], a.c[2], a.c[3], a.c[4], float(quotient(a.lr, st.bc1, st.inv_bc1)), st.rsb2, a.c[7],
+          float(quotient(clip, st.s.loss_scale, st.inv_scale))};
 }
 
-// Largest value over the wave, in every lane.
+constexpr float TOP8 = 448.0f, TINY8 = 0x1p-100f, LOW8 = 0x1p-9f;        // largest and smallest number of the format; blocks of less than TINY8 are zero
+
+// Largest of x over the wave (of numbers >= 0), in every lane: in four steps over the 16 lanes of a row, then over the rows.
+template <int CTRL> __device__ __forceinline__ float dpp_max(float x) {
+  return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false)));
+}
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-  return x;
+  x = dpp_max<0xb1>(x);          // lane ^ 1
+  x = dpp_max<0x4e>(x);          // lane ^ 2
+  x = dpp_max<0x141>(x);         // mirrored in eight
+  x = dpp_max<0x140>(x);         // mirrored in 16
+  const int i = __float_as_int(x);
+  const float a = __int_as_float(__builtin_amdgcn_readlane(i, 0)), b = __int_as_float(__builtin_amdgcn_readlane(i, 16));
+  const float c = __int_as_float(__builtin_amdgcn_readlane(i, 32)), d = __int_as_float(__builtin_amdgcn_readlane(i, 48));
+  return fmaxf(fmaxf(a, b), fmaxf(c, d));
 }
 
-constexpr float TOP8 = 448.0f, TINY8 = 0x1p-100f;        // largest number of the format; blocks of smaller ones are zero
-
-// One number in 8 bits: |x| / scale lies on the format's grid or between two of its codes; random (of 20 bits) decides.  In fp32 with the exponent
-// moved by 120 the format is the number's upper 12 bits, the steps below the smallest power of two included.
-__device__ __forceinline__ uint32_t encode8(float x, float inv, uint32_t random) {
-  const float y = fminf(__builtin_fabsf(x) * inv, TOP8);
-  const uint32_t bits = __float_as_uint(y * 0x1p-120f);
-  return min((bits + random) >> 20, 0x7eu);
+// sqrt of a number >= 0, rounded to the nearest but for one in some millions (x of normal size): the reciprocal root is right to its last
+// place, one step on the remainder.
+__device__ __forceinline__ float root(float x) {
+  const float y = __builtin_amdgcn_rsqf(x), s = x * y;
+  const float r = __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+  return x > 0x1p-100f ? r : __builtin_sqrtf(x);
 }
 
 // The update with states in 8 bits: as update_element, but every product is rounded before it is added.  A code is a threshold on m and r, and a
 // difference in their last bit turns over one in a million of them, each by 6 % or more; so the two averages are what any plain evaluation
-// in fp32 gives.
+// in fp32 gives.  The quotient is good to two units in the last place: nothing but w depends on it.
 __device__ __forceinline__ void update_element8(const Consts& k, float decay, float g, float& w, float& m, float& v, float& s) {
   g = g * k.gm;
   const float m1 = k.b1 * m, m2 = k.omb1 * g;
@@ -216,126 +247,201 @@ __device__ __forceinline__ void update_element8(const Consts& k, float decay, fl
   v2 = v2 * g;
   const float v1 = k.b2 * v;
   v = v1 + v2;
-  s = __builtin_sqrtf(v);
+  s = root(v);
   const float d = __builtin_fmaf(s, k.rsb2, k.eps);
-  const float u = m / d;
+  const float u = m * __builtin_amdgcn_rcpf(d);
   w = __builtin_fmaf(-k.step_size, u, w * decay);
 }
 
-// BITS == 8: dequantises.  codes: four e4m3 numbers.
+// To the nearest 16-bit numbers, two an instruction.
+template <int DT>
+__device__ __forceinline__ u32x2 encode16x4(f32x4 x) {
+  if constexpr (DT == PT_BF16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
+  } else {
+    return u32x2{encode16<DT>(x[0]) | encode16<DT>(x[1]) << 16, encode16<DT>(x[2]) | encode16<DT>(x[3]) << 16};
+  }
+}
+
+// A lane's four codes; policy as pt_store.
+__device__ __forceinline__ void store_word(PT_GLOBAL uint8_t* base, uint32_t x) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)base, 0, 0xffffffffu, 0x27000);
+  __builtin_amdgcn_raw_buffer_store_b32(x, r, 4 * threadIdx.x, 0, PT_NT_THROUGH);
+}
+
+// Four e4m3 numbers.
 __device__ __forceinline__ f32x4 decode8(uint32_t codes, float scale) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), true);
   return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
 }
 
+// A block of 256 elements, four a lane, as they lie in memory.
 template <int DT, int BITS>
-__global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
-  const uint32_t lane = threadIdx.x;
-  double clip;
-  const Consts k = list_consts(a, clip);
-  const int32_t skip = a.st->s.skip;
-  const uint64_t key = a.st->key;
-  if (blockIdx.x == 0 && lane == 0) {          // what no other workgroup reads
-    a.st->applied = 1;
-    a.st->s.clip_coef = clip;
-    const float c[9] = {k.b1, k.b2, k.omb1, k.omb2, k.decay, k.step_size, k.rsb2, k.eps, k.gm};
-#pragma unroll
-    for (int j = 0; j < 9; ++j) a.st->s.c[j] = c[j];
-  }
-  if (skip) return;
-  for (uint32_t b = blockIdx.x; b < a.blocks.n; b += gridDim.x) {
+struct Block {
+  Desc d;
+  uint32_t nb, len;          // number of the block in its tensor, elements
+  f32x4 w, m, v, g32;        // m, v: of states in 32 bits; g32 or g16, as the tensor's gradient is
+  u32x2 g16;
+  uint32_t cm, cv;           // codes
+  float ms, vs;
+
+  template <class P> __device__ __forceinline__ P at(uint64_t base) const { return (P)base + uint64_t(nb) * BLOCK + threadIdx.x * 4; }
+
+  // Loads block b, with hints but for the gradient, which the norm has just read.
+  __device__ __forceinline__ void load(const UpdateArgs& a, uint32_t b) {
     const uint32_t t = owner(a.blocks, b);
-    const Desc d = a.desc[t];
-    const uint32_t nb = b - a.blocks.first[t];
-    const uint64_t at = uint64_t(nb) * BLOCK;
-    const uint32_t len = uint32_t(min(uint64_t(BLOCK), d.elems - at)), e = lane * 4;
-    const bool whole = len == BLOCK;
-    const float decay = d.flags & PT_TENSOR_NO_DECAY ? 1.0f : k.decay;
-    PT_GLOBAL float* pw = (PT_GLOBAL float*)d.master + at + e;
-    const PT_GLOBAL uint16_t* pg = (const PT_GLOBAL uint16_t*)d.grad + at + e;
-    const PT_GLOBAL float* pg32 = (const PT_GLOBAL float*)d.grad + at + e;
-    PT_GLOBAL uint16_t* pp = (PT_GLOBAL uint16_t*)d.param + at + e;
-    PT_GLOBAL float *pm = (PT_GLOBAL float*)d.m + at + e, *pv = (PT_GLOBAL float*)d.v + at + e;
-    PT_GLOBAL uint8_t *pm8 = (PT_GLOBAL uint8_t*)d.m + at + e, *pv8 = (PT_GLOBAL uint8_t*)d.v + at + e;
-    f32x4 w = {}, m = {}, v = {}, g = {};
-    uint32_t cm = 0, cv = 0;
-    float ms = 0.0f, vs = 0.0f;
-    if constexpr (BITS == 8) { ms = ((const PT_GLOBAL float*)d.ms)[nb]; vs = ((const PT_GLOBAL float*)d.vs)[nb]; }
-    if (whole) {
-      if (d.flags & PT_TENSOR_GRAD_F32) g = *(const PT_GLOBAL f32x4_a*)pg32;
-      else {
-        const u32x2 q = *(const PT_GLOBAL u32x2_a*)pg;
-        g = f32x4{decode16<DT>(q.x & 0xffffu), decode16<DT>(q.x >> 16), decode16<DT>(q.y & 0xffffu), decode16<DT>(q.y >> 16)};
+    d = describe(a.desc + t);
+    nb = b - a.blocks.first[t];
+    const uint64_t left = d.elems - uint64_t(nb) * BLOCK;
+    len = left < BLOCK ? uint32_t(left) : BLOCK;
+    const auto pw = at<const PT_GLOBAL float*>(d.master);
+    const auto pg = at<const PT_GLOBAL uint16_t*>(d.grad);
+    const auto pg32 = at<const PT_GLOBAL float*>(d.grad);
+    const auto pm = at<const PT_GLOBAL float*>(d.m), pv = at<const PT_GLOBAL float*>(d.v);
+    const auto pm8 = at<const PT_GLOBAL uint8_t*>(d.m), pv8 = at<const PT_GLOBAL uint8_t*>(d.v);
+    if (len == BLOCK) {
+      if (d.flags & PT_TENSOR_GRAD_F32) g32 = *(const PT_GLOBAL f32x4_a*)pg32;
+      else g16 = *(const PT_GLOBAL u32x2_a*)pg;
+      w = __builtin_nontemporal_load((const PT_GLOBAL f32x4_a*)pw);
+      if constexpr (BITS == 8) {
+        cm = __builtin_nontemporal_load((const PT_GLOBAL uint32_t*)pm8);
+        cv = __builtin_nontemporal_load((const PT_GLOBAL uint32_t*)pv8);
+      } else {
+        m = __builtin_nontemporal_load((const PT_GLOBAL f32x4_a*)pm);
+        v = __builtin_nontemporal_load((const PT_GLOBAL f32x4_a*)pv);
       }
-      w = *(const PT_GLOBAL f32x4_a*)pw;
-      if constexpr (BITS == 8) { cm = *(const PT_GLOBAL uint32_t*)pm8; cv = *(const PT_GLOBAL uint32_t*)pv8; }
-      else { m = *(const PT_GLOBAL f32x4_a*)pm; v = *(const PT_GLOBAL f32x4_a*)pv; }
     } else {
+      w = m = v = g32 = f32x4{};
+      g16 = u32x2{};
+      cm = cv = 0;
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j)
-        if (e + j < len) {
-          g[j] = d.flags & PT_TENSOR_GRAD_F32 ? pg32[j] : decode16<DT>(pg[j]);
+        if (threadIdx.x * 4 + j < len) {
+          if (d.flags & PT_TENSOR_GRAD_F32) g32[j] = pg32[j];
+          else g16[j / 2] |= uint32_t(pg[j]) << (16 * (j & 1));
           w[j] = pw[j];
           if constexpr (BITS == 8) { cm |= uint32_t(pm8[j]) << (8 * j); cv |= uint32_t(pv8[j]) << (8 * j); }
           else { m[j] = pm[j]; v[j] = pv[j]; }
         }
     }
+    if constexpr (BITS == 8) { ms = ((const PT_GLOBAL float*)d.ms)[nb]; vs = ((const PT_GLOBAL float*)d.vs)[nb]; }
+  }
+
+  // Updates and stores it.  counter: of the random numbers of the lane's first pair of elements.
+  __device__ __forceinline__ void finish(const Consts& k, uint64_t counter) {
+    const float decay = d.flags & PT_TENSOR_NO_DECAY ? 1.0f : k.decay;
+    f32x4 g;
+    if (d.flags & PT_TENSOR_GRAD_F32) g = g32;
+    else g = f32x4{decode16<DT>(g16.x & 0xffffu), decode16<DT>(g16.x >> 16), decode16<DT>(g16.y & 0xffffu), decode16<DT>(g16.y >> 16)};
     if constexpr (BITS == 8) {
       m = decode8(cm, ms);
       v = decode8(cv, vs);
       v = v * v;
     }
     float r[4];
-    uint32_t p[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float wj = w[j], mj = m[j], vj = v[j];
       if constexpr (BITS == 8) update_element8(k, decay, g[j], wj, mj, vj, r[j]);
       else update_element(k, decay, g[j], wj, mj, vj, r[j]);
       w[j] = wj; m[j] = mj; v[j] = vj;
-      p[j] = encode16<DT>(wj);
     }
+    const u32x2 p2 = encode16x4<DT>(w);
     if constexpr (BITS == 8) {
-      float bm = fmaxf(fmaxf(__builtin_fabsf(m[0]), __builtin_fabsf(m[1])), fmaxf(__builtin_fabsf(m[2]), __builtin_fabsf(m[3])));
-      float bv = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
-      bm = fminf(wave_max(bm), 3.402823466e38f);
-      bv = fminf(wave_max(bv), 3.402823466e38f);
+      const float bm = fminf(wave_max(fmaxf(fmaxf(__builtin_fabsf(m[0]), __builtin_fabsf(m[1])), fmaxf(__builtin_fabsf(m[2]), __builtin_fabsf(m[3])))),
+                             3.402823466e38f);
+      const float bv = fminf(wave_max(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]))), 3.402823466e38f);
       const bool hm = bm >= TINY8, hv = bv >= TINY8;
       const float im = hm ? TOP8 / bm : 0.0f, iv = hv ? TOP8 / bv : 0.0f;
-      cm = cv = 0;
-#pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        const uint64_t z = mix64((uint64_t(b) * (BLOCK / 2) + (e + j) / 2 + 1) * PHI + key);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t rm = uint32_t(z >> (32 * i)) & 0xffffu, rv = uint32_t(z >> (32 * i + 16)) & 0xffffu;
-          cm |= (encode8(m[j + i], im, rm * 16 + 8) | (m[j + i] < 0.0f ? 0x80u : 0u)) << (8 * (j + i));
-          cv |= max(encode8(r[j + i], iv, rv * 16 + 8), hv && r[j + i] > 0.0f ? 1u : 0u) << (8 * (j + i));
-        }
+      uint32_t z[4];
+      {
+        const uint64_t z0 = mix64(counter), z1 = mix64(counter + PHI);
+        z[0] = uint32_t(z0); z[1] = uint32_t(z0 >> 32); z[2] = uint32_t(z1); z[3] = uint32_t(z1 >> 32);
       }
-      if (lane == 0) {
+      int qm = 0, qv = 0;
+#define PT_CODE(j)                                                                                                                  \
+      {                                                                                                                             \
+        const float ym = __builtin_amdgcn_fmed3f(m[j] * im, -TOP8, TOP8), y = r[j] * iv;                                            \
+        const float yv = __builtin_amdgcn_fmed3f(y, y > 0.0f ? LOW8 : 0.0f, TOP8);                                                  \
+        qm = __builtin_amdgcn_cvt_sr_fp8_f32(ym, int(z[j] << 16 | 0x8000u), qm, j);                                                 \
+        qv = __builtin_amdgcn_cvt_sr_fp8_f32(yv, int((z[j] & 0xffff0000u) | 0x8000u), qv, j);                                       \
+      }
+      PT_CODE(0) PT_CODE(1) PT_CODE(2) PT_CODE(3)
+#undef PT_CODE
+      cm = uint32_t(qm); cv = uint32_t(qv);
+      if (threadIdx.x == 0) {
         ((PT_GLOBAL float*)d.ms)[nb] = hm ? bm / TOP8 : 0.0f;
         ((PT_GLOBAL float*)d.vs)[nb] = hv ? bv / TOP8 : 0.0f;
       }
     }
-    if (whole) {
-      *(PT_GLOBAL f32x4_a*)pw = w;
-      if (d.param) *(PT_GLOBAL u32x2_a*)pp = u32x2{p[0] | (p[1] << 16), p[2] | (p[3] << 16)};
-      if constexpr (BITS == 8) { *(PT_GLOBAL uint32_t*)pm8 = cm; *(PT_GLOBAL uint32_t*)pv8 = cv; }
-      else { *(PT_GLOBAL f32x4_a*)pm = m; *(PT_GLOBAL f32x4_a*)pv = v; }
-    } else {
-#pragma unroll
-      for (uint32_t j = 0; j < 4; ++j)
-        if (e + j < len) {
-          pw[j] = w[j];
-          if (d.param) pp[j] = uint16_t(p[j]);
-          if constexpr (BITS == 8) { pm8[j] = uint8_t(cm >> (8 * j)); pv8[j] = uint8_t(cv >> (8 * j)); }
-          else { pm[j] = m[j]; pv[j] = v[j]; }
-        }
+    const auto pw = at<PT_GLOBAL float*>(d.master);
+    const auto pp = at<PT_GLOBAL uint16_t*>(d.param);
+    const auto pm = at<PT_GLOBAL float*>(d.m), pv = at<PT_GLOBAL float*>(d.v);
+    const auto pm8 = at<PT_GLOBAL uint8_t*>(d.m), pv8 = at<PT_GLOBAL uint8_t*>(d.v);
+    if (len == BLOCK && (d.flags & ALIGNED)) {
+      const uint64_t e = uint64_t(nb) * BLOCK;
+      pt_store<PT_NT_THROUGH>(w, (PT_GLOBAL float*)d.master + e, 16 * threadIdx.x);
+      if (d.param) pt_store<PT_NT_THROUGH>(p2, (PT_GLOBAL uint16_t*)d.param + e, 8 * threadIdx.x);
+      if constexpr (BITS == 8) {
+        store_word((PT_GLOBAL uint8_t*)d.m + e, cm);
+        store_word((PT_GLOBAL uint8_t*)d.v + e, cv);
+      } else {
+        pt_store<PT_NT_THROUGH>(m, (PT_GLOBAL float*)d.m + e, 16 * threadIdx.x);
+        pt_store<PT_NT_THROUGH>(v, (PT_GLOBAL float*)d.v + e, 16 * threadIdx.x);
+      }
+      return;
     }
+    if (len == BLOCK) {
+      __builtin_nontemporal_store(w, (PT_GLOBAL f32x4_a*)pw);
+      if (d.param) __builtin_nontemporal_store(p2, (PT_GLOBAL u32x2_a*)pp);
+      if constexpr (BITS == 8) {
+        __builtin_nontemporal_store(cm, (PT_GLOBAL uint32_t*)pm8);
+        __builtin_nontemporal_store(cv, (PT_GLOBAL uint32_t*)pv8);
+      } else {
+        __builtin_nontemporal_store(m, (PT_GLOBAL f32x4_a*)pm);
+        __builtin_nontemporal_store(v, (PT_GLOBAL f32x4_a*)pv);
+      }
+      return;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+      if (threadIdx.x * 4 + j < len) {
+        pw[j] = w[j];
+        if (d.param) pp[j] = uint16_t(p2[j / 2] >> (16 * (j & 1)));
+        if constexpr (BITS == 8) { pm8[j] = uint8_t(cm >> (8 * j)); pv8[j] = uint8_t(cv >> (8 * j)); }
+        else { pm[j] = m[j]; pv[j] = v[j]; }
+      }
   }
+};
+
+// A wave a block, in the order of the list: as for the chunks, few bytes in flight that lie next to each other are moved fastest
+// (unused LDS keeps 11 waves on a compute unit).  With states in 8 bits a wave has little more than half the bytes and the arithmetic counts:
+// as many waves as there is room for.
+template <int DT, int BITS>
+__global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
+  const PT_SCALAR ListState* st = (const PT_SCALAR ListState*)a.st;
+  Block<DT, BITS> x;
+  x.load(a, blockIdx.x);                       // a skipped step reads in vain
+  asm volatile("" ::: "memory");
+  double clip;
+  const Consts k = list_consts(a, clip);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {   // what no other workgroup reads
+    a.st->applied = 1;
+    a.st->s.clip_coef = clip;
+    const float c[9] = {k.b1, k.b2, k.omb1, k.omb2, k.decay, k.step_size, k.rsb2, k.eps, k.gm};
+#pragma unroll
+    for (int j = 0; j < 9; ++j) a.st->s.c[j] = c[j];
+  }
+  if (st->s.skip) return;
+  x.finish(k, st->key + PHI * (uint64_t(blockIdx.x) * (BLOCK / 2) + 2 * threadIdx.x + 1));
 }
+
+// The update of a list without an element: its step has happened.
+__global__ void k_list_applied(ListState* st) { st->applied = 1; st->s.clip_coef = 1.0; }
+
+constexpr uint32_t UPDATE_LDS8 = 0, UPDATE_LDS32 = PT_ADAMW_LDS;
 
 // Tables of an Index over `counts` pieces of every tensor.
 void build_index(const std::vector<uint64_t>& counts, std::vector<uint32_t>& first, std::vector<uint32_t>& coarse) {
@@ -356,14 +462,14 @@ struct pt_tensors {
   bool scaler = false;
   uint64_t seed = 0;
   Index units{}, blocks{};
-  uint32_t norm_grid = 0, update_grid = 0;
+  uint32_t norm_grid = 0;
   bool open = false;                      // a norm has been taken that no update has used
   double beta1 = 0.9, beta2 = 0.95;       // those the last norm was taken with
   double next_beta1 = 0.9, next_beta2 = 0.95;
   uint8_t* mem = nullptr;                 // everything below lies in it
   ListState* st = nullptr;
   double* part = nullptr;
-  const Desc* desc = nullptr;
+  const PT_SCALAR Desc* desc = nullptr;
 };
 
 namespace {
@@ -386,7 +492,8 @@ int create(pt_tensors* l, const pt_tensor* list, uint32_t n, const pt_scaler_cfg
     if (at32 % 4 != 0 || ((uintptr_t)t.grad | (uintptr_t)t.param16) % 2 != 0)
       return pt_fail(nullptr, PT_ERR_ALIGNMENT, "%s: tensor %u: 16-bit arrays need 2-byte, all others 4-byte alignment", who, i);
     desc.push_back({(uint64_t)t.grad, (uint64_t)t.master, (uint64_t)t.param16, (uint64_t)t.m, (uint64_t)t.v, (uint64_t)t.m_scale,
-                    (uint64_t)t.v_scale, t.elems, t.flags, 0});
+                    (uint64_t)t.v_scale, t.elems,
+                    t.flags | (((uintptr_t)t.master | (q ? 0 : (uintptr_t)t.m | (uintptr_t)t.v)) % 16 == 0 && (uintptr_t)t.param16 % 8 == 0 ? ALIGNED : 0), 0});
     if (t.elems > (uint64_t(1) << 40)) return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: tensor %u has more than 2^40 elements", who, i);
     nb.push_back((t.elems + BLOCK - 1) / BLOCK);
     nu.push_back((t.elems + UNIT - 1) / UNIT);
@@ -399,7 +506,6 @@ int create(pt_tensors* l, const pt_tensor* list, uint32_t n, const pt_scaler_cfg
   l->blocks.n = bf.back();
   l->units.n = uf.back();
   l->norm_grid = std::min(NORM_BLOCKS, std::max(1u, (l->units.n + NORM_WAVES - 1) / NORM_WAVES));
-  l->update_grid = std::min(UPDATE_WAVES, std::max(1u, l->blocks.n));
   // one allocation: state, partial sums, descriptions, tables
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   const size_t o_part = up(sizeof(ListState)), o_desc = o_part + up(NORM_BLOCKS * sizeof(double)), o_bf = o_desc + up(desc.size() * sizeof(Desc)),
@@ -423,11 +529,11 @@ int create(pt_tensors* l, const pt_tensor* list, uint32_t n, const pt_scaler_cfg
   PT_HIP(nullptr, hipMemcpy(l->mem, host.data(), total, hipMemcpyHostToDevice));
   l->st = (ListState*)l->mem;
   l->part = (double*)(l->mem + o_part);
-  l->desc = (const Desc*)(l->mem + o_desc);
-  l->blocks.first = (const uint32_t*)(l->mem + o_bf);
-  l->blocks.coarse = (const uint32_t*)(l->mem + o_bc);
-  l->units.first = (const uint32_t*)(l->mem + o_uf);
-  l->units.coarse = (const uint32_t*)(l->mem + o_uc);
+  l->desc = (const PT_SCALAR Desc*)(l->mem + o_desc);
+  l->blocks.first = (const PT_SCALAR uint32_t*)(l->mem + o_bf);
+  l->blocks.coarse = (const PT_SCALAR uint32_t*)(l->mem + o_bc);
+  l->units.first = (const PT_SCALAR uint32_t*)(l->mem + o_uf);
+  l->units.coarse = (const PT_SCALAR uint32_t*)(l->mem + o_uc);
   return PT_OK;
 }
 
@@ -504,10 +610,13 @@ extern "C" int pt_tensors_adamw_step(pt_tensors* l, const pt_hparams* hp, void* 
     l->next_beta1 = hp->beta1;
     l->next_beta2 = hp->beta2;
   }
-  const UpdateArgs a = {l->blocks, l->desc, l->st, *hp};
+  const UpdateArgs a = {l->blocks, l->desc, l->st, hp->lr, hp->max_norm,
+                        {float(hp->beta1), float(hp->beta2), float(1.0 - hp->beta1), float(1.0 - hp->beta2),
+                         float(1.0 - hp->lr * hp->weight_decay), 0.0f, 0.0f, float(hp->eps)}};
   const auto kernel = l->dtype == PT_BF16 ? (l->bits == 8 ? k_list_adamw<PT_BF16, 8> : k_list_adamw<PT_BF16, 32>)
                                           : (l->bits == 8 ? k_list_adamw<PT_FP16, 8> : k_list_adamw<PT_FP16, 32>);
-  hipLaunchKernelGGL(kernel, dim3(l->update_grid), dim3(64), 0, (hipStream_t)stream, a);
+  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3(l->blocks.n), dim3(64), l->bits == 8 ? UPDATE_LDS8 : UPDATE_LDS32, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(k_list_applied, dim3(1), dim3(1), 0, (hipStream_t)stream, l->st);
   PT_LAUNCH_CHECK(nullptr, "k_list_adamw");
   l->open = false;
   return PT_OK;
