@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(256) k_head_gather(const uint16_t* __restrict_
   const uint32_t n = meta->count;
   PT_GLOBAL uint16_t* to = (PT_GLOBAL uint16_t*)packed + size_t(r) * s.Kd;
   if (r < n) copy_row((const PT_GLOBAL uint16_t*)hidden + row_of[r] * stride, to, s.d, s.Kd, lane, 64);
-  else if (r < (n + BK - 1) / BK * BK) {
+  else if (r < (n + TWO - 1) / TWO * TWO) {
     for (uint32_t c = lane * 8; c < s.Kd; c += 512) *(PT_GLOBAL u32x4*)(to + c) = u32x4{0, 0, 0, 0};
   }
   if (r < s.R && uint64_t(target[r]) >= s.V) {
@@ -158,7 +158,7 @@ struct LogitArgs {
 template <int DT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN) k_head_logits(const LogitArgs a) {
   typedef Tile<DT, true, true, BM, BN, WM, WN> T;
-  __shared__ __attribute__((aligned(16))) char lds[2 * T::BYTES];
+  __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   uint32_t tm, tn;
   if (!tile_of(blockIdx.x, (a.s.V + BM - 1) / BM, (n_rows + BN - 1) / BN, tm, tn)) return;
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_head_logits(const LogitArgs a)
   Operand h = a.h;
   h.extent = n_rows;
   T t;
-  t.run((lds_char*)lds, a.w, h, m0, n0, 0, (a.s.d + BK - 1) / BK);
+  t.run((lds_char*)even, (lds_char*)odd, a.w, h, m0, n0, 0, a.s.Kd / TWO);
   const uint32_t lane = threadIdx.x & 63, mb = m0 + t.wave_m() + (lane >> 4) * 4;
   // of rows m behind the vocabulary there is nothing to sum
   if (m0 + BM > a.s.V) {
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   const uint32_t r = blockIdx.x, tid = threadIdx.x, n = piece_rows(a.meta, a.first, a.rows);
-  if (r >= (n + BK - 1) / BK * BK) return;
+  if (r >= (n + TWO - 1) / TWO * TWO) return;
   PT_GLOBAL float* z = (PT_GLOBAL float*)a.z + size_t(r) * a.s.Vp;
   PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)z;
   if (r >= n) {                                            // rows up to a whole step: zero
@@ -313,14 +313,14 @@ struct GradArgs {
 template <int DT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN) k_head_d_hidden(const GradArgs a) {
   typedef Tile<DT, false, true, BM, BN, WM, WN> T;
-  __shared__ __attribute__((aligned(16))) char lds[2 * T::BYTES];
+  __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   uint32_t tm, tn;
   if (!tile_of(blockIdx.x, (a.s.d + BM - 1) / BM, (n_rows + BN - 1) / BN, tm, tn)) return;
   Operand q = a.q;
   q.extent = n_rows;
   T t;
-  t.run((lds_char*)lds, a.p, q, tm * BM, tn * BN, 0, (a.s.V + BK - 1) / BK);
+  t.run((lds_char*)even, (lds_char*)odd, a.p, q, tm * BM, tn * BN, 0, a.s.Vp / TWO);
   const uint32_t lane = threadIdx.x & 63, mb = tm * BM + t.wave_m() + (lane >> 4) * 4;
   const float down = a.meta->down;
 #pragma unroll
@@ -337,15 +337,15 @@ __global__ void __launch_bounds__(64 * WM * WN) k_head_d_hidden(const GradArgs a
 template <int DT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN) k_head_d_weight(const GradArgs a) {
   typedef Tile<DT, false, false, BM, BN, WM, WN> T;
-  __shared__ __attribute__((aligned(16))) char lds[2 * T::BYTES];
+  __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   if (!n_rows && a.read_acc && a.write_acc) return;
   uint32_t tm, tn;
   if (!tile_of(blockIdx.x, (a.s.d + BM - 1) / BM, (a.s.V + BN - 1) / BN, tm, tn)) return;
   Operand p = a.p, q = a.q;
-  p.k = q.k = (n_rows + BK - 1) / BK * BK;
+  p.k = q.k = (n_rows + TWO - 1) / TWO * TWO;
   T t;
-  t.run((lds_char*)lds, p, q, tm * BM, tn * BN, 0, p.k / BK);
+  t.run((lds_char*)even, (lds_char*)odd, p, q, tm * BM, tn * BN, 0, p.k / TWO);
   const uint32_t lane = threadIdx.x & 63, mb = tm * BM + t.wave_m() + (lane >> 4) * 4;
   const float down = a.meta->down;
 #pragma unroll
@@ -382,9 +382,9 @@ struct Plan {
 
 Plan make_plan(const pt_head& h, uint64_t rows) {
   Plan p{};
-  p.s = {h.rows, h.vocab, h.width, uint32_t(up(h.width, BK)), uint32_t(up(h.vocab, BM))};
+  p.s = {h.rows, h.vocab, h.width, uint32_t(up(h.width, TWO)), uint32_t(up(h.vocab, BM))};
   p.grads = h.d_hidden || h.d_weight;
-  p.direct = h.width % 8 == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
+  p.direct = h.width % BK == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
   p.parts = p.s.Vp / BM * WM;
   p.pitch = uint32_t(up(h.width, 4));
   p.rows = uint32_t(std::min<uint64_t>(rows, up(h.rows, PIECE_STEP)));
@@ -397,7 +397,7 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   p.row_of = take(4ull * h.rows);
   p.target_of = take(4ull * h.rows);
   p.at_target = take(4ull * p.rows);
-  p.packed = take(2ull * up(h.rows, BK) * p.s.Kd);
+  p.packed = take(2ull * up(h.rows, TWO) * p.s.Kd);
   p.weight = take(p.direct ? 0 : 2ull * h.vocab * p.s.Kd);
   p.part = take(8ull * p.rows * p.parts);
   p.z = take(p.grads ? 4ull * p.rows * p.s.Vp : 0);
@@ -432,7 +432,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   uint16_t* packed = (uint16_t*)(ws + p.packed);
   hipLaunchKernelGGL(k_head_rows, dim3(1), dim3(1024), 0, st, h.target, h.row_scale, s, meta, row_of, target_of);
   PT_LAUNCH_CHECK(nullptr, "k_head_rows");
-  hipLaunchKernelGGL(k_head_gather, dim3(uint32_t(up(s.R, BK) / 4)), dim3(256), 0, st, (const uint16_t*)h.hidden, h.hidden_stride, h.target, s, meta,
+  hipLaunchKernelGGL(k_head_gather, dim3(uint32_t(up(s.R, TWO) / 4)), dim3(256), 0, st, (const uint16_t*)h.hidden, h.hidden_stride, h.target, s, meta,
                      row_of, packed, h.loss, (uint16_t*)h.d_hidden, h.d_hidden_stride);
   PT_LAUNCH_CHECK(nullptr, "k_head_gather");
   Operand w = {h.weight, h.weight_stride * 2, 0, 0};
@@ -460,7 +460,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
       PT_LAUNCH_CHECK(nullptr, "k_head_loss");
       continue;
     }
-    hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, BK))), dim3(256), 0, st, sa);
+    hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO))), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
     const uint64_t z_pitch = 4ull * s.Vp;
     if (h.d_hidden) {

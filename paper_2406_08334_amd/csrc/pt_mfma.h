@@ -20,14 +20,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 
-constexpr int BK = 64;
-#ifdef NOPRIO
-#define PRIO(x)
-#else
-#define PRIO(x) __builtin_amdgcn_s_setprio(x)
-#endif
-
-
+constexpr int BK = 64, TWO = 2 * BK;
 template <int DT>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   if constexpr (DT == PT_BF16)
@@ -36,12 +29,13 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// One operand of a product.
+// One operand of a product.  What lies behind its m (or n) and behind its last k is loaded as zero, or as what lies between its rows where the
+// result is not used; a row that ends inside a step (k next to each other, k no multiple of 64) must be followed by zeros there.
 struct Operand {
   const void* at;
   uint64_t pitch;            // bytes from one row in memory to the next
-  uint32_t extent;           // of m (or n); what lies behind is loaded from inside and its results are not used
-  uint32_t k;                // k that may be read; the other operand is zero behind it, up to a multiple of 64
+  uint32_t extent;           // of m (or n)
+  uint32_t k;
 };
 
 // KC: k lies next to each other.
@@ -50,72 +44,54 @@ struct Stage {
   static constexpr int PER_ROW = KC ? BK / 8 : B / 8;                      // pieces of 16 bytes
   static constexpr int N = B * BK / 8 / THREADS;                           // pieces a lane fetches for a step
   static constexpr int BYTES = B * BK * 2;
-  static_assert(N >= 1, "more lanes than pieces");
-  uint64_t base;
-  uint64_t step;
-  uint32_t off[N];
-  uint32_t pitch, k;
+  static_assert(N >= 1 && THREADS % PER_ROW == 0 && THREADS / PER_ROW % (KC ? 8 : 16) == 0, "a lane's pieces lie alike in their rows");
+  uint64_t base, end, step;  // of the step to be fetched next; behind the operand's last element
+  uint32_t off, rows;        // the lane's first piece, and from there to its next one
+  uint32_t lane_at;          // where in a buffer the lane's first k of the first row of its wave lies
 
   static __device__ __forceinline__ uint32_t swizzle(uint32_t row) {
     if constexpr (KC) return row & 7;
     else return (((row & 3) | ((row >> 1) & 4)) * 2) & (PER_ROW - 1);
   }
-  __device__ __forceinline__ void init(const Operand& o, uint32_t mn0, uint32_t k0) {
-    pitch = uint32_t(o.pitch);
-    k = o.k;
+  // wave: the first row of the lane's wave, a multiple of what the wave takes (a power of two).
+  __device__ __forceinline__ void init(const Operand& o, uint32_t mn0, uint32_t k0, uint32_t wave) {
+    const uint32_t g = (threadIdx.x >> 4) & 3, l = threadIdx.x & 15;
+    if constexpr (KC) lane_at = (wave + l) * (BK * 2) + ((g ^ swizzle(l)) * 16);
+    else {
+      const uint32_t row = g * 8 + (l >> 2), c = (wave >> 3) + ((l & 3) >> 1);
+      lane_at = row * (B * 2) + ((c ^ swizzle(row)) * 16) + (l & 1) * 8;
+    }
     base = uint64_t(o.at) + (KC ? mn0 * o.pitch + uint64_t(k0) * 2 : k0 * o.pitch + uint64_t(mn0) * 2);
+    end = uint64_t(o.at) + (KC ? (o.extent - 1) * o.pitch + uint64_t(o.k) * 2 : (o.k - 1) * o.pitch + uint64_t(o.extent) * 2);
     step = KC ? BK * 2 : BK * o.pitch;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t s = threadIdx.x + i * THREADS, row = s / PER_ROW;
-      uint32_t c = (s % PER_ROW) ^ swizzle(row);
-      if constexpr (KC) off[i] = min(row, o.extent - 1 - mn0) * pitch + c * 16;
-      else {
-        if (mn0 + c * 8 >= o.extent) c = 0;
-        off[i] = row * pitch + c * 16;
-      }
-    }
+    const uint32_t row = threadIdx.x / PER_ROW, c = (threadIdx.x % PER_ROW) ^ swizzle(row);
+    off = row * uint32_t(o.pitch) + c * 16;
+    rows = THREADS / PER_ROW * uint32_t(o.pitch);
   }
-  // Fetches step k0 to `to`.
-  __device__ __forceinline__ void fetch(lds_char* to, uint32_t k0) {
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x27000);
+  // Fetches piece i of the lane's N of the step at `base` to `to`.  The hardware checks the range.
+  __device__ __forceinline__ void fetch(lds_char* to, int i) const {
+    const uint64_t left = base < end ? end - base : 0;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, left > 0xffffffffull ? 0xffffffffu : uint32_t(left), 0x27000);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (k0 + BK <= k) {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + (wave * 64 + i * THREADS) * 16), 16, off[i], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t s = threadIdx.x + i * THREADS, row = s / PER_ROW, c = (s % PER_ROW) ^ swizzle(row);
-        uint32_t o = off[i];
-        if constexpr (KC) { if (k0 + c * 8 >= k) o -= c * 16; }
-        else { if (k0 + row >= k) o -= (k0 + row - (k - 1)) * pitch; }
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + (wave * 64 + i * THREADS) * 16), 16, o, 0, 0, 0);
-      }
-    }
-    base += step;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + (wave * 64 + i * THREADS) * 16), 16, off, i * rows, 0, 0);
   }
-  // The lane's eight k (32 kk + 8 (lane / 16) on) of row mn + lane % 16.
-  static __device__ __forceinline__ s16x8 read(const lds_char* from, uint32_t mn, int kk) {
-    const uint32_t lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+  __device__ __forceinline__ void advance() { base += step; }
+  // The lane's eight k (32 kk + 8 (lane / 16) on) of row 16 i + lane % 16 of its wave's.
+  __device__ __forceinline__ s16x8 read(const lds_char* from, int i, int kk) const {
     if constexpr (KC) {
-      const uint32_t row = mn + i;
-      return *(const __attribute__((address_space(3))) s16x8*)(from + row * (BK * 2) + (((kk * 4 + g) ^ swizzle(row)) * 16));
+      return *(const __attribute__((address_space(3))) s16x8*)(from + (lane_at ^ (kk * 64)) + i * (16 * BK * 2));
     } else {
-      s16x4 h[2];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const uint32_t row = kk * 32 + g * 8 + q * 4 + (i >> 2), c = (mn >> 3) + ((i & 3) >> 1);
-        h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(from + row * (B * 2) + ((c ^ swizzle(row)) * 16) + (i & 1) * 8));
-      }
-      return __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      uint32_t flip = i * 32;
+      asm volatile("" : "+s"(flip));               // an address of every read in a register of its own would be too many
+      const lds_char* at = from + (lane_at ^ flip) + kk * (32 * B * 2);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 4 * B * 2));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
 };
 
-// The product of a tile: `steps` steps of 64 k.  lds: 2 * BYTES of it.
+// The product of a tile: `twos` times two steps of 64 k.
 template <int DT, bool PK, bool QK, int BM, int BN, int WM, int WN>
 struct Tile {
   static constexpr int THREADS = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
@@ -128,65 +104,89 @@ struct Tile {
   __device__ __forceinline__ uint32_t wave_n() const { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WM) * TN; }
 
   struct Frags { s16x8 a[FM], b[FN]; };
-  __device__ __forceinline__ void read(Frags& f, const lds_char* from, uint32_t wm, uint32_t wn, int kk) const {
-#pragma unroll
-    for (int i = 0; i < FM; ++i) f.a[i] = SP::read(from, wm + i * 16, kk);
-#pragma unroll
-    for (int j = 0; j < FN; ++j) f.b[j] = SQ::read(from + SP::BYTES, wn + j * 16, kk);
+  SP sp;
+  SQ sq;
+
+  __device__ __forceinline__ void read(Frags& f, const lds_char* from, int kk, int r) const {
+    if (r < FN) f.b[r] = sq.read(from + SP::BYTES, r, kk);
+    else f.a[r - FN] = sp.read(from, r - FN, kk);
   }
-  __device__ __forceinline__ void multiply(const Frags& f) {
+
+  // Multiplies half a step, and in between reads another half (READ) and fetches a step (FETCH): a wave issues in order, so what waits for its
+  // turn at the LDS would hold the products up if it were not spread over them.
+  template <bool READ, bool FETCH>
+  __device__ __forceinline__ void half(const Frags& now, Frags& then, const lds_char* from, int kk, lds_char* to) {
+    constexpr int READS = FM + FN, FETCHES = SP::N + SQ::N, PRODUCTS = FM * FN, PER = 3;
     __builtin_amdgcn_sched_barrier(0);
-    PRIO(1);
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int x = 0; x < PRODUCTS; ++x) {
+      acc[x / FN][x % FN] = mfma<DT>(now.a[x / FN], now.b[x % FN], acc[x / FN][x % FN]);
+      if (x % PER == PER - 1 || x + 1 == PRODUCTS) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int slot = x / PER, slots = (PRODUCTS + PER - 1) / PER;
+        const int f0 = slot, f1 = x + 1 == PRODUCTS ? (FETCHES > slots ? FETCHES : slots) : slot + 1;
+        if (FETCH)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = mfma<DT>(f.a[i], f.b[j], acc[i][j]);
-    PRIO(0);
-    __builtin_amdgcn_sched_barrier(0);
+          for (int i = f0; i < f1 && i < FETCHES; ++i) { if (i < SP::N) sp.fetch(to, i); else sq.fetch(to + SP::BYTES, i - SP::N); }
+        const int r1 = x + 1 == PRODUCTS ? READS : slot + 1;
+        if (READ)
+#pragma unroll
+          for (int r = slot; r < r1 && r < READS; ++r) read(then, from, kk, r);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  static __device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  // A step whose first half is in f0; the step after the next is fetched.
+  __device__ __forceinline__ void step(Frags& f0, Frags& f1, lds_char* now, lds_char* then) {
+    half<true, false>(f0, f1, now, 1, nullptr);
+    meet();
+    half<true, true>(f1, f0, then, 0, now);
+    sp.advance();
+    sq.advance();
+  }
+  __device__ __forceinline__ void fetch(lds_char* to) {
+#pragma unroll
+    for (int i = 0; i < SP::N; ++i) sp.fetch(to, i);
+#pragma unroll
+    for (int i = 0; i < SQ::N; ++i) sq.fetch(to + SP::BYTES, i);
+    sp.advance();
+    sq.advance();
   }
 
   // Two steps' operands are in LDS, half a step's in registers: what a half needs is read from LDS while the half before is multiplied, and a
   // step is fetched while the one before it is multiplied.  The workgroup meets in the middle of a step, when every wave has read the last of
   // one buffer: that one is fetched into then, and the other one has arrived.
-  __device__ __forceinline__ void run(lds_char* lds, const Operand& p, const Operand& q, uint32_t m0, uint32_t n0, uint32_t k0, uint32_t steps) {
+  // Steps are taken in twos, and the last two fetch two more that nothing needs: one loop without exceptions, whose sums stay in their
+  // registers.  even, odd: the buffers of even and odd steps, BYTES each, two arrays: a transposing read waits for all fetches that the compiler
+  // cannot tell from what it reads.
+  __device__ __forceinline__ void run(lds_char* even, lds_char* odd, const Operand& p, const Operand& q, uint32_t m0, uint32_t n0, uint32_t k0,
+                                      uint32_t twos) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (!steps) return;
-    SP sp;
-    SQ sq;
-    sp.init(p, m0, k0);
-    sq.init(q, n0, k0);
-    const uint32_t wm = wave_m(), wn = wave_n();
-    sp.fetch(lds, k0);
-    sq.fetch(lds + SP::BYTES, k0);
-    if (steps > 1) {
-      sp.fetch(lds + BYTES, k0 + BK);
-      sq.fetch(lds + BYTES + SP::BYTES, k0 + BK);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SP::N + SQ::N) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+    if (!twos) return;
+    sp.init(p, m0, k0, wave_m());
+    sq.init(q, n0, k0, wave_n());
+    fetch(even);
+    fetch(odd);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SP::N + SQ::N) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     Frags f0, f1;
-    read(f0, lds, wm, wn, 0);
-    for (uint32_t s = 0; s < steps; ++s) {
-      lds_char* here = lds + (s & 1) * BYTES;
-      lds_char* there = lds + ((s + 1) & 1) * BYTES;
-      read(f1, here, wm, wn, 1);
-      multiply(f0);
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (s + 2 < steps) {
-        sp.fetch(here, k0 + (s + 2) * BK);
-        sq.fetch(here + SP::BYTES, k0 + (s + 2) * BK);
-      }
-      if (s + 1 < steps) read(f0, there, wm, wn, 0);
-      multiply(f1);
+#pragma unroll
+    for (int r = 0; r < FM + FN; ++r) read(f0, even, 0, r);
+#pragma unroll 1
+    for (; twos; --twos) {
+      step(f0, f1, even, odd);
+      step(f0, f1, odd, even);
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   }
 };
 
