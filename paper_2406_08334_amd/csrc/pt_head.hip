@@ -37,34 +37,39 @@ struct Meta {
 struct Shape {
   uint32_t R, V, d;
   uint32_t Kd, Vp;           // width and vocabulary rounded up to whole steps and tiles
+  uint32_t low;              // 0, or, of few rows, how far behind a row of G what its rounding has left lies (and h once more)
 };
 
 // ---- rows ---------------------------------------------------------------------------------------------
 
-// One workgroup lists the rows that have a target, in order.
-__global__ void __launch_bounds__(1024) k_head_rows(const int64_t* __restrict__ target, const float* __restrict__ scale, Shape s, Meta* __restrict__ meta,
-                                                    uint32_t* __restrict__ row_of, uint32_t* __restrict__ target_of) {
-  __shared__ uint32_t s_n[16];
-  __shared__ float s_big[16];
+// The rows that have a target, in order, by a workgroup of THREADS.
+struct RowArgs {
+  const int64_t* target;
+  const float* scale;
+  Shape s;
+  Meta* meta;
+  uint32_t *row_of, *target_of;
+};
+template <int THREADS, class F>
+__device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& each) {
+  constexpr uint32_t WAVES = THREADS / 64;
+  __shared__ uint32_t s_n[WAVES];
+  __shared__ float s_big[WAVES];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t n = 0;
   float big = 0.0f;
-  for (uint32_t r0 = 0; r0 < s.R; r0 += 1024) {
+  for (uint32_t r0 = 0; r0 < a.s.R; r0 += THREADS) {
     const uint32_t r = r0 + threadIdx.x;
-    const int64_t y = r < s.R ? target[r] : -1;
-    const bool has = uint64_t(y) < s.V;
-    if (has) big = fmaxf(big, scale ? __builtin_fabsf(scale[r]) : 1.0f);
+    const int64_t y = r < a.s.R ? a.target[r] : -1;
+    const bool has = uint64_t(y) < a.s.V;
+    if (has) big = fmaxf(big, a.scale ? __builtin_fabsf(a.scale[r]) : 1.0f);
     const uint64_t mask = __ballot(has);
     if (lane == 0) s_n[wave] = uint32_t(__popcll(mask));
     __syncthreads();
     uint32_t before = 0, all = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < 16; ++w) { const uint32_t k = s_n[w]; before += w < wave ? k : 0; all += k; }
-    if (has) {
-      const uint32_t at = n + before + uint32_t(__popcll(mask & ((uint64_t(1) << lane) - 1)));
-      row_of[at] = r;
-      target_of[at] = uint32_t(y);
-    }
+    for (uint32_t w = 0; w < WAVES; ++w) { const uint32_t k = s_n[w]; before += w < wave ? k : 0; all += k; }
+    if (has) each(n + before + uint32_t(__popcll(mask & ((uint64_t(1) << lane) - 1))), r, uint32_t(y));
     n += all;
     __syncthreads();
   }
@@ -72,13 +77,19 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int64_t* __restrict__ 
   for (int off = 32; off > 0; off >>= 1) big = fmaxf(big, __shfl_xor(big, off, 64));
   if (lane == 0) s_big[wave] = big;
   __syncthreads();
-  if (threadIdx.x != 0) return;
 #pragma unroll
-  for (int w = 1; w < 16; ++w) big = fmaxf(big, s_big[w]);
+  for (uint32_t w = 0; w < WAVES; ++w) big = fmaxf(big, s_big[w]);
   int e = 0;
   if (big > 0.0f && big < 3.4e38f) (void)frexpf(big, &e);       // big < 2^e
   e = max(-100, min(100, 14 - e));
-  *meta = {n, ldexpf(1.0f, e), ldexpf(1.0f, -e)};
+  found = {n, ldexpf(1.0f, e), ldexpf(1.0f, -e)};
+}
+
+// One workgroup lists the rows of a call.
+__global__ void __launch_bounds__(1024) k_head_rows(const RowArgs a) {
+  Meta m;
+  list_rows<1024>(a, m, [&](uint32_t at, uint32_t r, uint32_t y) { a.row_of[at] = r; a.target_of[at] = y; });
+  if (threadIdx.x == 0) *a.meta = m;
 }
 
 // One row of 16-bit words, at any address, into one of Kd words that begins at a multiple of 16 bytes; zero behind its end.
@@ -95,17 +106,37 @@ __device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOB
 }
 
 // A wave a row: the hidden states of the rows with a target, zero rows up to a whole step behind them, and nothing for those without one.
-__global__ void __launch_bounds__(256) k_head_gather(const uint16_t* __restrict__ hidden, uint64_t stride, const int64_t* __restrict__ target, Shape s,
-                                                     const Meta* __restrict__ meta, const uint32_t* __restrict__ row_of, uint16_t* __restrict__ packed,
+// LIST: every workgroup lists the rows by itself, of which there are LISTED at most: a launch less, 4 us.
+constexpr uint32_t LISTED = 1024;
+template <bool LIST>
+__global__ void __launch_bounds__(256) k_head_gather(const RowArgs a, const uint16_t* __restrict__ hidden, uint64_t stride, uint16_t* __restrict__ packed,
                                                      float* __restrict__ loss, uint16_t* __restrict__ d_hidden, uint64_t d_stride) {
+  __shared__ uint32_t s_row[LIST ? LISTED : 1];
   const uint32_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const uint32_t n = meta->count;
-  PT_GLOBAL uint16_t* to = (PT_GLOBAL uint16_t*)packed + size_t(r) * s.Kd;
-  if (r < n) copy_row((const PT_GLOBAL uint16_t*)hidden + row_of[r] * stride, to, s.d, s.Kd, lane, 64);
-  else if (r < (n + TWO - 1) / TWO * TWO) {
-    for (uint32_t c = lane * 8; c < s.Kd; c += 512) *(PT_GLOBAL u32x4*)(to + c) = u32x4{0, 0, 0, 0};
+  const Shape& s = a.s;
+  uint32_t n, from = 0;
+  if constexpr (LIST) {
+    Meta m;
+    list_rows<256>(a, m, [&](uint32_t at, uint32_t row, uint32_t y) {
+      s_row[at] = row;
+      if (blockIdx.x == 0) { a.row_of[at] = row; a.target_of[at] = y; }
+    });
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.meta = m;
+    n = m.count;
+    if (r < n) from = s_row[r];
+  } else {
+    n = a.meta->count;
+    if (r < n) from = a.row_of[r];
   }
-  if (r < s.R && uint64_t(target[r]) >= s.V) {
+  const uint32_t zeros = s.low ? s.low : (n + TWO - 1) / TWO * TWO;
+  for (uint32_t at = r; at < zeros + s.low && r < zeros; at += s.low) {          // once, or twice
+    PT_GLOBAL uint16_t* to = (PT_GLOBAL uint16_t*)packed + size_t(at) * s.Kd;
+    if (r < n) copy_row((const PT_GLOBAL uint16_t*)hidden + from * stride, to, s.d, s.Kd, lane, 64);
+    else
+      for (uint32_t c = lane * 8; c < s.Kd; c += 512) *(PT_GLOBAL u32x4*)(to + c) = u32x4{0, 0, 0, 0};
+    if (!s.low) break;
+  }
+  if (r < s.R && uint64_t(a.target[r]) >= s.V) {
     if (lane == 0) loss[r] = 0.0f;
     if (d_hidden)
       for (uint32_t c = lane; c < s.d; c += 64) d_hidden[r * d_stride + c] = 0;
@@ -124,6 +155,27 @@ __global__ void __launch_bounds__(256) k_head_zero(uint16_t* __restrict__ d_weig
 }
 
 // ---- products ------------------------------------------------------------------------------------------
+
+// Tiles of the products and how their waves lie in them.  `SLOTS` of them run at a time, TWO_NS is what two steps of them take then (measured), and
+// PART_NS what a tile of partial sums costs that is written and read once more.
+template <int BM_, int BN_, int WM_, int WN_, int SLOTS_, int TWO_NS_> struct Cfg {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, THREADS = 64 * WM_ * WN_, SLOTS = SLOTS_, TWO_NS = TWO_NS_, PART_NS = BM_ * BN_ / 625;
+  template <int DT, bool PK, bool QK> using Of = Tile<DT, PK, QK, BM_, BN_, WM_, WN_>;
+};
+typedef Cfg<256, 256, 2, 4, 256, 1700> Big;
+typedef Cfg<128, 128, 2, 2, 512, 1100> Mid;
+typedef Cfg<128, 64, 4, 1, 768, 900> Few;      // up to 64 rows
+
+// Workgroups that share the k of a tile: as many as finish first, the sums that they leave to be added counted in.
+template <class C> __host__ __device__ inline uint32_t shares(uint32_t tiles, uint32_t twos) {
+  uint32_t best = 1, least = 0xffffffffu;
+  for (uint32_t n : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
+    if (n > 1 && n * 2 > twos) break;
+    const uint32_t ns = (tiles * n + C::SLOTS - 1) / C::SLOTS * ((twos + n - 1) / n * C::TWO_NS + 3000) + (n > 1 ? tiles * n * C::PART_NS + 4000 : 0);
+    if (ns < least) { least = ns; best = n; }
+  }
+  return best;
+}
 
 // Tile `id` of tm x tn: the XCDs, which workgroups go to in turn, get tiles next to each other, in patches of a few n.
 __device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
@@ -155,21 +207,21 @@ struct LogitArgs {
   float* z;                  // [rows][Vp], or NULL
 };
 
-template <int DT, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) k_head_logits(const LogitArgs a) {
-  typedef Tile<DT, true, true, BM, BN, WM, WN> T;
+template <int DT, class C>
+__global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
+  typedef typename C::template Of<DT, true, true> T;
   __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   uint32_t tm, tn;
-  if (!tile_of(blockIdx.x, (a.s.V + BM - 1) / BM, (n_rows + BN - 1) / BN, tm, tn)) return;
-  const uint32_t m0 = tm * BM, n0 = tn * BN;
+  if (!tile_of(blockIdx.x, (a.s.V + C::BM - 1) / C::BM, (n_rows + C::BN - 1) / C::BN, tm, tn)) return;
+  const uint32_t m0 = tm * C::BM, n0 = tn * C::BN;
   Operand h = a.h;
   h.extent = n_rows;
   T t;
   t.run((lds_char*)even, (lds_char*)odd, a.w, h, m0, n0, 0, a.s.Kd / TWO);
   const uint32_t lane = threadIdx.x & 63, mb = m0 + t.wave_m() + (lane >> 4) * 4;
   // of rows m behind the vocabulary there is nothing to sum
-  if (m0 + BM > a.s.V) {
+  if (m0 + C::BM > a.s.V) {
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
@@ -182,6 +234,9 @@ __global__ void __launch_bounds__(64 * WM * WN) k_head_logits(const LogitArgs a)
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = n0 + t.wave_n() + j * 16 + (lane & 15);
     const bool live = n < n_rows;
+    if (a.z && live)
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i) *(PT_GLOBAL f32x4*)((PT_GLOBAL float*)a.z + size_t(n) * a.s.Vp + mb + i * 16) = t.acc[i][j];
     float big = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
@@ -189,25 +244,25 @@ __global__ void __launch_bounds__(64 * WM * WN) k_head_logits(const LogitArgs a)
       for (int q = 0; q < 4; ++q) big = fmaxf(big, t.acc[i][j][q]);
     big = fmaxf(big, __shfl_xor(big, 16, 64));
     big = fmaxf(big, __shfl_xor(big, 32, 64));
-    const float top = big == -__builtin_inff() ? 0.0f : big;          // of nothing but -inf the sum is 0
+    const float top = big == -__builtin_inff() ? 0.0f : big * LOG2E;          // of nothing but -inf the sum is 0
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f((t.acc[i][j][q] - top) * LOG2E);
+      for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][q], LOG2E, -top));
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    if (live && lane < 16) a.part[size_t(n) * a.parts + tm * WM + t.wave_m() / T::TM] = f32x2{big, sum};
+    if (live && lane < 16) a.part[size_t(n) * a.parts + tm * C::WM + t.wave_m() / T::TM] = f32x2{big, sum};
     const uint32_t y = live ? a.target_of[n] - mb : ~0u;              // the lane's z are mb + 16 i + q
-    float zy = 0.0f;
+    const bool mine = y < uint32_t(T::TM) && (y & 15) < 4;
+    if (__any(mine)) {
+      float zy = 0.0f;
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i)
+      for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) zy = y == uint32_t(i * 16 + q) ? t.acc[i][j][q] : zy;
-    if (y < uint32_t(T::TM) && (y & 15) < 4) a.at_target[n] = zy;
-    if (a.z && live)
-#pragma unroll
-      for (int i = 0; i < T::FM; ++i) *(PT_GLOBAL f32x4*)((PT_GLOBAL float*)a.z + size_t(n) * a.s.Vp + mb + i * 16) = t.acc[i][j];
+        for (int q = 0; q < 4; ++q) zy = y == uint32_t(i * 16 + q) ? t.acc[i][j][q] : zy;
+      if (mine) a.at_target[n] = zy;
+    }
   }
 }
 
@@ -234,6 +289,7 @@ struct SoftArgs {
   const float* scale;
   float* loss;
   float* z;
+  float* rest;               // [rows]: of G at the target, what its rounding has left
 };
 
 // The loss alone: a wave a row.
@@ -246,15 +302,36 @@ __global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
   if (lane == 0) a.loss[a.row_of[r]] = x[0] + logf(x[1]) - a.at_target[r];
 }
 
-// Loss and G of a row by a workgroup: the row's z lie where its G goes, which is half as long.
+// Eight numbers in 16 bits, and what is left of them.
+template <int DT>
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
+  u32x4 q;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) q[j] = encode16<DT>(x[2 * j]) | encode16<DT>(x[2 * j + 1]) << 16;
+  return q;
+}
+template <int DT>
+__device__ __forceinline__ u32x4 pack8_rest(const float (&x)[8], const u32x4& q) {
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = x[j] - decode16<DT>((q[j / 2] >> (16 * (j & 1))) & 0xffffu);
+  return pack8<DT>(y);
+}
+
+// Loss and G of a row by a workgroup: the row's z lie where its G goes, which is half as long.  Each round takes 2048 z; a lane has its own of the
+// next round under way while it stores those of this one, and stores when every lane has this round's.
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   const uint32_t r = blockIdx.x, tid = threadIdx.x, n = piece_rows(a.meta, a.first, a.rows);
-  if (r >= (n + TWO - 1) / TWO * TWO) return;
+  if (r >= (a.s.low ? a.s.low : (n + TWO - 1) / TWO * TWO)) return;
   PT_GLOBAL float* z = (PT_GLOBAL float*)a.z + size_t(r) * a.s.Vp;
   PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)z;
+  PT_GLOBAL uint16_t* g_low = (PT_GLOBAL uint16_t*)(z + size_t(a.s.low) * a.s.Vp);
   if (r >= n) {                                            // rows up to a whole step: zero
-    for (uint32_t c = tid * 8; c < a.s.Vp; c += 2048) *(PT_GLOBAL u32x4*)(g + c) = u32x4{0, 0, 0, 0};
+    for (uint32_t c = tid * 8; c < a.s.Vp; c += 2048) {
+      *(PT_GLOBAL u32x4*)(g + c) = u32x4{0, 0, 0, 0};
+      if (a.s.low) *(PT_GLOBAL u32x4*)(g_low + c) = u32x4{0, 0, 0, 0};
+    }
     return;
   }
   __shared__ f32x2 s_x[4];
@@ -266,21 +343,34 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   x = join(join(s_x[0], s_x[1]), join(s_x[2], s_x[3]));
   const uint32_t row = a.row_of[r], y = a.target_of[r];
   const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * a.meta->up;
-  if (tid == 0) a.loss[row] = lse - zy;
   const float off = lse * LOG2E, gy = s * expm1f(zy - lse);
-  for (uint32_t c0 = 0; c0 < a.s.Vp; c0 += 2048) {
-    const uint32_t c = c0 + tid * 8;
-    f32x4 q[2] = {};
-    if (c < a.s.Vp) { q[0] = *(PT_GLOBAL f32x4*)(z + c); q[1] = *(PT_GLOBAL f32x4*)(z + c + 4); }
-    uint32_t w[8];
+  if (tid == 0) {
+    a.loss[row] = lse - zy;
+    a.rest[r] = gy - decode16<DT>(encode16<DT>(gy));
+  }
+  const uint32_t last = a.s.Vp - 8;                        // lanes behind the row's end load its last ones, and store nothing
+  f32x4 q[2], next[2];
+  uint32_t c = tid * 8, at = min(c, last);
+  q[0] = *(PT_GLOBAL f32x4*)(z + at); q[1] = *(PT_GLOBAL f32x4*)(z + at + 4);
+  for (; c < a.s.Vp + tid * 8; c += 2048) {
+    at = min(c + 2048, last);
+    next[0] = *(PT_GLOBAL f32x4*)(z + at); next[1] = *(PT_GLOBAL f32x4*)(z + at + 4);
+    float p[8];
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
-      float p = s * __builtin_amdgcn_exp2f(__builtin_fmaf(q[j / 4][j % 4], LOG2E, -off));
-      if (c + j == y) p = gy;
-      w[j] = c + j < a.s.V ? encode16<DT>(p) : 0u;
+      p[j] = s * __builtin_amdgcn_exp2f(__builtin_fmaf(q[j / 4][j % 4], LOG2E, -off));
+      if (c + j == y) p[j] = gy;
+      if (c + j >= a.s.V) p[j] = 0.0f;
     }
-    __syncthreads();                                       // every lane has its z of this round and of those before
-    if (c < a.s.Vp) *(PT_GLOBAL u32x4*)(g + c) = u32x4{w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16};
+    const u32x4 w = pack8<DT>(p);
+    asm volatile("" : : "v"(w) : "memory");                // this round's z are in registers
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (c < a.s.Vp) {
+      *(PT_GLOBAL u32x4*)(g + c) = w;
+      if (a.s.low) *(PT_GLOBAL u32x4*)(g_low + c) = pack8_rest<DT>(p, w);
+    }
+    q[0] = next[0]; q[1] = next[1];
   }
 }
 
@@ -300,57 +390,106 @@ struct GradArgs {
   Operand p, q;
   const Meta* meta;
   uint32_t first, rows;
-  const uint32_t* row_of;    // of the piece
+  const uint32_t *row_of, *target_of;      // of the piece
   uint16_t* out;
   uint64_t stride;
   bool wide;                 // four results may be stored at once
+  uint32_t pitch;            // of the sums below
+  float* part;               // d_hidden by several workgroups a tile: [shares][rows][pitch]
+  const float* rest;
+  const uint16_t* weight;
+  uint64_t weight_stride;
   float* acc;                // d_weight over several pieces: sums so far [V][pitch]
-  uint32_t pitch;
   bool read_acc, write_acc;
 };
 
+// G at the target has been rounded like the rest of its row, of which it can be the only number that counts: what that has left, times the target's
+// row of the weight, goes into the sum in fp32.
+template <int DT>
+__device__ __forceinline__ f32x4 add_rest(f32x4 x, float rest, const PT_GLOBAL uint16_t* w, uint32_t m, uint32_t d) {
+  if (m >= d) return x;
+  const u32x2 q = *(const PT_GLOBAL u32x2*)(w + m);        // the rows that the products take are whole pieces of 16 bytes
+  const float v[4] = {decode16<DT>(q.x & 0xffffu), decode16<DT>(q.x >> 16), decode16<DT>(q.y & 0xffffu), decode16<DT>(q.y >> 16)};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(rest, v[j], x[j]);
+  return x;
+}
+
 // d_hidden of a piece: m runs over the width, n over rows, k over the vocabulary.
-template <int DT, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) k_head_d_hidden(const GradArgs a) {
-  typedef Tile<DT, false, true, BM, BN, WM, WN> T;
+template <int DT, class C>
+__global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) {
+  typedef typename C::template Of<DT, false, true> T;
   __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
+  const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM, tiles_n = (n_rows + C::BN - 1) / C::BN, twos = a.s.Vp / TWO;
+  const uint32_t share = shares<C>(tiles_m * tiles_n, twos);
   uint32_t tm, tn;
-  if (!tile_of(blockIdx.x, (a.s.d + BM - 1) / BM, (n_rows + BN - 1) / BN, tm, tn)) return;
+  if (!tile_of(blockIdx.x, tiles_m * share, tiles_n, tm, tn)) return;
+  const uint32_t part = tm / tiles_m, t0 = uint32_t(uint64_t(twos) * part / share), t1 = uint32_t(uint64_t(twos) * (part + 1) / share);
+  tm -= part * tiles_m;
   Operand q = a.q;
   q.extent = n_rows;
   T t;
-  t.run((lds_char*)even, (lds_char*)odd, a.p, q, tm * BM, tn * BN, 0, a.s.Vp / TWO);
-  const uint32_t lane = threadIdx.x & 63, mb = tm * BM + t.wave_m() + (lane >> 4) * 4;
+  t.run((lds_char*)even, (lds_char*)odd, a.p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+  const uint32_t lane = threadIdx.x & 63, mb = tm * C::BM + t.wave_m() + (lane >> 4) * 4;
   const float down = a.meta->down;
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
-    const uint32_t n = tn * BN + t.wave_n() + j * 16 + (lane & 15);
+    const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
     if (n >= n_rows) continue;
-    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
+    if (share > 1) {
+      PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.rows + n) * a.pitch;
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i) store4<DT>(row, mb + i * 16, a.s.d, a.wide, t.acc[i][j] * down);
+      for (int i = 0; i < T::FM; ++i)
+        if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
+      continue;
+    }
+    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
+    const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[n] * a.weight_stride;
+    const float rest = a.rest[n];
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+      const uint32_t m = mb + i * 16;
+      store4<DT>(row, m, a.s.d, a.wide, add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down);
+    }
+  }
+}
+
+// Adds up what several workgroups a tile have left: a workgroup a row.
+template <int DT, class C>
+__global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
+  const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows), n = blockIdx.x;
+  if (n >= n_rows) return;
+  const uint32_t share = shares<C>((a.s.d + C::BM - 1) / C::BM * ((n_rows + C::BN - 1) / C::BN), a.s.Vp / TWO);
+  if (share == 1) return;
+  PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
+  const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[n] * a.weight_stride;
+  const float rest = a.rest[n], down = a.meta->down;
+  for (uint32_t m = threadIdx.x * 4; m < a.s.d; m += 1024) {
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t k = 0; k < share; ++k) x += *(const PT_GLOBAL f32x4*)((const PT_GLOBAL float*)a.part + (size_t(k) * a.rows + n) * a.pitch + m);
+    store4<DT>(row, m, a.s.d, a.wide, add_rest<DT>(x, rest, w, m, a.s.d) * down);
   }
 }
 
 // d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
-template <int DT, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) k_head_d_weight(const GradArgs a) {
-  typedef Tile<DT, false, false, BM, BN, WM, WN> T;
+template <int DT, class C>
+__global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) {
+  typedef typename C::template Of<DT, false, false> T;
   __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   if (!n_rows && a.read_acc && a.write_acc) return;
   uint32_t tm, tn;
-  if (!tile_of(blockIdx.x, (a.s.d + BM - 1) / BM, (a.s.V + BN - 1) / BN, tm, tn)) return;
+  if (!tile_of(blockIdx.x, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
   Operand p = a.p, q = a.q;
-  p.k = q.k = (n_rows + TWO - 1) / TWO * TWO;
+  p.k = q.k = !n_rows ? 0 : a.s.low ? 2 * a.s.low : (n_rows + TWO - 1) / TWO * TWO;
   T t;
-  t.run((lds_char*)even, (lds_char*)odd, p, q, tm * BM, tn * BN, 0, p.k / TWO);
-  const uint32_t lane = threadIdx.x & 63, mb = tm * BM + t.wave_m() + (lane >> 4) * 4;
+  t.run((lds_char*)even, (lds_char*)odd, p, q, tm * C::BM, tn * C::BN, 0, p.k / TWO);
+  const uint32_t lane = threadIdx.x & 63, mb = tm * C::BM + t.wave_m() + (lane >> 4) * 4;
   const float down = a.meta->down;
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
-    const uint32_t n = tn * BN + t.wave_n() + j * 16 + (lane & 15);
+    const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
     if (n >= a.s.V) continue;
     PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + n * a.stride;
 #pragma unroll
@@ -368,7 +507,14 @@ __global__ void __launch_bounds__(64 * WM * WN) k_head_d_weight(const GradArgs a
 
 // ---- host -----------------------------------------------------------------------------------------------
 
-constexpr uint32_t BM = 256, BN = 256, WM = 2, WN = 4, THREADS = 64 * WM * WN;
+// Up to this many rows the gradient of the weight is a matter of writing it: what rounding G has left is multiplied as well, as rows of its own.
+constexpr uint32_t LOW_ROWS = 256, FEW_ROWS = 64;
+
+// Whether a product of m x n is sooner done in tiles of Mid.
+inline bool mid_tiles(uint64_t m, uint64_t n) {
+  const auto rounds = [&](uint64_t bm, uint64_t bn, uint64_t slots) { return ((m + bm - 1) / bm * ((n + bn - 1) / bn) + slots - 1) / slots; };
+  return rounds(Mid::BM, Mid::BN, Mid::SLOTS) * Mid::TWO_NS < rounds(Big::BM, Big::BN, Big::SLOTS) * Big::TWO_NS;
+}
 
 uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
@@ -377,15 +523,39 @@ struct Plan {
   Shape s;
   uint32_t parts, pitch, pieces, rows;
   bool grads, direct;                      // direct: the weight is taken where it lies
-  uint64_t meta, row_of, target_of, at_target, packed, weight, part, z, acc, total;
+  uint32_t shared;                         // rows times workgroups a tile of d_hidden, at most
+  uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, sums, acc, total;
 };
+
+// Partial sums of a row's exponentials.
+template <class C> uint32_t parts(uint32_t vocab) { return (vocab + C::BM - 1) / C::BM * C::WM; }
+
+// The most rows times workgroups, and the most workgroups, of d_hidden for any number of rows up to `rows` that turns out to have a target.
+template <class C> void most_shared(const Shape& s, uint32_t rows, uint32_t& shared, uint32_t& grid) {
+  shared = grid = 0;
+  const uint32_t tm = (s.d + C::BM - 1) / C::BM;
+  for (uint32_t tn = 1; tn <= (rows + C::BN - 1) / C::BN; ++tn) {
+    const uint32_t n = shares<C>(tm * tn, s.Vp / TWO);
+    if (n > 1) shared = std::max(shared, n * rows);
+    grid = std::max(grid, tile_grid(uint64_t(tm) * n, tn));
+  }
+}
+
+uint32_t shared_rows(const Shape& s, uint32_t rows) {
+  uint32_t shared, grid;
+  if (rows <= FEW_ROWS) most_shared<Few>(s, rows, shared, grid);
+  else if (mid_tiles(s.d, rows)) most_shared<Mid>(s, rows, shared, grid);
+  else most_shared<Big>(s, rows, shared, grid);
+  return shared;
+}
 
 Plan make_plan(const pt_head& h, uint64_t rows) {
   Plan p{};
-  p.s = {h.rows, h.vocab, h.width, uint32_t(up(h.width, TWO)), uint32_t(up(h.vocab, BM))};
+  p.s = {h.rows, h.vocab, h.width, uint32_t(up(h.width, TWO)), uint32_t(up(h.vocab, 256)), 0};
+  if (h.d_weight && h.rows <= LOW_ROWS) p.s.low = uint32_t(up(h.rows, BK));
   p.grads = h.d_hidden || h.d_weight;
   p.direct = h.width % BK == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
-  p.parts = p.s.Vp / BM * WM;
+  p.parts = std::max({parts<Few>(h.vocab), parts<Mid>(h.vocab), parts<Big>(h.vocab)});
   p.pitch = uint32_t(up(h.width, 4));
   p.rows = uint32_t(std::min<uint64_t>(rows, up(h.rows, PIECE_STEP)));
   p.pieces = (h.rows + p.rows - 1) / p.rows;
@@ -397,10 +567,14 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   p.row_of = take(4ull * h.rows);
   p.target_of = take(4ull * h.rows);
   p.at_target = take(4ull * p.rows);
-  p.packed = take(2ull * up(h.rows, TWO) * p.s.Kd);
+  p.rest = take(p.grads ? 4ull * p.rows : 0);
+  p.packed = take(2ull * (up(h.rows, TWO) + p.s.low) * p.s.Kd);
   p.weight = take(p.direct ? 0 : 2ull * h.vocab * p.s.Kd);
   p.part = take(8ull * p.rows * p.parts);
-  p.z = take(p.grads ? 4ull * p.rows * p.s.Vp : 0);
+  p.z = take(p.grads ? 4ull * (p.rows + p.s.low) * p.s.Vp : 0);
+  if (h.d_hidden)                            // of a whole piece and of the last one
+    for (uint32_t rows : {std::min(p.rows, h.rows), h.rows - (p.pieces - 1) * p.rows}) p.shared = std::max(p.shared, shared_rows(p.s, rows));
+  p.sums = take(4ull * p.shared * p.pitch);
   p.acc = take(h.d_weight && p.pieces > 1 ? 4ull * h.vocab * p.pitch : 0);
   p.total = at;
   return p;
@@ -424,37 +598,68 @@ int check(const pt_head* h, const char* who) {
   return PT_OK;
 }
 
+// Launches.
+template <int DT, class C> int logits(const LogitArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_head_logits<DT, C>), dim3(tile_grid((a.s.V + C::BM - 1) / C::BM, (a.rows + C::BN - 1) / C::BN)), dim3(C::THREADS), 0, st, a);
+  PT_LAUNCH_CHECK(nullptr, "k_head_logits");
+  return PT_OK;
+}
+template <int DT, class C> int d_hidden(const GradArgs& a, hipStream_t st) {
+  uint32_t shared, grid;
+  most_shared<C>(a.s, a.rows, shared, grid);
+  hipLaunchKernelGGL((k_head_d_hidden<DT, C>), dim3(grid), dim3(C::THREADS), 0, st, a);
+  PT_LAUNCH_CHECK(nullptr, "k_head_d_hidden");
+  if (!shared) return PT_OK;
+  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(a.rows), dim3(256), 0, st, a);
+  PT_LAUNCH_CHECK(nullptr, "k_head_join");
+  return PT_OK;
+}
+template <int DT, class C> int d_weight(const GradArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_head_d_weight<DT, C>), dim3(tile_grid((a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN)), dim3(C::THREADS), 0, st, a);
+  PT_LAUNCH_CHECK(nullptr, "k_head_d_weight");
+  return PT_OK;
+}
+
 template <int DT>
 int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   const Shape& s = p.s;
   Meta* meta = (Meta*)(ws + p.meta);
   uint32_t *row_of = (uint32_t*)(ws + p.row_of), *target_of = (uint32_t*)(ws + p.target_of);
   uint16_t* packed = (uint16_t*)(ws + p.packed);
-  hipLaunchKernelGGL(k_head_rows, dim3(1), dim3(1024), 0, st, h.target, h.row_scale, s, meta, row_of, target_of);
-  PT_LAUNCH_CHECK(nullptr, "k_head_rows");
-  hipLaunchKernelGGL(k_head_gather, dim3(uint32_t(up(s.R, TWO) / 4)), dim3(256), 0, st, (const uint16_t*)h.hidden, h.hidden_stride, h.target, s, meta,
-                     row_of, packed, h.loss, (uint16_t*)h.d_hidden, h.d_hidden_stride);
-  PT_LAUNCH_CHECK(nullptr, "k_head_gather");
-  Operand w = {h.weight, h.weight_stride * 2, 0, 0};
-  if (!p.direct) {
-    hipLaunchKernelGGL(k_head_weight, dim3((s.V + 3) / 4), dim3(256), 0, st, (const uint16_t*)h.weight, h.weight_stride, s, (uint16_t*)(ws + p.weight));
-    PT_LAUNCH_CHECK(nullptr, "k_head_weight");
-    w.at = ws + p.weight;
-    w.pitch = 2ull * s.Kd;
+  const RowArgs ra = {h.target, h.row_scale, s, meta, row_of, target_of};
+  const dim3 gather(uint32_t(up(s.R, TWO) / 4));
+  if (s.R <= LISTED) {
+    hipLaunchKernelGGL(k_head_gather<true>, gather, dim3(256), 0, st, ra, (const uint16_t*)h.hidden, h.hidden_stride, packed, h.loss, (uint16_t*)h.d_hidden,
+                       h.d_hidden_stride);
+  } else {
+    hipLaunchKernelGGL(k_head_rows, dim3(1), dim3(1024), 0, st, ra);
+    PT_LAUNCH_CHECK(nullptr, "k_head_rows");
+    hipLaunchKernelGGL(k_head_gather<false>, gather, dim3(256), 0, st, ra, (const uint16_t*)h.hidden, h.hidden_stride, packed, h.loss,
+                       (uint16_t*)h.d_hidden, h.d_hidden_stride);
   }
-  const uint32_t wide_k = p.direct ? s.d : s.Kd;            // of a row of the weight that may be read
-  for (uint32_t i = 0; i < p.pieces; ++i) {
+  PT_LAUNCH_CHECK(nullptr, "k_head_gather");
+  // the weight: k (of the logits) next to each other in rows of `width` elements
+  uint32_t width = s.d;
+  const uint16_t* weight = (const uint16_t*)h.weight;
+  uint64_t stride = h.weight_stride;
+  if (!p.direct) {
+    hipLaunchKernelGGL(k_head_weight, dim3((s.V + 3) / 4), dim3(256), 0, st, weight, stride, s, (uint16_t*)(ws + p.weight));
+    PT_LAUNCH_CHECK(nullptr, "k_head_weight");
+    weight = (const uint16_t*)(ws + p.weight);
+    stride = width = s.Kd;
+  }
+  int rc = PT_OK;
+  for (uint32_t i = 0; i < p.pieces && rc == PT_OK; ++i) {
     const uint32_t first = i * p.rows, rows = std::min(p.rows, s.R - first);
-    const Operand hid = {packed + size_t(first) * s.Kd, 2ull * s.Kd, 0, s.Kd};
-    Operand wk = w;
-    wk.extent = s.V;
-    wk.k = wide_k;
-    const LogitArgs la = {s, wk, hid, meta, first, rows, target_of + first, (f32x2*)(ws + p.part), p.parts, (float*)(ws + p.at_target),
+    uint16_t* hid = packed + size_t(first) * s.Kd;
+    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_tiles(s.d, rows), mid_w = mid_tiles(s.d, s.V);
+    const LogitArgs la = {s, {weight, stride * 2, s.V, width}, {hid, 2ull * s.Kd, 0, s.Kd}, meta, first, rows, target_of + first, (f32x2*)(ws + p.part),
+                          few ? parts<Few>(s.V) : mid ? parts<Mid>(s.V) : parts<Big>(s.V), (float*)(ws + p.at_target),
                           p.grads ? (float*)(ws + p.z) : nullptr};
-    hipLaunchKernelGGL((k_head_logits<DT, BM, BN, WM, WN>), dim3(tile_grid((s.V + BM - 1) / BM, (rows + BN - 1) / BN)), dim3(THREADS), 0, st, la);
-    PT_LAUNCH_CHECK(nullptr, "k_head_logits");
-    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, (const f32x2*)(ws + p.part), p.parts,
-                         (const float*)(ws + p.at_target), h.row_scale, h.loss, (float*)(ws + p.z)};
+    rc = few ? logits<DT, Few>(la, st) : mid ? logits<DT, Mid>(la, st) : logits<DT, Big>(la, st);
+    if (rc != PT_OK) return rc;
+    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.part, la.parts, la.at_target, h.row_scale, h.loss,
+                         (float*)(ws + p.z), (float*)(ws + p.rest)};
     if (!p.grads) {
       hipLaunchKernelGGL(k_head_loss, dim3((rows + 3) / 4), dim3(256), 0, st, sa);
       PT_LAUNCH_CHECK(nullptr, "k_head_loss");
@@ -463,25 +668,22 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO))), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
     const uint64_t z_pitch = 4ull * s.Vp;
-    if (h.d_hidden) {
-      Operand wm = w;
-      wm.extent = wide_k;
-      wm.k = s.V;
-      const GradArgs ga = {s, wm, {ws + p.z, z_pitch, 0, s.Vp}, meta, first, rows, row_of + first, (uint16_t*)h.d_hidden, h.d_hidden_stride,
-                           (uintptr_t)h.d_hidden % 8 == 0 && h.d_hidden_stride % 4 == 0, nullptr, 0, false, false};
-      hipLaunchKernelGGL((k_head_d_hidden<DT, BM, BN, WM, WN>), dim3(tile_grid((s.d + BM - 1) / BM, (rows + BN - 1) / BN)), dim3(THREADS), 0, st, ga);
-      PT_LAUNCH_CHECK(nullptr, "k_head_d_hidden");
-    }
-    if (h.d_weight) {
-      Operand hm = hid;
-      hm.extent = s.Kd;
-      const GradArgs ga = {s, hm, {ws + p.z, z_pitch, s.Vp, 0}, meta, first, rows, nullptr, (uint16_t*)h.d_weight, h.d_weight_stride,
-                           (uintptr_t)h.d_weight % 8 == 0 && h.d_weight_stride % 4 == 0, (float*)(ws + p.acc), p.pitch, i > 0, i + 1 < p.pieces};
-      hipLaunchKernelGGL((k_head_d_weight<DT, BM, BN, WM, WN>), dim3(tile_grid((s.d + BM - 1) / BM, (s.V + BN - 1) / BN)), dim3(THREADS), 0, st, ga);
-      PT_LAUNCH_CHECK(nullptr, "k_head_d_weight");
-    }
+    GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.z, z_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
+                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 8 == 0 && h.d_hidden_stride % 4 == 0, p.pitch,
+                   (float*)(ws + p.sums), sa.rest, weight, stride, nullptr, false, false};
+    if (h.d_hidden) rc = few ? d_hidden<DT, Few>(ga, st) : mid_h ? d_hidden<DT, Mid>(ga, st) : d_hidden<DT, Big>(ga, st);
+    if (!h.d_weight || rc != PT_OK) continue;
+    ga.p = {hid, 2ull * s.Kd, s.Kd, 0};
+    ga.q = {ws + p.z, z_pitch, s.Vp, 0};
+    ga.out = (uint16_t*)h.d_weight;
+    ga.stride = h.d_weight_stride;
+    ga.wide = (uintptr_t)h.d_weight % 8 == 0 && h.d_weight_stride % 4 == 0;
+    ga.acc = (float*)(ws + p.acc);
+    ga.read_acc = i > 0;
+    ga.write_acc = i + 1 < p.pieces;
+    rc = mid_w ? d_weight<DT, Mid>(ga, st) : d_weight<DT, Big>(ga, st);
   }
-  return PT_OK;
+  return rc;
 }
 
 }  // namespace
