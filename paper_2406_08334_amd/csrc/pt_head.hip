@@ -2,8 +2,9 @@
 //
 //   rows     the rows with a target, counted and listed on the device (ignored ones take no part in anything that follows)
 //   gather   their hidden states next to each other, zero-padded to whole steps of the products
-//   logits   z = W h^T on the matrix cores, tile by tile; of each tile the largest z and the sum of exp(z - that) of every row, and, for gradients, z in fp32
-//   soft     from the tiles' sums lse and loss of a row; G = s (exp(z - lse) - [target]) in 16 bits over the row's z, in place
+//   logits   z = W h^T on the matrix cores, tile by tile; of each wave's part of a tile the largest z and the sum of exp(z - that) of every row, and, for
+//            gradients, exp(z - that) (fp16 inputs: z in fp32)
+//   soft     from those lse and loss of a row; G = s (exp(z - lse) - [target]) in 16 bits, in place
 //   d_hidden = G W, d_weight = G^T h on the matrix cores
 //
 // Three products of 2 rows vocab width operations each are what it costs.  Gradients want lse of a whole row before the first of them: pieces of the
@@ -19,14 +20,18 @@ using namespace pt_mfma;
 
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a __attribute__((aligned(2)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t PIECE_STEP = 256;       // pieces are multiples of this many rows
 constexpr uint32_t PIECE_BEST = 8192;
 constexpr float LOG2E = 1.44269504088896340736f;
+
+// What is kept of the logits of a piece.  bf16 inputs: exp(z - the largest of the wave's part of the row) as an fp16 number, 2^15 being 1: a rounding of 2^-12
+// ahead of G's own of 2^-9.  fp16 inputs, whose G is rounded by 2^-12 itself: z in fp32.
+template <int DT> constexpr bool KEEP_EXP = DT == PT_BF16;
+template <int DT> constexpr uint32_t KEPT_BYTES = KEEP_EXP<DT> ? 2 : 4;
+constexpr float ONE_EXP = 15.0f;
 
 // What the device finds out about the rows.
 struct Meta {
@@ -204,7 +209,7 @@ struct LogitArgs {
   f32x2* part;               // [rows][parts] of the piece: largest z, sum of exp(z - largest)
   uint32_t parts;
   float* at_target;          // [rows]
-  float* z;                  // [rows][Vp], or NULL
+  void* z;                   // [rows][Vp], or NULL: what is kept of the logits
 };
 
 template <int DT, class C>
@@ -234,9 +239,6 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = n0 + t.wave_n() + j * 16 + (lane & 15);
     const bool live = n < n_rows;
-    if (a.z && live)
-#pragma unroll
-      for (int i = 0; i < T::FM; ++i) *(PT_GLOBAL f32x4*)((PT_GLOBAL float*)a.z + size_t(n) * a.s.Vp + mb + i * 16) = t.acc[i][j];
     float big = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
@@ -244,12 +246,36 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
       for (int q = 0; q < 4; ++q) big = fmaxf(big, t.acc[i][j][q]);
     big = fmaxf(big, __shfl_xor(big, 16, 64));
     big = fmaxf(big, __shfl_xor(big, 32, 64));
-    const float top = big == -__builtin_inff() ? 0.0f : big * LOG2E;          // of nothing but -inf the sum is 0
+    const float top = (big == -__builtin_inff() ? 0.0f : big * LOG2E) - ONE_EXP;          // of nothing but -inf the sum is 0
     float sum = 0.0f;
+    if (KEEP_EXP<DT> && a.z) {
+      typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+      PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.z + size_t(n) * a.s.Vp + m0 + t.wave_m() + eight_at();
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i)
+      for (int i = 0; i < T::FM; i += 2) {
+        u32x2 w[2];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][q], LOG2E, -top));
+        for (int h = 0; h < 2; ++h) {
+          f32x4 e;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            e[q] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i + h][j][q], LOG2E, -top));
+            sum += e[q];
+          }
+          w[h] = __builtin_bit_cast(u32x2, __builtin_convertvector(e, f16x4));
+        }
+        const u32x4 x = eight(w[0], w[1]);
+        if (live) *(PT_GLOBAL u32x4*)(row + i * 16) = x;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i) {
+        if (a.z && live) *(PT_GLOBAL f32x4*)((PT_GLOBAL float*)a.z + size_t(n) * a.s.Vp + mb + i * 16) = t.acc[i][j];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][q], LOG2E, -top));
+      }
+    }
+    sum *= 0x1p-15f;
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
     if (live && lane < 16) a.part[size_t(n) * a.parts + tm * C::WM + t.wave_m() / T::TM] = f32x2{big, sum};
@@ -266,7 +292,7 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
   }
 }
 
-// lse of a row from its tiles' sums, by `lanes` lanes of which this is `lane`; in all of them.
+// Largest z and sum of two parts of a row together; lse of a row from all of them.
 __device__ __forceinline__ f32x2 join(f32x2 a, f32x2 b) {
   const float top = fmaxf(a[0], b[0]);
   if (top == -__builtin_inff()) return f32x2{top, a[1] + b[1]};
@@ -284,31 +310,38 @@ struct SoftArgs {
   uint32_t first, rows;
   const uint32_t *row_of, *target_of;      // of the piece
   const f32x2* part;
-  uint32_t parts;
+  uint32_t parts, part_width;
   const float* at_target;
   const float* scale;
   float* loss;
-  float* z;
+  void* z;
   float* rest;               // [rows]: of G at the target, what its rounding has left
 };
 
-// The loss alone: a wave a row.
-__global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
-  const uint32_t r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (r >= piece_rows(a.meta, a.first, a.rows)) return;
+// Of the workgroup, in all its lanes.
+__device__ __forceinline__ f32x2 join_row(const f32x2* part, uint32_t parts) {
+  __shared__ f32x2 s_x[4];
   f32x2 x = {-__builtin_inff(), 0.0f};
-  for (uint32_t i = lane; i < a.parts; i += 64) x = join(x, a.part[size_t(r) * a.parts + i]);
+  for (uint32_t i = threadIdx.x; i < parts; i += 256) x = join(x, part[i]);
   x = join_wave(x);
-  if (lane == 0) a.loss[a.row_of[r]] = x[0] + logf(x[1]) - a.at_target[r];
+  if ((threadIdx.x & 63) == 0) s_x[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return join(join(s_x[0], s_x[1]), join(s_x[2], s_x[3]));
+}
+
+// The loss alone: a workgroup a row.
+__global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
+  const uint32_t r = blockIdx.x;
+  if (r >= piece_rows(a.meta, a.first, a.rows)) return;
+  const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
+  if (threadIdx.x == 0) a.loss[a.row_of[r]] = x[0] + logf(x[1]) - a.at_target[r];
 }
 
 // Eight numbers in 16 bits, and what is left of them.
 template <int DT>
 __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
-  u32x4 q;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) q[j] = encode16<DT>(x[2 * j]) | encode16<DT>(x[2 * j + 1]) << 16;
-  return q;
+  const u32x2 a = encode16x4<DT>(f32x4{x[0], x[1], x[2], x[3]}), b = encode16x4<DT>(f32x4{x[4], x[5], x[6], x[7]});
+  return u32x4{a.x, a.y, b.x, b.y};
 }
 template <int DT>
 __device__ __forceinline__ u32x4 pack8_rest(const float (&x)[8], const u32x4& q) {
@@ -318,15 +351,16 @@ __device__ __forceinline__ u32x4 pack8_rest(const float (&x)[8], const u32x4& q)
   return pack8<DT>(y);
 }
 
-// Loss and G of a row by a workgroup: the row's z lie where its G goes, which is half as long.  Each round takes 2048 z; a lane has its own of the
-// next round under way while it stores those of this one, and stores when every lane has this round's.
+// Loss and G of a row by a workgroup, G where what is kept of the row's logits lies.
+// Of z in fp32, which are twice as long, a round takes 2048: a lane has its own of the next round under way while it stores those of this one,
+// and stores when every lane has this round's.
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   const uint32_t r = blockIdx.x, tid = threadIdx.x, n = piece_rows(a.meta, a.first, a.rows);
   if (r >= (a.s.low ? a.s.low : (n + TWO - 1) / TWO * TWO)) return;
-  PT_GLOBAL float* z = (PT_GLOBAL float*)a.z + size_t(r) * a.s.Vp;
-  PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)z;
-  PT_GLOBAL uint16_t* g_low = (PT_GLOBAL uint16_t*)(z + size_t(a.s.low) * a.s.Vp);
+  const size_t pitch = size_t(a.s.Vp) * KEPT_BYTES<DT>;
+  PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)a.z + r * pitch);
+  PT_GLOBAL uint16_t* g_low = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)g + a.s.low * pitch);
   if (r >= n) {                                            // rows up to a whole step: zero
     for (uint32_t c = tid * 8; c < a.s.Vp; c += 2048) {
       *(PT_GLOBAL u32x4*)(g + c) = u32x4{0, 0, 0, 0};
@@ -334,13 +368,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     }
     return;
   }
-  __shared__ f32x2 s_x[4];
-  f32x2 x = {-__builtin_inff(), 0.0f};
-  for (uint32_t i = tid; i < a.parts; i += 256) x = join(x, a.part[size_t(r) * a.parts + i]);
-  x = join_wave(x);
-  if ((tid & 63) == 0) s_x[tid >> 6] = x;
-  __syncthreads();
-  x = join(join(s_x[0], s_x[1]), join(s_x[2], s_x[3]));
+  const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
   const uint32_t row = a.row_of[r], y = a.target_of[r];
   const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * a.meta->up;
   const float off = lse * LOG2E, gy = s * expm1f(zy - lse);
@@ -348,13 +376,34 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     a.loss[row] = lse - zy;
     a.rest[r] = gy - decode16<DT>(encode16<DT>(gy));
   }
+  if constexpr (KEEP_EXP<DT>) {
+    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    const PT_GLOBAL f32x2* part = (const PT_GLOBAL f32x2*)a.part + size_t(r) * a.parts;
+#pragma unroll 4
+    for (uint32_t c = tid * 8; c < a.s.Vp; c += 2048) {
+      const f16x8 e = __builtin_bit_cast(f16x8, *(const PT_GLOBAL u32x4*)(g + c));
+      const float f = s * __builtin_amdgcn_exp2f(__builtin_fmaf(part[min(c / a.part_width, a.parts - 1)][0], LOG2E, -off - ONE_EXP));
+      float p[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        p[j] = f * float(e[j]);
+        if (c + j == y) p[j] = gy;
+        if (c + j >= a.s.V) p[j] = 0.0f;
+      }
+      const u32x4 w = pack8<DT>(p);
+      *(PT_GLOBAL u32x4*)(g + c) = w;
+      if (a.s.low) *(PT_GLOBAL u32x4*)(g_low + c) = pack8_rest<DT>(p, w);
+    }
+    return;
+  }
+  const PT_GLOBAL float* z = (const PT_GLOBAL float*)g;
   const uint32_t last = a.s.Vp - 8;                        // lanes behind the row's end load its last ones, and store nothing
   f32x4 q[2], next[2];
   uint32_t c = tid * 8, at = min(c, last);
-  q[0] = *(PT_GLOBAL f32x4*)(z + at); q[1] = *(PT_GLOBAL f32x4*)(z + at + 4);
+  q[0] = *(const PT_GLOBAL f32x4*)(z + at); q[1] = *(const PT_GLOBAL f32x4*)(z + at + 4);
   for (; c < a.s.Vp + tid * 8; c += 2048) {
     at = min(c + 2048, last);
-    next[0] = *(PT_GLOBAL f32x4*)(z + at); next[1] = *(PT_GLOBAL f32x4*)(z + at + 4);
+    next[0] = *(const PT_GLOBAL f32x4*)(z + at); next[1] = *(const PT_GLOBAL f32x4*)(z + at + 4);
     float p[8];
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
@@ -377,12 +426,12 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
 // Four values of consecutive m of a row that has d of them.
 template <int DT>
 __device__ __forceinline__ void store4(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, bool wide, f32x4 x) {
-  const uint32_t w[4] = {encode16<DT>(x[0]), encode16<DT>(x[1]), encode16<DT>(x[2]), encode16<DT>(x[3])};
-  if (wide && m + 4 <= d) *(PT_GLOBAL u32x2*)(row + m) = u32x2{w[0] | w[1] << 16, w[2] | w[3] << 16};
+  const u32x2 w = encode16x4<DT>(x);
+  if (wide && m + 4 <= d) *(PT_GLOBAL u32x2*)(row + m) = w;
   else
 #pragma unroll
     for (uint32_t q = 0; q < 4; ++q)
-      if (m + q < d) row[m + q] = uint16_t(w[q]);
+      if (m + q < d) row[m + q] = uint16_t(w[q / 2] >> (16 * (q & 1)));
 }
 
 struct GradArgs {
@@ -571,7 +620,7 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   p.packed = take(2ull * (up(h.rows, TWO) + p.s.low) * p.s.Kd);
   p.weight = take(p.direct ? 0 : 2ull * h.vocab * p.s.Kd);
   p.part = take(8ull * p.rows * p.parts);
-  p.z = take(p.grads ? 4ull * (p.rows + p.s.low) * p.s.Vp : 0);
+  p.z = take(p.grads ? (h.dtype == PT_BF16 ? KEPT_BYTES<PT_BF16> : KEPT_BYTES<PT_FP16>) * uint64_t(p.rows + p.s.low) * p.s.Vp : 0);
   if (h.d_hidden)                            // of a whole piece and of the last one
     for (uint32_t rows : {std::min(p.rows, h.rows), h.rows - (p.pieces - 1) * p.rows}) p.shared = std::max(p.shared, shared_rows(p.s, rows));
   p.sums = take(4ull * p.shared * p.pitch);
@@ -655,19 +704,20 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_tiles(s.d, rows), mid_w = mid_tiles(s.d, s.V);
     const LogitArgs la = {s, {weight, stride * 2, s.V, width}, {hid, 2ull * s.Kd, 0, s.Kd}, meta, first, rows, target_of + first, (f32x2*)(ws + p.part),
                           few ? parts<Few>(s.V) : mid ? parts<Mid>(s.V) : parts<Big>(s.V), (float*)(ws + p.at_target),
-                          p.grads ? (float*)(ws + p.z) : nullptr};
+                          p.grads ? ws + p.z : nullptr};
     rc = few ? logits<DT, Few>(la, st) : mid ? logits<DT, Mid>(la, st) : logits<DT, Big>(la, st);
     if (rc != PT_OK) return rc;
-    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.part, la.parts, la.at_target, h.row_scale, h.loss,
-                         (float*)(ws + p.z), (float*)(ws + p.rest)};
+    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.part, la.parts,
+                         uint32_t(few ? Few::BM / Few::WM : mid ? Mid::BM / Mid::WM : Big::BM / Big::WM), la.at_target, h.row_scale, h.loss, ws + p.z,
+                         (float*)(ws + p.rest)};
     if (!p.grads) {
-      hipLaunchKernelGGL(k_head_loss, dim3((rows + 3) / 4), dim3(256), 0, st, sa);
+      hipLaunchKernelGGL(k_head_loss, dim3(rows), dim3(256), 0, st, sa);
       PT_LAUNCH_CHECK(nullptr, "k_head_loss");
       continue;
     }
     hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO))), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
-    const uint64_t z_pitch = 4ull * s.Vp;
+    const uint64_t z_pitch = uint64_t(KEPT_BYTES<DT>) * s.Vp;
     GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.z, z_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
                    (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 8 == 0 && h.d_hidden_stride % 4 == 0, p.pitch,
                    (float*)(ws + p.sums), sa.rest, weight, stride, nullptr, false, false};

@@ -81,9 +81,7 @@ struct Stage {
     if constexpr (KC) {
       return *(const __attribute__((address_space(3))) s16x8*)(from + (lane_at ^ (kk * 64)) + i * (16 * BK * 2));
     } else {
-      uint32_t flip = i * 32;
-      asm volatile("" : "+s"(flip));               // an address of every read in a register of its own would be too many
-      const lds_char* at = from + (lane_at ^ flip) + kk * (32 * B * 2);
+      const lds_char* at = from + (lane_at ^ (i * 32)) + kk * (32 * B * 2);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 4 * B * 2));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -189,5 +187,16 @@ struct Tile {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   }
 };
+
+// Of four values of consecutive m a lane has of fragment i (two words of 16-bit numbers, a) and of fragment i + 1 (b): eight of one of the two.
+// Lanes 0-15 and 32-47 keep i and get its next four from the 16 lanes behind them, those give it for i + 1.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 eight(u32x2 a, u32x2 b) {
+  const u32x2 x = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false), y = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+  return u32x4{x[0], y[0], x[1], y[1]};
+}
+// Where those eight begin, from the first m of fragment i on.
+__device__ __forceinline__ uint32_t eight_at() { const uint32_t g = (threadIdx.x >> 4) & 3; return (g & 1) * 16 + (g >> 1) * 8; }
 
 }  // namespace pt_mfma

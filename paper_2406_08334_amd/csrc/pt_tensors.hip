@@ -21,8 +21,8 @@
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef pt_f32x4 f32x4;
+typedef pt_u32x2 u32x2;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // global memory takes these at any address of an element
 typedef f32x4 f32x4_a __attribute__((aligned(4)));
@@ -251,17 +251,6 @@ __device__ __forceinline__ void update_element8(const Consts& k, float decay, fl
   const float d = __builtin_fmaf(s, k.rsb2, k.eps);
   const float u = m * __builtin_amdgcn_rcpf(d);
   w = __builtin_fmaf(-k.step_size, u, w * decay);
-}
-
-// To the nearest 16-bit numbers, two an instruction.
-template <int DT>
-__device__ __forceinline__ u32x2 encode16x4(f32x4 x) {
-  if constexpr (DT == PT_BF16) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
-  } else {
-    return u32x2{encode16<DT>(x[0]) | encode16<DT>(x[1]) << 16, encode16<DT>(x[2]) | encode16<DT>(x[3]) << 16};
-  }
 }
 
 // A lane's four codes; policy as pt_store.

@@ -34,6 +34,19 @@ __device__ __forceinline__ uint32_t encode16(float x) {
   }
 }
 
+typedef float pt_f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t pt_u32x2 __attribute__((ext_vector_type(2)));
+// To the nearest 16-bit numbers, two an instruction.
+template <int DT>
+__device__ __forceinline__ pt_u32x2 encode16x4(pt_f32x4 x) {
+  if constexpr (DT == PT_BF16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(pt_u32x2, __builtin_convertvector(x, bf16x4));
+  } else {
+    return pt_u32x2{encode16<DT>(x[0]) | encode16<DT>(x[1]) << 16, encode16<DT>(x[2]) | encode16<DT>(x[3]) << 16};
+  }
+}
+
 struct Consts { float b1, b2, omb1, omb2, decay, step_size, rsb2, eps, gm; };
 
 // g: the gradient as stored; decay: the element's decay factor.  s: sqrt of the new variance.
