@@ -343,7 +343,7 @@ struct Block {
                              3.402823466e38f);
       const float bv = fminf(wave_max(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]))), 3.402823466e38f);
       const bool hm = bm >= TINY8, hv = bv >= TINY8;
-      const float im = hm ? TOP8 / bm : 0.0f, iv = hv ? TOP8 / bv : 0.0f;
+      const float im = hm ? 1.0f / bm * TOP8 : 0.0f, iv = hv ? 1.0f / bv * TOP8 : 0.0f;
       uint32_t z[4];
       {
         const uint64_t z0 = mix64(counter), z1 = mix64(counter + PHI);
@@ -361,8 +361,8 @@ struct Block {
 #undef PT_CODE
       cm = uint32_t(qm); cv = uint32_t(qv);
       if (threadIdx.x == 0) {
-        ((PT_GLOBAL float*)d.ms)[nb] = hm ? bm / TOP8 : 0.0f;
-        ((PT_GLOBAL float*)d.vs)[nb] = hv ? bv / TOP8 : 0.0f;
+        ((PT_GLOBAL float*)d.ms)[nb] = hm ? bm * (1.0f / TOP8) : 0.0f;
+        ((PT_GLOBAL float*)d.vs)[nb] = hv ? bv * (1.0f / TOP8) : 0.0f;
       }
     }
     const auto pw = at<PT_GLOBAL float*>(d.master);
