@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(1024) k_head_rows(const RowArgs a) {
 
 // One row of 16-bit words, at any address, into one of Kd words that begins at a multiple of 16 bytes; zero behind its end.
 __device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOBAL uint16_t* to, uint32_t d, uint32_t Kd, uint32_t lane, uint32_t lanes) {
+#pragma unroll 4
   for (uint32_t c = lane * 8; c < Kd; c += lanes * 8) {
     u32x4 q = {0, 0, 0, 0};
     if (c + 8 <= d) q = *(const PT_GLOBAL u32x4_a*)(from + c);
@@ -167,17 +168,18 @@ template <int BM_, int BN_, int WM_, int WN_, int SLOTS_, int TWO_NS_> struct Cf
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, THREADS = 64 * WM_ * WN_, SLOTS = SLOTS_, TWO_NS = TWO_NS_, PART_NS = BM_ * BN_ / 625;
   template <int DT, bool PK, bool QK> using Of = Tile<DT, PK, QK, BM_, BN_, WM_, WN_>;
 };
-typedef Cfg<256, 256, 2, 4, 256, 1700> Big;
-typedef Cfg<128, 128, 2, 2, 512, 1100> Mid;
-typedef Cfg<128, 64, 4, 1, 768, 900> Few;      // up to 64 rows
+typedef Cfg<256, 256, 2, 4, 256, 2970> Big;
+typedef Cfg<128, 128, 2, 2, 512, 1910> Mid;
+typedef Cfg<128, 64, 4, 1, 256, 1700> Few;     // up to 64 rows: 256 of them read at the rate of the memory
 
-// Workgroups that share the k of a tile: as many as finish first, the sums that they leave to be added counted in.
-template <class C> __host__ __device__ inline uint32_t shares(uint32_t tiles, uint32_t twos) {
-  uint32_t best = 1, least = 0xffffffffu;
+// Workgroups that share the k of a tile: as many as finish first, the sums that they leave to be added counted in; and when that is, in ns.
+struct Shares { uint32_t n, ns; };
+template <class C> __host__ __device__ inline Shares shares(uint32_t tiles, uint32_t twos) {
+  Shares best = {1, 0xffffffffu};
   for (uint32_t n : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
     if (n > 1 && n * 2 > twos) break;
     const uint32_t ns = (tiles * n + C::SLOTS - 1) / C::SLOTS * ((twos + n - 1) / n * C::TWO_NS + 3000) + (n > 1 ? tiles * n * C::PART_NS + 4000 : 0);
-    if (ns < least) { least = ns; best = n; }
+    if (ns < best.ns) best = {n, ns};
   }
   return best;
 }
@@ -315,6 +317,8 @@ struct SoftArgs {
   const float* scale;
   float* loss;
   void* z;
+  uint16_t* g;               // G; where z lies, or, of few rows, elsewhere
+  uint64_t g_pitch;          // bytes
   float* rest;               // [rows]: of G at the target, what its rounding has left
 };
 
@@ -351,18 +355,19 @@ __device__ __forceinline__ u32x4 pack8_rest(const float (&x)[8], const u32x4& q)
   return pack8<DT>(y);
 }
 
-// Loss and G of a row by a workgroup, G where what is kept of the row's logits lies.
+// Loss and G of a row by a workgroup, G where what is kept of the row's logits lies.  Of few rows G has a place of its own, and several workgroups
+// (gridDim.y) share a row.
 // Of z in fp32, which are twice as long, a round takes 2048: a lane has its own of the next round under way while it stores those of this one,
 // and stores when every lane has this round's.
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   const uint32_t r = blockIdx.x, tid = threadIdx.x, n = piece_rows(a.meta, a.first, a.rows);
   if (r >= (a.s.low ? a.s.low : (n + TWO - 1) / TWO * TWO)) return;
-  const size_t pitch = size_t(a.s.Vp) * KEPT_BYTES<DT>;
-  PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)a.z + r * pitch);
-  PT_GLOBAL uint16_t* g_low = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)g + a.s.low * pitch);
+  PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)a.g + r * a.g_pitch);
+  PT_GLOBAL uint16_t* g_low = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)g + a.s.low * a.g_pitch);
+  const uint32_t first = blockIdx.y * 2048 + tid * 8, turn = gridDim.y * 2048;
   if (r >= n) {                                            // rows up to a whole step: zero
-    for (uint32_t c = tid * 8; c < a.s.Vp; c += 2048) {
+    for (uint32_t c = first; c < a.s.Vp; c += turn) {
       *(PT_GLOBAL u32x4*)(g + c) = u32x4{0, 0, 0, 0};
       if (a.s.low) *(PT_GLOBAL u32x4*)(g_low + c) = u32x4{0, 0, 0, 0};
     }
@@ -372,7 +377,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   const uint32_t row = a.row_of[r], y = a.target_of[r];
   const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * a.meta->up;
   const float off = lse * LOG2E, gy = s * expm1f(zy - lse);
-  if (tid == 0) {
+  if (tid == 0 && blockIdx.y == 0) {
     a.loss[row] = lse - zy;
     a.rest[r] = gy - decode16<DT>(encode16<DT>(gy));
   }
@@ -380,8 +385,8 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
     const PT_GLOBAL f32x2* part = (const PT_GLOBAL f32x2*)a.part + size_t(r) * a.parts;
 #pragma unroll 4
-    for (uint32_t c = tid * 8; c < a.s.Vp; c += 2048) {
-      const f16x8 e = __builtin_bit_cast(f16x8, *(const PT_GLOBAL u32x4*)(g + c));
+    for (uint32_t c = first; c < a.s.Vp; c += turn) {
+      const f16x8 e = __builtin_bit_cast(f16x8, *(const PT_GLOBAL u32x4*)((const PT_GLOBAL uint16_t*)a.z + size_t(r) * a.s.Vp + c));
       const float f = s * __builtin_amdgcn_exp2f(__builtin_fmaf(part[min(c / a.part_width, a.parts - 1)][0], LOG2E, -off - ONE_EXP));
       float p[8];
 #pragma unroll
@@ -396,13 +401,13 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     }
     return;
   }
-  const PT_GLOBAL float* z = (const PT_GLOBAL float*)g;
+  const PT_GLOBAL float* z = (const PT_GLOBAL float*)a.z + size_t(r) * a.s.Vp;
   const uint32_t last = a.s.Vp - 8;                        // lanes behind the row's end load its last ones, and store nothing
   f32x4 q[2], next[2];
-  uint32_t c = tid * 8, at = min(c, last);
+  uint32_t c = first, at = min(c, last);
   q[0] = *(const PT_GLOBAL f32x4*)(z + at); q[1] = *(const PT_GLOBAL f32x4*)(z + at + 4);
-  for (; c < a.s.Vp + tid * 8; c += 2048) {
-    at = min(c + 2048, last);
+  for (; c < a.s.Vp + tid * 8; c += turn) {
+    at = min(c + turn, last);
     next[0] = *(const PT_GLOBAL f32x4*)(z + at); next[1] = *(const PT_GLOBAL f32x4*)(z + at + 4);
     float p[8];
 #pragma unroll
@@ -423,14 +428,12 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   }
 }
 
-// Four values of consecutive m of a row that has d of them.
-template <int DT>
-__device__ __forceinline__ void store4(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, bool wide, f32x4 x) {
-  const u32x2 w = encode16x4<DT>(x);
-  if (wide && m + 4 <= d) *(PT_GLOBAL u32x2*)(row + m) = w;
+// Of a row of d 16-bit numbers the eight from m on; wide: whole ones may be stored at once.
+__device__ __forceinline__ void store8(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, bool wide, u32x4 w) {
+  if (wide && m + 8 <= d) *(PT_GLOBAL u32x4*)(row + m) = w;
   else
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q)
+    for (uint32_t q = 0; q < 8; ++q)
       if (m + q < d) row[m + q] = uint16_t(w[q / 2] >> (16 * (q & 1)));
 }
 
@@ -442,7 +445,7 @@ struct GradArgs {
   const uint32_t *row_of, *target_of;      // of the piece
   uint16_t* out;
   uint64_t stride;
-  bool wide;                 // four results may be stored at once
+  bool wide;                 // eight results may be stored at once
   uint32_t pitch;            // of the sums below
   float* part;               // d_hidden by several workgroups a tile: [shares][rows][pitch]
   const float* rest;
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) 
   __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM, tiles_n = (n_rows + C::BN - 1) / C::BN, twos = a.s.Vp / TWO;
-  const uint32_t share = shares<C>(tiles_m * tiles_n, twos);
+  const uint32_t share = shares<C>(tiles_m * tiles_n, twos).n;
   uint32_t tm, tn;
   if (!tile_of(blockIdx.x, tiles_m * share, tiles_n, tm, tn)) return;
   const uint32_t part = tm / tiles_m, t0 = uint32_t(uint64_t(twos) * part / share), t1 = uint32_t(uint64_t(twos) * (part + 1) / share);
@@ -485,40 +488,49 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) 
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
-    if (n >= n_rows) continue;
+    const bool live = n < n_rows;
     if (share > 1) {
+      if (!live) continue;
       PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.rows + n) * a.pitch;
 #pragma unroll
       for (int i = 0; i < T::FM; ++i)
         if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
       continue;
     }
-    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
-    const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[n] * a.weight_stride;
-    const float rest = a.rest[n];
+    const uint32_t at = live ? n : 0;                      // lanes without a row take part in the exchange
+    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[at] * a.stride;
+    const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[at] * a.weight_stride;
+    const float rest = a.rest[at];
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i) {
+    for (int i = 0; i < T::FM; i += 2) {
       const uint32_t m = mb + i * 16;
-      store4<DT>(row, m, a.s.d, a.wide, add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down);
+      const u32x4 x = eight(encode16x4<DT>(add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down),
+                            encode16x4<DT>(add_rest<DT>(t.acc[i + 1][j], rest, w, m + 16, a.s.d) * down));
+      if (live) store8(row, tm * C::BM + t.wave_m() + i * 16 + eight_at(), a.s.d, a.wide, x);
     }
   }
 }
 
-// Adds up what several workgroups a tile have left: a workgroup a row.
+// Adds up what several workgroups a tile have left: a lane four results of a row.
 template <int DT, class C>
 __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
-  const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows), n = blockIdx.x;
-  if (n >= n_rows) return;
-  const uint32_t share = shares<C>((a.s.d + C::BM - 1) / C::BM * ((n_rows + C::BN - 1) / C::BN), a.s.Vp / TWO);
+  const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows), n = blockIdx.x, m = (blockIdx.y * 256 + threadIdx.x) * 4;
+  if (n >= n_rows || m >= a.s.d) return;
+  const uint32_t share = shares<C>((a.s.d + C::BM - 1) / C::BM * ((n_rows + C::BN - 1) / C::BN), a.s.Vp / TWO).n;
   if (share == 1) return;
-  PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
+  const PT_GLOBAL float* part = (const PT_GLOBAL float*)a.part + size_t(n) * a.pitch + m;
+  const size_t next = size_t(a.rows) * a.pitch;
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+  for (uint32_t k = 0; k < share; ++k) x += *(const PT_GLOBAL f32x4*)(part + k * next);
   const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[n] * a.weight_stride;
-  const float rest = a.rest[n], down = a.meta->down;
-  for (uint32_t m = threadIdx.x * 4; m < a.s.d; m += 1024) {
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t k = 0; k < share; ++k) x += *(const PT_GLOBAL f32x4*)((const PT_GLOBAL float*)a.part + (size_t(k) * a.rows + n) * a.pitch + m);
-    store4<DT>(row, m, a.s.d, a.wide, add_rest<DT>(x, rest, w, m, a.s.d) * down);
-  }
+  const u32x2 y = encode16x4<DT>(add_rest<DT>(x, a.rest[n], w, m, a.s.d) * a.meta->down);
+  PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
+  if (a.wide && m + 4 <= a.s.d) *(PT_GLOBAL u32x2*)(row + m) = y;
+  else
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q)
+      if (m + q < a.s.d) row[m + q] = uint16_t(y[q / 2] >> (16 * (q & 1)));
 }
 
 // d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
@@ -539,17 +551,33 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) 
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
-    if (n >= a.s.V) continue;
-    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + n * a.stride;
+    const bool live = n < a.s.V;
+    if (!a.read_acc && !a.write_acc) {
+      PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + n * a.stride;
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i) {
-      const uint32_t m = mb + i * 16;
-      if (m >= a.s.d) continue;
-      f32x4 x = t.acc[i][j] * down;
-      PT_GLOBAL f32x4* sum = (PT_GLOBAL f32x4*)((PT_GLOBAL float*)a.acc + size_t(n) * a.pitch + m);
-      if (a.read_acc) x += *sum;
-      if (a.write_acc) *sum = x;
-      else store4<DT>(row, m, a.s.d, a.wide, x);
+      for (int i = 0; i < T::FM; i += 2) {
+        const u32x4 x = eight(encode16x4<DT>(t.acc[i][j] * down), encode16x4<DT>(t.acc[i + 1][j] * down));
+        if (live) store8(row, tm * C::BM + t.wave_m() + i * 16 + eight_at(), a.s.d, a.wide, x);
+      }
+      continue;
+    }
+    // over several pieces: the sums so far, in fp32
+    const uint32_t at = live ? n : 0;
+    PT_GLOBAL float* sums = (PT_GLOBAL float*)a.acc + size_t(at) * a.pitch;
+    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + at * a.stride;
+#pragma unroll
+    for (int i = 0; i < T::FM; i += 2) {
+      u32x2 w[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t m = mb + (i + h) * 16;
+        f32x4 x = t.acc[i + h][j] * down;
+        if (a.read_acc && m < a.s.d) x += *(const PT_GLOBAL f32x4*)(sums + m);
+        if (a.write_acc && m < a.s.d && live) *(PT_GLOBAL f32x4*)(sums + m) = x;
+        w[h] = encode16x4<DT>(x);
+      }
+      const u32x4 x = eight(w[0], w[1]);
+      if (live && !a.write_acc) store8(row, tm * C::BM + t.wave_m() + i * 16 + eight_at(), a.s.d, a.wide, x);
     }
   }
 }
@@ -573,7 +601,7 @@ struct Plan {
   uint32_t parts, pitch, pieces, rows;
   bool grads, direct;                      // direct: the weight is taken where it lies
   uint32_t shared;                         // rows times workgroups a tile of d_hidden, at most
-  uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, sums, acc, total;
+  uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, g, g_pitch, sums, acc, total;
 };
 
 // Partial sums of a row's exponentials.
@@ -584,16 +612,25 @@ template <class C> void most_shared(const Shape& s, uint32_t rows, uint32_t& sha
   shared = grid = 0;
   const uint32_t tm = (s.d + C::BM - 1) / C::BM;
   for (uint32_t tn = 1; tn <= (rows + C::BN - 1) / C::BN; ++tn) {
-    const uint32_t n = shares<C>(tm * tn, s.Vp / TWO);
+    const uint32_t n = shares<C>(tm * tn, s.Vp / TWO).n;
     if (n > 1) shared = std::max(shared, n * rows);
     grid = std::max(grid, tile_grid(uint64_t(tm) * n, tn));
   }
 }
 
+// Whether d_hidden is sooner done in tiles of Mid.
+inline bool mid_hidden(const Shape& s, uint32_t rows) {
+  const auto ns = [&](auto c) {
+    typedef decltype(c) C;
+    return shares<C>((s.d + C::BM - 1) / C::BM * ((rows + C::BN - 1) / C::BN), s.Vp / TWO).ns;
+  };
+  return ns(Mid{}) < ns(Big{});
+}
+
 uint32_t shared_rows(const Shape& s, uint32_t rows) {
   uint32_t shared, grid;
   if (rows <= FEW_ROWS) most_shared<Few>(s, rows, shared, grid);
-  else if (mid_tiles(s.d, rows)) most_shared<Mid>(s, rows, shared, grid);
+  else if (mid_hidden(s, rows)) most_shared<Mid>(s, rows, shared, grid);
   else most_shared<Big>(s, rows, shared, grid);
   return shared;
 }
@@ -620,7 +657,14 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   p.packed = take(2ull * (up(h.rows, TWO) + p.s.low) * p.s.Kd);
   p.weight = take(p.direct ? 0 : 2ull * h.vocab * p.s.Kd);
   p.part = take(8ull * p.rows * p.parts);
-  p.z = take(p.grads ? (h.dtype == PT_BF16 ? KEPT_BYTES<PT_BF16> : KEPT_BYTES<PT_FP16>) * uint64_t(p.rows + p.s.low) * p.s.Vp : 0);
+  const uint64_t kept = h.dtype == PT_BF16 ? KEPT_BYTES<PT_BF16> : KEPT_BYTES<PT_FP16>;
+  p.z = take(p.grads ? kept * p.rows * p.s.Vp : 0);
+  p.g = p.z;
+  p.g_pitch = kept * p.s.Vp;
+  if (p.grads && h.rows <= LOW_ROWS) {
+    p.g_pitch = 2ull * p.s.Vp;
+    p.g = take(p.g_pitch * (up(h.rows, TWO) + p.s.low));
+  }
   if (h.d_hidden)                            // of a whole piece and of the last one
     for (uint32_t rows : {std::min(p.rows, h.rows), h.rows - (p.pieces - 1) * p.rows}) p.shared = std::max(p.shared, shared_rows(p.s, rows));
   p.sums = take(4ull * p.shared * p.pitch);
@@ -659,7 +703,7 @@ template <int DT, class C> int d_hidden(const GradArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_head_d_hidden<DT, C>), dim3(grid), dim3(C::THREADS), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_d_hidden");
   if (!shared) return PT_OK;
-  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(a.rows), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(a.rows, (a.s.d + 1023) / 1024), dim3(256), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_join");
   return PT_OK;
 }
@@ -701,7 +745,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   for (uint32_t i = 0; i < p.pieces && rc == PT_OK; ++i) {
     const uint32_t first = i * p.rows, rows = std::min(p.rows, s.R - first);
     uint16_t* hid = packed + size_t(first) * s.Kd;
-    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_tiles(s.d, rows), mid_w = mid_tiles(s.d, s.V);
+    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_hidden(s, rows), mid_w = mid_tiles(s.d, s.V);
     const LogitArgs la = {s, {weight, stride * 2, s.V, width}, {hid, 2ull * s.Kd, 0, s.Kd}, meta, first, rows, target_of + first, (f32x2*)(ws + p.part),
                           few ? parts<Few>(s.V) : mid ? parts<Mid>(s.V) : parts<Big>(s.V), (float*)(ws + p.at_target),
                           p.grads ? ws + p.z : nullptr};
@@ -709,25 +753,25 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     if (rc != PT_OK) return rc;
     const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.part, la.parts,
                          uint32_t(few ? Few::BM / Few::WM : mid ? Mid::BM / Mid::WM : Big::BM / Big::WM), la.at_target, h.row_scale, h.loss, ws + p.z,
-                         (float*)(ws + p.rest)};
+                         (uint16_t*)(ws + p.g), p.g_pitch, (float*)(ws + p.rest)};
     if (!p.grads) {
       hipLaunchKernelGGL(k_head_loss, dim3(rows), dim3(256), 0, st, sa);
       PT_LAUNCH_CHECK(nullptr, "k_head_loss");
       continue;
     }
-    hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO))), dim3(256), 0, st, sa);
+    const uint32_t slices = p.g == p.z ? 1 : std::max(1u, std::min((s.Vp + 2047) / 2048, 512 / rows));
+    hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO)), slices), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
-    const uint64_t z_pitch = uint64_t(KEPT_BYTES<DT>) * s.Vp;
-    GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.z, z_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
-                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 8 == 0 && h.d_hidden_stride % 4 == 0, p.pitch,
+    GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.g, p.g_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
+                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 16 == 0 && h.d_hidden_stride % 8 == 0, p.pitch,
                    (float*)(ws + p.sums), sa.rest, weight, stride, nullptr, false, false};
     if (h.d_hidden) rc = few ? d_hidden<DT, Few>(ga, st) : mid_h ? d_hidden<DT, Mid>(ga, st) : d_hidden<DT, Big>(ga, st);
     if (!h.d_weight || rc != PT_OK) continue;
     ga.p = {hid, 2ull * s.Kd, s.Kd, 0};
-    ga.q = {ws + p.z, z_pitch, s.Vp, 0};
+    ga.q = {ws + p.g, p.g_pitch, s.Vp, 0};
     ga.out = (uint16_t*)h.d_weight;
     ga.stride = h.d_weight_stride;
-    ga.wide = (uintptr_t)h.d_weight % 8 == 0 && h.d_weight_stride % 4 == 0;
+    ga.wide = (uintptr_t)h.d_weight % 16 == 0 && h.d_weight_stride % 8 == 0;
     ga.acc = (float*)(ws + p.acc);
     ga.read_acc = i > 0;
     ga.write_acc = i + 1 < p.pieces;
