@@ -208,6 +208,7 @@ struct LogitArgs {
   const Meta* meta;
   uint32_t first, rows;
   const uint32_t* target_of; // of the piece
+  const int64_t* target;     // the call's own rows instead, those without a target among them (then there are no gradients); or NULL
   f32x2* part;               // [rows][parts] of the piece: largest z, sum of exp(z - largest)
   uint32_t parts;
   float* at_target;          // [rows]
@@ -218,7 +219,7 @@ template <int DT, class C>
 __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
   typedef typename C::template Of<DT, true, true> T;
   __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
-  const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
+  const uint32_t n_rows = a.target ? a.rows : piece_rows(a.meta, a.first, a.rows);
   uint32_t tm, tn;
   if (!tile_of(blockIdx.x, (a.s.V + C::BM - 1) / C::BM, (n_rows + C::BN - 1) / C::BN, tm, tn)) return;
   const uint32_t m0 = tm * C::BM, n0 = tn * C::BN;
@@ -281,7 +282,8 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
     if (live && lane < 16) a.part[size_t(n) * a.parts + tm * C::WM + t.wave_m() / T::TM] = f32x2{big, sum};
-    const uint32_t y = live ? a.target_of[n] - mb : ~0u;              // the lane's z are mb + 16 i + q
+    uint32_t y = ~0u;                                                 // the lane's z are mb + 16 i + q
+    if (live) y = a.target ? (uint64_t(a.target[n]) < a.s.V ? uint32_t(a.target[n]) - mb : ~0u) : a.target_of[n] - mb;
     const bool mine = y < uint32_t(T::TM) && (y & 15) < 4;
     if (__any(mine)) {
       float zy = 0.0f;
@@ -311,6 +313,7 @@ struct SoftArgs {
   const Meta* meta;
   uint32_t first, rows;
   const uint32_t *row_of, *target_of;      // of the piece
+  const int64_t* target;                   // as in LogitArgs
   const f32x2* part;
   uint32_t parts, part_width;
   const float* at_target;
@@ -336,9 +339,11 @@ __device__ __forceinline__ f32x2 join_row(const f32x2* part, uint32_t parts) {
 // The loss alone: a workgroup a row.
 __global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
   const uint32_t r = blockIdx.x;
-  if (r >= piece_rows(a.meta, a.first, a.rows)) return;
+  if (r >= (a.target ? a.rows : piece_rows(a.meta, a.first, a.rows))) return;
   const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
-  if (threadIdx.x == 0) a.loss[a.row_of[r]] = x[0] + logf(x[1]) - a.at_target[r];
+  if (threadIdx.x != 0) return;
+  if (a.target) a.loss[r] = uint64_t(a.target[r]) < a.s.V ? x[0] + logf(x[1]) - a.at_target[r] : 0.0f;
+  else a.loss[a.row_of[r]] = x[0] + logf(x[1]) - a.at_target[r];
 }
 
 // Eight numbers in 16 bits, and what is left of them.
@@ -467,11 +472,22 @@ __device__ __forceinline__ f32x4 add_rest(f32x4 x, float rest, const PT_GLOBAL u
   return x;
 }
 
+// Tiles of the gradients at the end of the width: of Big's, 256 wide, what is left of the width is often a small part (width 1600: 64 of it), and takes a
+// narrower tile.  f: called with the tile.
+template <int DT, class C, bool PK, bool QK, class F>
+__device__ __forceinline__ void with_tile(uint32_t left, F&& f) {
+  if constexpr (C::BM == 256) {
+    if (left <= 64) return f(Tile<DT, PK, QK, 64, C::BN, 1, 8>{});
+    if (left <= 128) return f(Tile<DT, PK, QK, 128, C::BN, 2, 4>{});
+  }
+  f(typename C::template Of<DT, PK, QK>{});
+}
+
 // d_hidden of a piece: m runs over the width, n over rows, k over the vocabulary.
 template <int DT, class C>
 __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) {
-  typedef typename C::template Of<DT, false, true> T;
-  __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
+  constexpr int BYTES = C::template Of<DT, false, true>::BYTES;
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM, tiles_n = (n_rows + C::BN - 1) / C::BN, twos = a.s.Vp / TWO;
   const uint32_t share = shares<C>(tiles_m * tiles_n, twos).n;
@@ -481,34 +497,36 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) 
   tm -= part * tiles_m;
   Operand q = a.q;
   q.extent = n_rows;
-  T t;
-  t.run((lds_char*)even, (lds_char*)odd, a.p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
-  const uint32_t lane = threadIdx.x & 63, mb = tm * C::BM + t.wave_m() + (lane >> 4) * 4;
   const float down = a.meta->down;
+  with_tile<DT, C, false, true>(a.s.d - tm * C::BM, [&](auto t) {
+    typedef decltype(t) T;
+    t.run((lds_char*)even, (lds_char*)odd, a.p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+    const uint32_t lane = threadIdx.x & 63, mw = tm * C::BM + t.wave_m(), mb = mw + (lane >> 4) * 4;
 #pragma unroll
-  for (int j = 0; j < T::FN; ++j) {
-    const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
-    const bool live = n < n_rows;
-    if (share > 1) {
-      if (!live) continue;
-      PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.rows + n) * a.pitch;
+    for (int j = 0; j < T::FN; ++j) {
+      const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
+      const bool live = n < n_rows;
+      if (share > 1) {
+        if (!live) continue;
+        PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.rows + n) * a.pitch;
 #pragma unroll
-      for (int i = 0; i < T::FM; ++i)
-        if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
-      continue;
+        for (int i = 0; i < T::FM; ++i)
+          if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
+        continue;
+      }
+      const uint32_t at = live ? n : 0;                    // lanes without a row take part in the exchange
+      PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[at] * a.stride;
+      const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[at] * a.weight_stride;
+      const float rest = a.rest[at];
+#pragma unroll
+      for (int i = 0; i < T::FM; i += 2) {
+        const uint32_t m = mb + i * 16;
+        const u32x4 x = eight(encode16x4<DT>(add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down),
+                              encode16x4<DT>(add_rest<DT>(t.acc[i + 1][j], rest, w, m + 16, a.s.d) * down));
+        if (live) store8(row, mw + i * 16 + eight_at(), a.s.d, a.wide, x);
+      }
     }
-    const uint32_t at = live ? n : 0;                      // lanes without a row take part in the exchange
-    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[at] * a.stride;
-    const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[at] * a.weight_stride;
-    const float rest = a.rest[at];
-#pragma unroll
-    for (int i = 0; i < T::FM; i += 2) {
-      const uint32_t m = mb + i * 16;
-      const u32x4 x = eight(encode16x4<DT>(add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down),
-                            encode16x4<DT>(add_rest<DT>(t.acc[i + 1][j], rest, w, m + 16, a.s.d) * down));
-      if (live) store8(row, tm * C::BM + t.wave_m() + i * 16 + eight_at(), a.s.d, a.wide, x);
-    }
-  }
+  });
 }
 
 // Adds up what several workgroups a tile have left: a lane four results of a row.
@@ -536,61 +554,60 @@ __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
 // d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
 template <int DT, class C>
 __global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) {
-  typedef typename C::template Of<DT, false, false> T;
-  __shared__ __attribute__((aligned(16))) char even[T::BYTES], odd[T::BYTES];
+  constexpr int BYTES = C::template Of<DT, false, false>::BYTES;
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   if (!n_rows && a.read_acc && a.write_acc) return;
   uint32_t tm, tn;
   if (!tile_of(blockIdx.x, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
   Operand p = a.p, q = a.q;
   p.k = q.k = !n_rows ? 0 : a.s.low ? 2 * a.s.low : (n_rows + TWO - 1) / TWO * TWO;
-  T t;
-  t.run((lds_char*)even, (lds_char*)odd, p, q, tm * C::BM, tn * C::BN, 0, p.k / TWO);
-  const uint32_t lane = threadIdx.x & 63, mb = tm * C::BM + t.wave_m() + (lane >> 4) * 4;
   const float down = a.meta->down;
+  with_tile<DT, C, false, false>(a.s.d - tm * C::BM, [&](auto t) {
+    typedef decltype(t) T;
+    t.run((lds_char*)even, (lds_char*)odd, p, q, tm * C::BM, tn * C::BN, 0, p.k / TWO);
+    const uint32_t lane = threadIdx.x & 63, mw = tm * C::BM + t.wave_m(), mb = mw + (lane >> 4) * 4;
 #pragma unroll
-  for (int j = 0; j < T::FN; ++j) {
-    const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
-    const bool live = n < a.s.V;
-    if (!a.read_acc && !a.write_acc) {
-      PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + n * a.stride;
+    for (int j = 0; j < T::FN; ++j) {
+      const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
+      const bool live = n < a.s.V;
+      const uint32_t at = live ? n : 0;                    // lanes without a row take part in the exchange
+      PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + at * a.stride;
+      PT_GLOBAL float* sums = (PT_GLOBAL float*)a.acc + size_t(at) * a.pitch;          // of the pieces before, in fp32
 #pragma unroll
       for (int i = 0; i < T::FM; i += 2) {
-        const u32x4 x = eight(encode16x4<DT>(t.acc[i][j] * down), encode16x4<DT>(t.acc[i + 1][j] * down));
-        if (live) store8(row, tm * C::BM + t.wave_m() + i * 16 + eight_at(), a.s.d, a.wide, x);
-      }
-      continue;
-    }
-    // over several pieces: the sums so far, in fp32
-    const uint32_t at = live ? n : 0;
-    PT_GLOBAL float* sums = (PT_GLOBAL float*)a.acc + size_t(at) * a.pitch;
-    PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + at * a.stride;
+        u32x2 w[2];
 #pragma unroll
-    for (int i = 0; i < T::FM; i += 2) {
-      u32x2 w[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t m = mb + (i + h) * 16;
-        f32x4 x = t.acc[i + h][j] * down;
-        if (a.read_acc && m < a.s.d) x += *(const PT_GLOBAL f32x4*)(sums + m);
-        if (a.write_acc && m < a.s.d && live) *(PT_GLOBAL f32x4*)(sums + m) = x;
-        w[h] = encode16x4<DT>(x);
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t m = mb + (i + h) * 16;
+          f32x4 x = t.acc[i + h][j] * down;
+          if (a.read_acc && m < a.s.d) x += *(const PT_GLOBAL f32x4*)(sums + m);
+          if (a.write_acc && m < a.s.d && live) *(PT_GLOBAL f32x4*)(sums + m) = x;
+          w[h] = encode16x4<DT>(x);
+        }
+        const u32x4 x = eight(w[0], w[1]);
+        if (live && !a.write_acc) store8(row, mw + i * 16 + eight_at(), a.s.d, a.wide, x);
       }
-      const u32x4 x = eight(w[0], w[1]);
-      if (live && !a.write_acc) store8(row, tm * C::BM + t.wave_m() + i * 16 + eight_at(), a.s.d, a.wide, x);
     }
-  }
+  });
 }
 
 // ---- host -----------------------------------------------------------------------------------------------
 
 // Up to this many rows the gradient of the weight is a matter of writing it: what rounding G has left is multiplied as well, as rows of its own.
-constexpr uint32_t LOW_ROWS = 256, FEW_ROWS = 64;
+constexpr uint32_t LOW_ROWS = 128, FEW_ROWS = 64;
 
 // Whether a product of m x n is sooner done in tiles of Mid.
 inline bool mid_tiles(uint64_t m, uint64_t n) {
   const auto rounds = [&](uint64_t bm, uint64_t bn, uint64_t slots) { return ((m + bm - 1) / bm * ((n + bn - 1) / bn) + slots - 1) / slots; };
   return rounds(Mid::BM, Mid::BN, Mid::SLOTS) * Mid::TWO_NS < rounds(Big::BM, Big::BN, Big::SLOTS) * Big::TWO_NS;
+}
+// The same for d_weight, whose last tile of the width may be a narrower one.
+inline bool mid_weight(uint64_t d, uint64_t V) {
+  const uint64_t left = d % 256, tenths = d / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
+  const uint64_t big = (tenths * ((V + Big::BN - 1) / Big::BN) + Big::SLOTS * 10 - 1) / (Big::SLOTS * 10);
+  const uint64_t mid = ((d + Mid::BM - 1) / Mid::BM * ((V + Mid::BN - 1) / Mid::BN) + Mid::SLOTS - 1) / Mid::SLOTS;
+  return mid * Mid::TWO_NS < big * Big::TWO_NS;
 }
 
 uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
@@ -599,7 +616,7 @@ uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 struct Plan {
   Shape s;
   uint32_t parts, pitch, pieces, rows;
-  bool grads, direct;                      // direct: the weight is taken where it lies
+  bool grads, direct, as_is;               // direct: the weight is taken where it lies; as_is: so are the hidden states
   uint32_t shared;                         // rows times workgroups a tile of d_hidden, at most
   uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, g, g_pitch, sums, acc, total;
 };
@@ -641,6 +658,7 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   if (h.d_weight && h.rows <= LOW_ROWS) p.s.low = uint32_t(up(h.rows, BK));
   p.grads = h.d_hidden || h.d_weight;
   p.direct = h.width % BK == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
+  p.as_is = !p.grads && p.direct && h.rows <= FEW_ROWS && h.hidden_stride % 8 == 0 && (uintptr_t)h.hidden % 16 == 0;
   p.parts = std::max({parts<Few>(h.vocab), parts<Mid>(h.vocab), parts<Big>(h.vocab)});
   p.pitch = uint32_t(up(h.width, 4));
   p.rows = uint32_t(std::min<uint64_t>(rows, up(h.rows, PIECE_STEP)));
@@ -721,7 +739,9 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   uint16_t* packed = (uint16_t*)(ws + p.packed);
   const RowArgs ra = {h.target, h.row_scale, s, meta, row_of, target_of};
   const dim3 gather(uint32_t(up(s.R, TWO) / 4));
-  if (s.R <= LISTED) {
+  if (p.as_is) {
+    // few rows, of which the losses alone are wanted: those without a target are multiplied too, and two launches do
+  } else if (s.R <= LISTED) {
     hipLaunchKernelGGL(k_head_gather<true>, gather, dim3(256), 0, st, ra, (const uint16_t*)h.hidden, h.hidden_stride, packed, h.loss, (uint16_t*)h.d_hidden,
                        h.d_hidden_stride);
   } else {
@@ -745,13 +765,14 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   for (uint32_t i = 0; i < p.pieces && rc == PT_OK; ++i) {
     const uint32_t first = i * p.rows, rows = std::min(p.rows, s.R - first);
     uint16_t* hid = packed + size_t(first) * s.Kd;
-    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_hidden(s, rows), mid_w = mid_tiles(s.d, s.V);
-    const LogitArgs la = {s, {weight, stride * 2, s.V, width}, {hid, 2ull * s.Kd, 0, s.Kd}, meta, first, rows, target_of + first, (f32x2*)(ws + p.part),
+    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_hidden(s, rows), mid_w = mid_weight(s.d, s.V);
+    const Operand hidden = p.as_is ? Operand{h.hidden, h.hidden_stride * 2, 0, s.d} : Operand{hid, 2ull * s.Kd, 0, s.Kd};
+    const LogitArgs la = {s, {weight, stride * 2, s.V, width}, hidden, meta, first, rows, target_of + first, p.as_is ? h.target : nullptr, (f32x2*)(ws + p.part),
                           few ? parts<Few>(s.V) : mid ? parts<Mid>(s.V) : parts<Big>(s.V), (float*)(ws + p.at_target),
                           p.grads ? ws + p.z : nullptr};
     rc = few ? logits<DT, Few>(la, st) : mid ? logits<DT, Mid>(la, st) : logits<DT, Big>(la, st);
     if (rc != PT_OK) return rc;
-    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.part, la.parts,
+    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.target, la.part, la.parts,
                          uint32_t(few ? Few::BM / Few::WM : mid ? Mid::BM / Mid::WM : Big::BM / Big::WM), la.at_target, h.row_scale, h.loss, ws + p.z,
                          (uint16_t*)(ws + p.g), p.g_pitch, (float*)(ws + p.rest)};
     if (!p.grads) {

@@ -29,8 +29,8 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// One operand of a product.  What lies behind its m (or n) and behind its last k is loaded as zero, or as what lies between its rows where the
-// result is not used; a row that ends inside a step (k next to each other, k no multiple of 64) must be followed by zeros there.
+// One operand of a product.  What lies behind its m (or n) and behind its last k is loaded as zero, or, of m and n, as what lies between its rows: the
+// result is not used.  Where k lies next to each other it is a multiple of 64.
 struct Operand {
   const void* at;
   uint64_t pitch;            // bytes from one row in memory to the next
@@ -46,6 +46,7 @@ struct Stage {
   static constexpr int BYTES = B * BK * 2;
   static_assert(N >= 1 && THREADS % PER_ROW == 0 && THREADS / PER_ROW % (KC ? 8 : 16) == 0, "a lane's pieces lie alike in their rows");
   uint64_t base, end, step;  // of the step to be fetched next; behind the operand's last element
+  uint64_t stop;             // `base` behind the last step
   uint32_t off, rows;        // the lane's first piece, and from there to its next one
   uint32_t lane_at;          // where in a buffer the lane's first k of the first row of its wave lies
 
@@ -63,6 +64,7 @@ struct Stage {
     }
     base = uint64_t(o.at) + (KC ? mn0 * o.pitch + uint64_t(k0) * 2 : k0 * o.pitch + uint64_t(mn0) * 2);
     end = uint64_t(o.at) + (KC ? (o.extent - 1) * o.pitch + uint64_t(o.k) * 2 : (o.k - 1) * o.pitch + uint64_t(o.extent) * 2);
+    stop = KC ? base + uint64_t(o.k - min(k0, o.k)) * 2 : end;
     step = KC ? BK * 2 : BK * o.pitch;
     const uint32_t row = threadIdx.x / PER_ROW, c = (threadIdx.x % PER_ROW) ^ swizzle(row);
     off = row * uint32_t(o.pitch) + c * 16;
@@ -70,7 +72,7 @@ struct Stage {
   }
   // Fetches piece i of the lane's N of the step at `base` to `to`.  The hardware checks the range.
   __device__ __forceinline__ void fetch(lds_char* to, int i) const {
-    const uint64_t left = base < end ? end - base : 0;
+    const uint64_t left = base < stop ? end - base : 0;
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, left > 0xffffffffull ? 0xffffffffu : uint32_t(left), 0x27000);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + (wave * 64 + i * THREADS) * 16), 16, off, i * rows, 0, 0);
