@@ -32,7 +32,7 @@ typedef u32x4 u32x4_a __attribute__((aligned(2)));
 constexpr uint32_t BLOCK = 256;              // elements of a block: a wave's, and those that share a scale
 constexpr uint32_t UNIT = 4096;              // elements a wave of the norm takes at a time
 constexpr uint32_t COARSE = 16;              // blocks / units per entry of the look-up tables
-constexpr uint32_t NORM_THREADS = 256, NORM_BLOCKS = 1024, NORM_WAVES = NORM_THREADS / 64;
+constexpr uint32_t NORM_THREADS = 256, NORM_BLOCKS = 512, NORM_WAVES = NORM_THREADS / 64;
 
 constexpr uint32_t ALIGNED = 1u << 31;       // of Desc::flags: a block's arrays begin at multiples of what a lane stores
 

@@ -68,22 +68,23 @@ def call(c, grads="both", workspace=None, pad=0, shift=0, stream=None):
     return loss, dh, dw
 
 
-def expected(c):
-    """Loss and gradients in 64 bits and their bounds, on the host."""
+def expected(c, where="cpu"):
+    """Loss and gradients in 64 bits and their bounds, on the host or the device."""
     dt = c["hidden"].dtype
     u, tiny = next((u, t) for d, u, t in DTYPES.values() if d == dt)
-    w = c["weight"].double().cpu()
-    y = c["target"].cpu()
+    w = c["weight"].double().to(where)
+    y = c["target"].to(where)
     on = ((y >= 0) & (y < w.shape[0])).nonzero()[:, 0]
     rows, width = c["hidden"].shape
-    h = c["hidden"].double().cpu()[on]
-    s = torch.ones(rows, dtype=torch.float64) if c["scale"] is None else c["scale"].double().cpu()
+    h = c["hidden"].double().to(where)[on]
+    s = torch.ones(rows, dtype=torch.float64, device=where) if c["scale"] is None else c["scale"].double().to(where)
     s, yy = s[on], y[on]
     z = h @ w.t()
-    D = (width + 64) * E * (h.abs() @ w.abs().t()).amax(1) if len(on) else torch.zeros(0, dtype=torch.float64)
+    D = (width + 64) * E * (h.abs() @ w.abs().t()).amax(1) if len(on) else torch.zeros(0, dtype=torch.float64, device=where)
     logp = torch.log_softmax(z, 1)
-    i = torch.arange(len(on))
-    loss, loss_b = torch.zeros(rows, dtype=torch.float64), torch.zeros(rows, dtype=torch.float64)
+    del z
+    i = torch.arange(len(on), device=where)
+    loss, loss_b = (torch.zeros(rows, dtype=torch.float64, device=where) for _ in range(2))
     loss[on], loss_b[on] = -logp[i, yy], 2 * D + 2e-5 + 4 * E * logp[i, yy].abs()
     p = logp.exp()
     g = p.clone()
@@ -91,7 +92,7 @@ def expected(c):
     big = float(s.abs().max()) if len(on) else 0.0
     dg = s.abs()[:, None] * (u * g.abs() + (2 * D + 2e-5)[:, None] * p) + big * 2.0 ** -38
     g = g * s[:, None]
-    dh, dh_b = torch.zeros(rows, width, dtype=torch.float64), torch.zeros(rows, width, dtype=torch.float64)
+    dh, dh_b = (torch.zeros(rows, width, dtype=torch.float64, device=where) for _ in range(2))
     dh[on] = g @ w
     dh_b[on] = dg @ w.abs() + (w.shape[0] + 64) * E * (g.abs() @ w.abs())
     dw, dw_b = g.t() @ h, dg.t() @ h.abs() + (len(on) + 64) * E * (g.abs().t() @ h.abs())
@@ -106,7 +107,7 @@ def check(got, want, grads="both"):
     for name, x, w, b in (("loss", got[0], loss, loss_b), ("d_hidden", got[1], dh, dh_b), ("d_weight", got[2], dw, dw_b)):
         if x is None:
             continue
-        off = (x.double().cpu() - w).abs()
+        off = (x.double().to(w.device) - w).abs()
         assert bool((off <= b).all()), f"{name}: worst {float((off / b.clamp(min=1e-300)).max()):.3g} of the bound"
 
 
@@ -121,6 +122,40 @@ def test_against_64_bits(rows, width, vocab, dtype):
     want = expected(c)
     check(call(c), want)
     check(call(c, grads="none"), want)
+
+
+# sizes that take tiles of 256 x 256: with the last 64, 128 and 3 of the width in narrower ones, workgroups that share a tile's k, several pieces
+LARGE = [(1024, 320, 12800, None), (1024, 384, 12800, None), (700, 515, 20000, None), (300, 320, 40000, None), (1300, 256, 25000, "least"),
+         (2100, 640, 9000, None)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,vocab,workspace", LARGE)
+def test_large_tiles(rows, width, vocab, workspace, dtype):
+    c = case(rows, width, vocab, dtype, ignored=0.1)
+    check(call(c, workspace=workspace), expected(c, "cuda"))
+
+
+def test_logits_beyond_32_bits():
+    """What is kept of a piece's logits is 4.3 GB: rows whose place passes 2^32 bytes."""
+    c = case(8192, 64, 131072, "fp16")
+    c["scale"] *= 1024.0
+    check(call(c), expected(c, "cuda"))
+
+
+@pytest.mark.parametrize("rows", [1, 20, 64, 65])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 8), (4, 0), (0, 1)])
+def test_losses_alone_of_few_rows(rows, pad, shift):
+    """Rows that are multiplied where they lie, and those that cannot be; ones without a target hold infinities."""
+    c = case(rows, 192, 1000, "bf16", ignored=0.3, pad=pad, shift=shift)
+    c["hidden"][c["target"] < 0] = float("inf")
+    check(call(c, grads="none"), expected(c))
+
+
+@pytest.mark.parametrize("rows", [128, 129])
+def test_either_side_of_the_rows_whose_rounding_is_made_good(rows):
+    c = case(rows, 200, 900, "bf16", ignored=0.1)
+    check(call(c), expected(c))
 
 
 @pytest.mark.parametrize("grads", ["hidden", "weight"])

@@ -389,3 +389,42 @@ def test_many_small_tensors():
         l.step()
         check(l, before, l.host(), 1)
         l.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_beyond_32_bits(bits):
+    """1.2e9 elements, 4.8 GB of master weights: the last ones are those of a small list with the same random numbers."""
+    n, tail = 1_200_000_000, 1000
+    base = n - tail - (n - tail) % 256
+    small = List([n - base], bits, dtype=torch.bfloat16)
+    w = torch.zeros(n, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    kind = torch.float32 if bits == 32 else torch.uint8
+    m, v = torch.zeros(n, dtype=kind, device="cuda"), torch.zeros(n, dtype=kind, device="cuda")
+    ms, vs = ((torch.zeros(-(-n // 256), device="cuda") for _ in range(2)) if bits == 8 else (None, None))
+    for big, part in ((w, small.w), (g, small.g), (p, small.p), (m, small.m), (v, small.v)):
+        big[base:].copy_(part[0])
+    if bits == 8:
+        ms[base // 256:].copy_(small.ms[0]), vs[base // 256:].copy_(small.vs[0])
+    before = small.host()
+    l = B.pt_tensors_create(B.PT_BF16, [B.tensor(g, w, m, v, p, ms, vs)], bits, None, 3)
+    B.pt_tensors_grad_sqnorm(l)
+    B.pt_tensors_adamw_step(l, B.hparams(**HP))
+    torch.cuda.synchronize()
+    for big, part in ((w, small.w), (p, small.p), (m, small.m), (v, small.v)):
+        part[0].copy_(big[base:])
+    if bits == 8:
+        small.ms[0].copy_(ms[base // 256:]), small.vs[0].copy_(vs[base // 256:])
+    global randoms                                            # of the last blocks of the large tensor
+    inner, first = randoms, base // 256
+
+    def shifted(sizes, seed, t):
+        return [tuple(x[first * 256:] for x in r) for r in inner([n], seed, t)]
+    try:
+        randoms = shifted
+        check(small, before, small.host(), 1)
+    finally:
+        randoms = inner
+    B.pt_tensors_destroy(l)
+    small.close()
