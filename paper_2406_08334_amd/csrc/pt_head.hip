@@ -47,6 +47,16 @@ struct Shape {
 
 // ---- rows ---------------------------------------------------------------------------------------------
 
+constexpr uint32_t NO_TARGET = ~0u;
+
+// big: the largest scale.
+__device__ __forceinline__ Meta found_rows(uint32_t n, float big) {
+  int e = 0;
+  if (big > 0.0f && big < 3.4e38f) (void)frexpf(big, &e);       // big < 2^e
+  e = max(-100, min(100, 14 - e));
+  return {n, ldexpf(1.0f, e), ldexpf(1.0f, -e)};
+}
+
 // The rows that have a target, in order, by a workgroup of THREADS.
 struct RowArgs {
   const int64_t* target;
@@ -84,10 +94,7 @@ __device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& eac
   __syncthreads();
 #pragma unroll
   for (uint32_t w = 0; w < WAVES; ++w) big = fmaxf(big, s_big[w]);
-  int e = 0;
-  if (big > 0.0f && big < 3.4e38f) (void)frexpf(big, &e);       // big < 2^e
-  e = max(-100, min(100, 14 - e));
-  found = {n, ldexpf(1.0f, e), ldexpf(1.0f, -e)};
+  found = found_rows(n, big);
 }
 
 // One workgroup lists the rows of a call.
@@ -310,10 +317,13 @@ __device__ __forceinline__ f32x2 join_wave(f32x2 x) {
 
 struct SoftArgs {
   Shape s;
-  const Meta* meta;
+  Meta* meta;
   uint32_t first, rows;
-  const uint32_t *row_of, *target_of;      // of the piece
+  uint32_t *row_of, *target_of;            // of the piece
   const int64_t* target;                   // as in LogitArgs
+  const uint16_t* hidden;                  // of such rows, and where they go
+  uint64_t hidden_stride;
+  uint16_t* packed;
   const f32x2* part;
   uint32_t parts, part_width;
   const float* at_target;
@@ -364,14 +374,56 @@ __device__ __forceinline__ u32x4 pack8_rest(const float (&x)[8], const u32x4& q)
 // (gridDim.y) share a row.
 // Of z in fp32, which are twice as long, a round takes 2048: a lane has its own of the next round under way while it stores those of this one,
 // and stores when every lane has this round's.
+// Rows as they are (few; SoftArgs::target): every one has its place, those without a target a G of zero, and the workgroups behind those of G do what
+// gathering does before otherwise.
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
-  const uint32_t r = blockIdx.x, tid = threadIdx.x, n = piece_rows(a.meta, a.first, a.rows);
+  uint32_t r = blockIdx.x, n, y = NO_TARGET;
+  const uint32_t tid = threadIdx.x;
+  float up;
+  if (a.target) {
+    if (r >= TWO) {
+      if (blockIdx.y) return;
+      r -= TWO;
+      const bool has = r < a.rows && uint64_t(a.target[r]) < a.s.V;
+      for (uint32_t at = r; at <= r + a.s.low; at += a.s.low) {
+        PT_GLOBAL uint16_t* to = (PT_GLOBAL uint16_t*)a.packed + size_t(at) * a.s.Kd;
+        if (has) copy_row((const PT_GLOBAL uint16_t*)a.hidden + r * a.hidden_stride, to, a.s.d, a.s.Kd, tid, 256);
+        else
+          for (uint32_t c = tid * 8; c < a.s.Kd; c += 2048) *(PT_GLOBAL u32x4*)(to + c) = u32x4{0, 0, 0, 0};
+      }
+      return;
+    }
+    // a wave sees all rows
+    const uint32_t lane = tid & 63;
+    const int64_t t = lane < a.rows ? a.target[lane] : -1;
+    const bool has = uint64_t(t) < a.s.V;
+    float big = has ? (a.scale ? __builtin_fabsf(a.scale[lane]) : 1.0f) : 0.0f;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) big = fmaxf(big, __shfl_xor(big, off, 64));
+    const Meta m = found_rows(a.rows, big);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && tid < a.rows) {
+      a.row_of[tid] = tid;
+      a.target_of[tid] = has ? uint32_t(t) : NO_TARGET;
+      if (!has) { a.loss[tid] = 0.0f; a.rest[tid] = 0.0f; }
+      if (tid == 0) *a.meta = m;
+    }
+    up = m.up;
+    n = a.rows;
+    if (r < n) {
+      const int64_t own = a.target[r];
+      if (uint64_t(own) < a.s.V) y = uint32_t(own);
+    }
+  } else {
+    n = piece_rows(a.meta, a.first, a.rows);
+    up = a.meta->up;
+    if (r < n) y = a.target_of[r];
+  }
   if (r >= (a.s.low ? a.s.low : (n + TWO - 1) / TWO * TWO)) return;
   PT_GLOBAL uint16_t* g = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)a.g + r * a.g_pitch);
   PT_GLOBAL uint16_t* g_low = (PT_GLOBAL uint16_t*)((PT_GLOBAL char*)g + a.s.low * a.g_pitch);
   const uint32_t first = blockIdx.y * 2048 + tid * 8, turn = gridDim.y * 2048;
-  if (r >= n) {                                            // rows up to a whole step: zero
+  if (y == NO_TARGET) {                                    // rows up to a whole step too: zero
     for (uint32_t c = first; c < a.s.Vp; c += turn) {
       *(PT_GLOBAL u32x4*)(g + c) = u32x4{0, 0, 0, 0};
       if (a.s.low) *(PT_GLOBAL u32x4*)(g_low + c) = u32x4{0, 0, 0, 0};
@@ -379,8 +431,8 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     return;
   }
   const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
-  const uint32_t row = a.row_of[r], y = a.target_of[r];
-  const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * a.meta->up;
+  const uint32_t row = a.target ? r : a.row_of[r];
+  const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * up;
   const float off = lse * LOG2E, gy = s * expm1f(zy - lse);
   if (tid == 0 && blockIdx.y == 0) {
     a.loss[row] = lse - zy;
@@ -485,14 +537,12 @@ __device__ __forceinline__ void with_tile(uint32_t left, F&& f) {
 
 // d_hidden of a piece: m runs over the width, n over rows, k over the vocabulary.
 template <int DT, class C>
-__global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) {
-  constexpr int BYTES = C::template Of<DT, false, true>::BYTES;
-  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+__device__ __forceinline__ void d_hidden_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM, tiles_n = (n_rows + C::BN - 1) / C::BN, twos = a.s.Vp / TWO;
   const uint32_t share = shares<C>(tiles_m * tiles_n, twos).n;
   uint32_t tm, tn;
-  if (!tile_of(blockIdx.x, tiles_m * share, tiles_n, tm, tn)) return;
+  if (!tile_of(block, tiles_m * share, tiles_n, tm, tn)) return;
   const uint32_t part = tm / tiles_m, t0 = uint32_t(uint64_t(twos) * part / share), t1 = uint32_t(uint64_t(twos) * (part + 1) / share);
   tm -= part * tiles_m;
   Operand q = a.q;
@@ -500,7 +550,7 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) 
   const float down = a.meta->down;
   with_tile<DT, C, false, true>(a.s.d - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
-    t.run((lds_char*)even, (lds_char*)odd, a.p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+    t.run(even, odd, a.p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
     const uint32_t lane = threadIdx.x & 63, mw = tm * C::BM + t.wave_m(), mb = mw + (lane >> 4) * 4;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -516,17 +566,26 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) 
       }
       const uint32_t at = live ? n : 0;                    // lanes without a row take part in the exchange
       PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[at] * a.stride;
-      const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[at] * a.weight_stride;
+      const uint32_t y = a.target_of[at];
+      const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + (y == NO_TARGET ? 0 : y) * a.weight_stride;
       const float rest = a.rest[at];
 #pragma unroll
       for (int i = 0; i < T::FM; i += 2) {
         const uint32_t m = mb + i * 16;
-        const u32x4 x = eight(encode16x4<DT>(add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down),
-                              encode16x4<DT>(add_rest<DT>(t.acc[i + 1][j], rest, w, m + 16, a.s.d) * down));
+        u32x4 x = eight(encode16x4<DT>(add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down),
+                        encode16x4<DT>(add_rest<DT>(t.acc[i + 1][j], rest, w, m + 16, a.s.d) * down));
+        if (y == NO_TARGET) x = u32x4{0, 0, 0, 0};         // whatever the weight holds
         if (live) store8(row, mw + i * 16 + eight_at(), a.s.d, a.wide, x);
       }
     }
   });
+}
+
+template <int DT, class C>
+__global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) {
+  constexpr int BYTES = C::template Of<DT, false, true>::BYTES;
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+  d_hidden_tile<DT, C>(a, (lds_char*)even, (lds_char*)odd, blockIdx.x);
 }
 
 // Adds up what several workgroups a tile have left: a lane four results of a row.
@@ -541,8 +600,12 @@ __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
   for (uint32_t k = 0; k < share; ++k) x += *(const PT_GLOBAL f32x4*)(part + k * next);
-  const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + a.target_of[n] * a.weight_stride;
-  const u32x2 y = encode16x4<DT>(add_rest<DT>(x, a.rest[n], w, m, a.s.d) * a.meta->down);
+  const uint32_t target = a.target_of[n];
+  u32x2 y = {0, 0};
+  if (target != NO_TARGET) {
+    const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + target * a.weight_stride;
+    y = encode16x4<DT>(add_rest<DT>(x, a.rest[n], w, m, a.s.d) * a.meta->down);
+  }
   PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
   if (a.wide && m + 4 <= a.s.d) *(PT_GLOBAL u32x2*)(row + m) = y;
   else
@@ -553,19 +616,17 @@ __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
 
 // d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
 template <int DT, class C>
-__global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) {
-  constexpr int BYTES = C::template Of<DT, false, false>::BYTES;
-  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+__device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   if (!n_rows && a.read_acc && a.write_acc) return;
   uint32_t tm, tn;
-  if (!tile_of(blockIdx.x, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
+  if (!tile_of(block, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
   Operand p = a.p, q = a.q;
   p.k = q.k = !n_rows ? 0 : a.s.low ? 2 * a.s.low : (n_rows + TWO - 1) / TWO * TWO;
   const float down = a.meta->down;
   with_tile<DT, C, false, false>(a.s.d - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
-    t.run((lds_char*)even, (lds_char*)odd, p, q, tm * C::BM, tn * C::BN, 0, p.k / TWO);
+    t.run(even, odd, p, q, tm * C::BM, tn * C::BN, 0, p.k / TWO);
     const uint32_t lane = threadIdx.x & 63, mw = tm * C::BM + t.wave_m(), mb = mw + (lane >> 4) * 4;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -590,6 +651,23 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) 
       }
     }
   });
+}
+
+template <int DT, class C>
+__global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) {
+  constexpr int BYTES = C::template Of<DT, false, false>::BYTES;
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+  d_weight_tile<DT, C>(a, (lds_char*)even, (lds_char*)odd, blockIdx.x);
+}
+
+// Both gradients of few rows in one launch: neither fills the chip for long.
+template <int DT>
+__global__ void __launch_bounds__(256) k_head_few_grads(const GradArgs h, const GradArgs w, uint32_t blocks_h) {
+  static_assert(Few::THREADS == 256 && Mid::THREADS == 256, "one launch");
+  constexpr int BYTES = std::max(Few::Of<DT, false, true>::BYTES, Mid::Of<DT, false, false>::BYTES);
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+  if (blockIdx.x < blocks_h) d_hidden_tile<DT, Few>(h, (lds_char*)even, (lds_char*)odd, blockIdx.x);
+  else d_weight_tile<DT, Mid>(w, (lds_char*)even, (lds_char*)odd, blockIdx.x - blocks_h);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------
@@ -658,7 +736,7 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   if (h.d_weight && h.rows <= LOW_ROWS) p.s.low = uint32_t(up(h.rows, BK));
   p.grads = h.d_hidden || h.d_weight;
   p.direct = h.width % BK == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
-  p.as_is = !p.grads && p.direct && h.rows <= FEW_ROWS && h.hidden_stride % 8 == 0 && (uintptr_t)h.hidden % 16 == 0;
+  p.as_is = p.direct && h.rows <= FEW_ROWS && h.hidden_stride % 8 == 0 && (uintptr_t)h.hidden % 16 == 0;
   p.parts = std::max({parts<Few>(h.vocab), parts<Mid>(h.vocab), parts<Big>(h.vocab)});
   p.pitch = uint32_t(up(h.width, 4));
   p.rows = uint32_t(std::min<uint64_t>(rows, up(h.rows, PIECE_STEP)));
@@ -715,15 +793,26 @@ template <int DT, class C> int logits(const LogitArgs& a, hipStream_t st) {
   PT_LAUNCH_CHECK(nullptr, "k_head_logits");
   return PT_OK;
 }
+template <int DT, class C> int join_hidden(const GradArgs& a, uint32_t shared, hipStream_t st) {
+  if (!shared) return PT_OK;
+  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(a.rows, (a.s.d + 1023) / 1024), dim3(256), 0, st, a);
+  PT_LAUNCH_CHECK(nullptr, "k_head_join");
+  return PT_OK;
+}
 template <int DT, class C> int d_hidden(const GradArgs& a, hipStream_t st) {
   uint32_t shared, grid;
   most_shared<C>(a.s, a.rows, shared, grid);
   hipLaunchKernelGGL((k_head_d_hidden<DT, C>), dim3(grid), dim3(C::THREADS), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_d_hidden");
-  if (!shared) return PT_OK;
-  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(a.rows, (a.s.d + 1023) / 1024), dim3(256), 0, st, a);
-  PT_LAUNCH_CHECK(nullptr, "k_head_join");
-  return PT_OK;
+  return join_hidden<DT, C>(a, shared, st);
+}
+template <int DT> int few_grads(const GradArgs& h, const GradArgs& w, hipStream_t st) {
+  uint32_t shared, grid;
+  most_shared<Few>(h.s, h.rows, shared, grid);
+  hipLaunchKernelGGL(k_head_few_grads<DT>, dim3(grid + tile_grid((w.s.d + Mid::BM - 1) / Mid::BM, (w.s.V + Mid::BN - 1) / Mid::BN)), dim3(256), 0, st, h, w,
+                     grid);
+  PT_LAUNCH_CHECK(nullptr, "k_head_few_grads");
+  return join_hidden<DT, Few>(h, shared, st);
 }
 template <int DT, class C> int d_weight(const GradArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_head_d_weight<DT, C>), dim3(tile_grid((a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN)), dim3(C::THREADS), 0, st, a);
@@ -740,7 +829,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   const RowArgs ra = {h.target, h.row_scale, s, meta, row_of, target_of};
   const dim3 gather(uint32_t(up(s.R, TWO) / 4));
   if (p.as_is) {
-    // few rows, of which the losses alone are wanted: those without a target are multiplied too, and two launches do
+    // few rows: those without a target are multiplied too, and what else gathering does is done with G
   } else if (s.R <= LISTED) {
     hipLaunchKernelGGL(k_head_gather<true>, gather, dim3(256), 0, st, ra, (const uint16_t*)h.hidden, h.hidden_stride, packed, h.loss, (uint16_t*)h.d_hidden,
                        h.d_hidden_stride);
@@ -772,7 +861,8 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
                           p.grads ? ws + p.z : nullptr};
     rc = few ? logits<DT, Few>(la, st) : mid ? logits<DT, Mid>(la, st) : logits<DT, Big>(la, st);
     if (rc != PT_OK) return rc;
-    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.target, la.part, la.parts,
+    const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.target, (const uint16_t*)h.hidden,
+                         h.hidden_stride, packed, la.part, la.parts,
                          uint32_t(few ? Few::BM / Few::WM : mid ? Mid::BM / Mid::WM : Big::BM / Big::WM), la.at_target, h.row_scale, h.loss, ws + p.z,
                          (uint16_t*)(ws + p.g), p.g_pitch, (float*)(ws + p.rest)};
     if (!p.grads) {
@@ -781,22 +871,26 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
       continue;
     }
     const uint32_t slices = p.g == p.z ? 1 : std::max(1u, std::min((s.Vp + 2047) / 2048, 512 / rows));
-    hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO)), slices), dim3(256), 0, st, sa);
+    hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO)) + (p.as_is ? s.low : 0), slices), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
-    GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.g, p.g_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
+    const GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.g, p.g_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
                    (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 16 == 0 && h.d_hidden_stride % 8 == 0, p.pitch,
                    (float*)(ws + p.sums), sa.rest, weight, stride, nullptr, false, false};
+    GradArgs gw = ga;
+    gw.p = {hid, 2ull * s.Kd, s.Kd, 0};
+    gw.q = {ws + p.g, p.g_pitch, s.Vp, 0};
+    gw.out = (uint16_t*)h.d_weight;
+    gw.stride = h.d_weight_stride;
+    gw.wide = (uintptr_t)h.d_weight % 16 == 0 && h.d_weight_stride % 8 == 0;
+    gw.acc = (float*)(ws + p.acc);
+    gw.read_acc = i > 0;
+    gw.write_acc = i + 1 < p.pieces;
+    if (few && h.d_hidden && h.d_weight) {
+      rc = few_grads<DT>(ga, gw, st);
+      continue;
+    }
     if (h.d_hidden) rc = few ? d_hidden<DT, Few>(ga, st) : mid_h ? d_hidden<DT, Mid>(ga, st) : d_hidden<DT, Big>(ga, st);
-    if (!h.d_weight || rc != PT_OK) continue;
-    ga.p = {hid, 2ull * s.Kd, s.Kd, 0};
-    ga.q = {ws + p.g, p.g_pitch, s.Vp, 0};
-    ga.out = (uint16_t*)h.d_weight;
-    ga.stride = h.d_weight_stride;
-    ga.wide = (uintptr_t)h.d_weight % 16 == 0 && h.d_weight_stride % 8 == 0;
-    ga.acc = (float*)(ws + p.acc);
-    ga.read_acc = i > 0;
-    ga.write_acc = i + 1 < p.pieces;
-    rc = mid_w ? d_weight<DT, Mid>(ga, st) : d_weight<DT, Big>(ga, st);
+    if (h.d_weight && rc == PT_OK) rc = mid_w ? d_weight<DT, Mid>(gw, st) : d_weight<DT, Big>(gw, st);
   }
   return rc;
 }
