@@ -24,7 +24,8 @@ typedef u32x4 u32x4_a __attribute__((aligned(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t PIECE_STEP = 256;       // pieces are multiples of this many rows
-constexpr uint32_t PIECE_BEST = 8192;
+// Of a piece at best: this many rows, or, of a small vocabulary, as many as keep this many bytes of logits.
+constexpr uint64_t PIECE_BEST = 8192, PIECE_BYTES = 1ull << 30, PIECE_MOST = 32768;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // What is kept of the logits of a piece.  bf16 inputs: exp(z - the largest of the wave's part of the row) as an fp16 number, 2^15 being 1: a rounding of 2^-12
@@ -67,25 +68,39 @@ struct RowArgs {
 };
 template <int THREADS, class F>
 __device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& each) {
-  constexpr uint32_t WAVES = THREADS / 64;
-  __shared__ uint32_t s_n[WAVES];
+  constexpr uint32_t WAVES = THREADS / 64, TURN = 4;       // rows of a lane at a time: their loads are under way together
+  __shared__ uint32_t s_n[TURN * WAVES];
   __shared__ float s_big[WAVES];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t n = 0;
   float big = 0.0f;
-  for (uint32_t r0 = 0; r0 < a.s.R; r0 += THREADS) {
-    const uint32_t r = r0 + threadIdx.x;
-    const int64_t y = r < a.s.R ? a.target[r] : -1;
-    const bool has = uint64_t(y) < a.s.V;
-    if (has) big = fmaxf(big, a.scale ? __builtin_fabsf(a.scale[r]) : 1.0f);
-    const uint64_t mask = __ballot(has);
-    if (lane == 0) s_n[wave] = uint32_t(__popcll(mask));
-    __syncthreads();
-    uint32_t before = 0, all = 0;
+  for (uint32_t r0 = 0; r0 < a.s.R; r0 += TURN * THREADS) {
+    int64_t y[TURN];
+    float scale[TURN];
+    uint64_t mask[TURN];
 #pragma unroll
-    for (uint32_t w = 0; w < WAVES; ++w) { const uint32_t k = s_n[w]; before += w < wave ? k : 0; all += k; }
-    if (has) each(n + before + uint32_t(__popcll(mask & ((uint64_t(1) << lane) - 1))), r, uint32_t(y));
-    n += all;
+    for (uint32_t q = 0; q < TURN; ++q) {
+      const uint32_t r = r0 + q * THREADS + threadIdx.x;
+      y[q] = r < a.s.R ? a.target[r] : -1;
+      scale[q] = r < a.s.R && a.scale ? __builtin_fabsf(a.scale[r]) : 1.0f;
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < TURN; ++q) {
+      const bool has = uint64_t(y[q]) < a.s.V;
+      if (has) big = fmaxf(big, scale[q]);
+      mask[q] = __ballot(has);
+      if (lane == 0) s_n[q * WAVES + wave] = uint32_t(__popcll(mask[q]));
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t q = 0; q < TURN; ++q) {
+      uint32_t before = 0, all = 0;
+#pragma unroll
+      for (uint32_t w = 0; w < WAVES; ++w) { const uint32_t k = s_n[q * WAVES + w]; before += w < wave ? k : 0; all += k; }
+      if (uint64_t(y[q]) < a.s.V)
+        each(n + before + uint32_t(__popcll(mask[q] & ((uint64_t(1) << lane) - 1))), r0 + q * THREADS + threadIdx.x, uint32_t(y[q]));
+      n += all;
+    }
     __syncthreads();
   }
 #pragma unroll
@@ -180,12 +195,13 @@ typedef Cfg<128, 128, 2, 2, 512, 1910> Mid;
 typedef Cfg<128, 64, 4, 1, 256, 1700> Few;     // up to 64 rows: 256 of them read at the rate of the memory
 
 // Workgroups that share the k of a tile: as many as finish first, the sums that they leave to be added counted in; and when that is, in ns.
-struct Shares { uint32_t n, ns; };
+struct Shares { uint32_t n; uint64_t ns; };
 template <class C> __host__ __device__ inline Shares shares(uint32_t tiles, uint32_t twos) {
-  Shares best = {1, 0xffffffffu};
+  Shares best = {1, ~0ull};
   for (uint32_t n : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
     if (n > 1 && n * 2 > twos) break;
-    const uint32_t ns = (tiles * n + C::SLOTS - 1) / C::SLOTS * ((twos + n - 1) / n * C::TWO_NS + 3000) + (n > 1 ? tiles * n * C::PART_NS + 4000 : 0);
+    const uint64_t rounds = (tiles * n + C::SLOTS - 1) / C::SLOTS, parts = n > 1 ? tiles * n : 0;
+    const uint64_t ns = rounds * ((twos + n - 1) / n * C::TWO_NS + 3000) + parts * C::PART_NS + (n > 1 ? 4000 : 0);
     if (ns < best.ns) best = {n, ns};
   }
   return best;
@@ -494,6 +510,14 @@ __device__ __forceinline__ void store8(PT_GLOBAL uint16_t* row, uint32_t m, uint
       if (m + q < d) row[m + q] = uint16_t(w[q / 2] >> (16 * (q & 1)));
 }
 
+__device__ __forceinline__ void store4(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, bool wide, u32x2 w) {
+  if (wide && m + 4 <= d) *(PT_GLOBAL u32x2*)(row + m) = w;
+  else
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q)
+      if (m + q < d) row[m + q] = uint16_t(w[q / 2] >> (16 * (q & 1)));
+}
+
 struct GradArgs {
   Shape s;
   Operand p, q;
@@ -504,7 +528,8 @@ struct GradArgs {
   uint64_t stride;
   bool wide;                 // eight results may be stored at once
   uint32_t pitch;            // of the sums below
-  float* part;               // d_hidden by several workgroups a tile: [shares][rows][pitch]
+  float* part;               // sums of several workgroups a tile: [shares][rows or words][pitch]
+  uint32_t share;            // of d_weight: workgroups a tile
   const float* rest;
   const uint16_t* weight;
   uint64_t weight_stride;
@@ -606,12 +631,7 @@ __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
     const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + target * a.weight_stride;
     y = encode16x4<DT>(add_rest<DT>(x, a.rest[n], w, m, a.s.d) * a.meta->down);
   }
-  PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride;
-  if (a.wide && m + 4 <= a.s.d) *(PT_GLOBAL u32x2*)(row + m) = y;
-  else
-#pragma unroll
-    for (uint32_t q = 0; q < 4; ++q)
-      if (m + q < a.s.d) row[m + q] = uint16_t(y[q / 2] >> (16 * (q & 1)));
+  store4((PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride, m, a.s.d, a.wide, y);
 }
 
 // d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
@@ -620,18 +640,30 @@ __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even,
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   if (!n_rows && a.read_acc && a.write_acc) return;
   uint32_t tm, tn;
-  if (!tile_of(block, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
+  const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM;
+  if (!tile_of(block, tiles_m * a.share, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
+  const uint32_t part = tm / tiles_m;
+  tm -= part * tiles_m;
   Operand p = a.p, q = a.q;
   p.k = q.k = !n_rows ? 0 : a.s.low ? 2 * a.s.low : (n_rows + TWO - 1) / TWO * TWO;
+  const uint32_t twos = p.k / TWO, t0 = uint32_t(uint64_t(twos) * part / a.share), t1 = uint32_t(uint64_t(twos) * (part + 1) / a.share);
   const float down = a.meta->down;
   with_tile<DT, C, false, false>(a.s.d - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
-    t.run(even, odd, p, q, tm * C::BM, tn * C::BN, 0, p.k / TWO);
+    t.run(even, odd, p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
     const uint32_t lane = threadIdx.x & 63, mw = tm * C::BM + t.wave_m(), mb = mw + (lane >> 4) * 4;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
       const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
       const bool live = n < a.s.V;
+      if (a.share > 1) {
+        if (!live) continue;
+        PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.s.V + n) * a.pitch;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+          if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
+        continue;
+      }
       const uint32_t at = live ? n : 0;                    // lanes without a row take part in the exchange
       PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)a.out + at * a.stride;
       PT_GLOBAL float* sums = (PT_GLOBAL float*)a.acc + size_t(at) * a.pitch;          // of the pieces before, in fp32
@@ -660,6 +692,18 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) 
   d_weight_tile<DT, C>(a, (lds_char*)even, (lds_char*)odd, blockIdx.x);
 }
 
+template <int DT>
+__global__ void __launch_bounds__(256) k_head_join_weight(const GradArgs a) {
+  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256 + threadIdx.x) * 4;
+  if (m >= a.s.d) return;
+  const PT_GLOBAL float* part = (const PT_GLOBAL float*)a.part + size_t(n) * a.pitch + m;
+  const size_t next = size_t(a.s.V) * a.pitch;
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+  for (uint32_t k = 0; k < a.share; ++k) x += *(const PT_GLOBAL f32x4*)(part + k * next);
+  store4((PT_GLOBAL uint16_t*)a.out + n * a.stride, m, a.s.d, a.wide, encode16x4<DT>(x * a.meta->down));
+}
+
 // Both gradients of few rows in one launch: neither fills the chip for long.
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_few_grads(const GradArgs h, const GradArgs w, uint32_t blocks_h) {
@@ -680,14 +724,6 @@ inline bool mid_tiles(uint64_t m, uint64_t n) {
   const auto rounds = [&](uint64_t bm, uint64_t bn, uint64_t slots) { return ((m + bm - 1) / bm * ((n + bn - 1) / bn) + slots - 1) / slots; };
   return rounds(Mid::BM, Mid::BN, Mid::SLOTS) * Mid::TWO_NS < rounds(Big::BM, Big::BN, Big::SLOTS) * Big::TWO_NS;
 }
-// The same for d_weight, whose last tile of the width may be a narrower one.
-inline bool mid_weight(uint64_t d, uint64_t V) {
-  const uint64_t left = d % 256, tenths = d / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
-  const uint64_t big = (tenths * ((V + Big::BN - 1) / Big::BN) + Big::SLOTS * 10 - 1) / (Big::SLOTS * 10);
-  const uint64_t mid = ((d + Mid::BM - 1) / Mid::BM * ((V + Mid::BN - 1) / Mid::BN) + Mid::SLOTS - 1) / Mid::SLOTS;
-  return mid * Mid::TWO_NS < big * Big::TWO_NS;
-}
-
 uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
 // Where everything lies in the workspace, for pieces of `rows` rows.
@@ -695,7 +731,8 @@ struct Plan {
   Shape s;
   uint32_t parts, pitch, pieces, rows;
   bool grads, direct, as_is;               // direct: the weight is taken where it lies; as_is: so are the hidden states
-  uint32_t shared;                         // rows times workgroups a tile of d_hidden, at most
+  uint32_t hidden_shared, hidden_grid;     // most_shared of a whole piece
+  uint32_t shared;                         // rows (or words) times workgroups a tile of a gradient, at most
   uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, g, g_pitch, sums, acc, total;
 };
 
@@ -722,12 +759,21 @@ inline bool mid_hidden(const Shape& s, uint32_t rows) {
   return ns(Mid{}) < ns(Big{});
 }
 
-uint32_t shared_rows(const Shape& s, uint32_t rows) {
-  uint32_t shared, grid;
+// d_weight of `rows` rows: whether it is sooner done in tiles of Mid, whose width ends at multiples of 128 (of Big's the last tile may be a narrower one),
+// and by how many workgroups a tile; it is shared in one piece alone, which needs no sums of pieces.
+struct WeightTiles { bool mid; uint32_t share; };
+inline WeightTiles weight_tiles(const Shape& s, uint32_t rows, bool one_piece) {
+  const uint32_t left = s.d % 256, tenths = s.d / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
+  const uint32_t twos = (rows + TWO - 1) / TWO;
+  const Shares big = shares<Big>(std::max(1u, (tenths * ((s.V + Big::BN - 1) / Big::BN) + 9) / 10), one_piece ? twos : 1);
+  const Shares mid = shares<Mid>((s.d + Mid::BM - 1) / Mid::BM * ((s.V + Mid::BN - 1) / Mid::BN), one_piece ? twos : 1);
+  return mid.ns < big.ns ? WeightTiles{true, mid.n} : WeightTiles{false, big.n};
+}
+
+void shared_rows(const Shape& s, uint32_t rows, uint32_t& shared, uint32_t& grid) {
   if (rows <= FEW_ROWS) most_shared<Few>(s, rows, shared, grid);
   else if (mid_hidden(s, rows)) most_shared<Mid>(s, rows, shared, grid);
   else most_shared<Big>(s, rows, shared, grid);
-  return shared;
 }
 
 Plan make_plan(const pt_head& h, uint64_t rows) {
@@ -736,7 +782,7 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   if (h.d_weight && h.rows <= LOW_ROWS) p.s.low = uint32_t(up(h.rows, BK));
   p.grads = h.d_hidden || h.d_weight;
   p.direct = h.width % BK == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
-  p.as_is = p.direct && h.rows <= FEW_ROWS && h.hidden_stride % 8 == 0 && (uintptr_t)h.hidden % 16 == 0;
+  p.as_is = p.direct && h.rows <= FEW_ROWS && h.hidden_stride % 8 == 0 && h.hidden_stride <= (1u << 21) && (uintptr_t)h.hidden % 16 == 0;
   p.parts = std::max({parts<Few>(h.vocab), parts<Mid>(h.vocab), parts<Big>(h.vocab)});
   p.pitch = uint32_t(up(h.width, 4));
   p.rows = uint32_t(std::min<uint64_t>(rows, up(h.rows, PIECE_STEP)));
@@ -761,12 +807,28 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
     p.g_pitch = 2ull * p.s.Vp;
     p.g = take(p.g_pitch * (up(h.rows, TWO) + p.s.low));
   }
-  if (h.d_hidden)                            // of a whole piece and of the last one
-    for (uint32_t rows : {std::min(p.rows, h.rows), h.rows - (p.pieces - 1) * p.rows}) p.shared = std::max(p.shared, shared_rows(p.s, rows));
+  if (h.d_hidden) {
+    shared_rows(p.s, std::min(p.rows, h.rows), p.hidden_shared, p.hidden_grid);
+    p.shared = p.hidden_shared;
+    if (p.pieces > 1) {
+      uint32_t shared, grid;
+      shared_rows(p.s, h.rows - (p.pieces - 1) * p.rows, shared, grid);
+      p.shared = std::max(p.shared, shared);
+    }
+  }
+  if (h.d_weight && p.pieces == 1 && h.rows > FEW_ROWS) {
+    const uint32_t share = weight_tiles(p.s, h.rows, true).share;
+    if (share > 1) p.shared = std::max(p.shared, share * h.vocab);     // one after the other: the same room
+  }
   p.sums = take(4ull * p.shared * p.pitch);
   p.acc = take(h.d_weight && p.pieces > 1 ? 4ull * h.vocab * p.pitch : 0);
   p.total = at;
   return p;
+}
+
+uint64_t best_rows(const pt_head& h) {
+  const uint64_t row = up(h.vocab, 256) * (h.dtype == PT_BF16 ? KEPT_BYTES<PT_BF16> : KEPT_BYTES<PT_FP16>);
+  return std::min({std::max(PIECE_BEST, PIECE_BYTES / row / PIECE_STEP * PIECE_STEP), PIECE_MOST, up(h.rows, PIECE_STEP)});
 }
 
 int check(const pt_head* h, const char* who) {
@@ -799,24 +861,24 @@ template <int DT, class C> int join_hidden(const GradArgs& a, uint32_t shared, h
   PT_LAUNCH_CHECK(nullptr, "k_head_join");
   return PT_OK;
 }
-template <int DT, class C> int d_hidden(const GradArgs& a, hipStream_t st) {
-  uint32_t shared, grid;
-  most_shared<C>(a.s, a.rows, shared, grid);
+template <int DT, class C> int d_hidden(const GradArgs& a, uint32_t shared, uint32_t grid, hipStream_t st) {
   hipLaunchKernelGGL((k_head_d_hidden<DT, C>), dim3(grid), dim3(C::THREADS), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_d_hidden");
   return join_hidden<DT, C>(a, shared, st);
 }
-template <int DT> int few_grads(const GradArgs& h, const GradArgs& w, hipStream_t st) {
-  uint32_t shared, grid;
-  most_shared<Few>(h.s, h.rows, shared, grid);
+template <int DT> int few_grads(const GradArgs& h, const GradArgs& w, uint32_t shared, uint32_t grid, hipStream_t st) {
   hipLaunchKernelGGL(k_head_few_grads<DT>, dim3(grid + tile_grid((w.s.d + Mid::BM - 1) / Mid::BM, (w.s.V + Mid::BN - 1) / Mid::BN)), dim3(256), 0, st, h, w,
                      grid);
   PT_LAUNCH_CHECK(nullptr, "k_head_few_grads");
   return join_hidden<DT, Few>(h, shared, st);
 }
 template <int DT, class C> int d_weight(const GradArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_head_d_weight<DT, C>), dim3(tile_grid((a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN)), dim3(C::THREADS), 0, st, a);
+  hipLaunchKernelGGL((k_head_d_weight<DT, C>), dim3(tile_grid((a.s.d + C::BM - 1) / C::BM * a.share, (a.s.V + C::BN - 1) / C::BN)), dim3(C::THREADS), 0, st,
+                     a);
   PT_LAUNCH_CHECK(nullptr, "k_head_d_weight");
+  if (a.share == 1) return PT_OK;
+  hipLaunchKernelGGL(k_head_join_weight<DT>, dim3(a.s.V, (a.s.d + 1023) / 1024), dim3(256), 0, st, a);
+  PT_LAUNCH_CHECK(nullptr, "k_head_join_weight");
   return PT_OK;
 }
 
@@ -854,7 +916,8 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   for (uint32_t i = 0; i < p.pieces && rc == PT_OK; ++i) {
     const uint32_t first = i * p.rows, rows = std::min(p.rows, s.R - first);
     uint16_t* hid = packed + size_t(first) * s.Kd;
-    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows), mid_h = mid_hidden(s, rows), mid_w = mid_weight(s.d, s.V);
+    const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows);
+    const WeightTiles wt = weight_tiles(s, rows, p.pieces == 1);
     const Operand hidden = p.as_is ? Operand{h.hidden, h.hidden_stride * 2, 0, s.d} : Operand{hid, 2ull * s.Kd, 0, s.Kd};
     const LogitArgs la = {s, {weight, stride * 2, s.V, width}, hidden, meta, first, rows, target_of + first, p.as_is ? h.target : nullptr, (f32x2*)(ws + p.part),
                           few ? parts<Few>(s.V) : mid ? parts<Mid>(s.V) : parts<Big>(s.V), (float*)(ws + p.at_target),
@@ -875,7 +938,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
     const GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.g, p.g_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
                    (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 16 == 0 && h.d_hidden_stride % 8 == 0, p.pitch,
-                   (float*)(ws + p.sums), sa.rest, weight, stride, nullptr, false, false};
+                   (float*)(ws + p.sums), 1, sa.rest, weight, stride, nullptr, false, false};
     GradArgs gw = ga;
     gw.p = {hid, 2ull * s.Kd, s.Kd, 0};
     gw.q = {ws + p.g, p.g_pitch, s.Vp, 0};
@@ -885,12 +948,18 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     gw.acc = (float*)(ws + p.acc);
     gw.read_acc = i > 0;
     gw.write_acc = i + 1 < p.pieces;
+    uint32_t shared = p.hidden_shared, grid = p.hidden_grid;
+    if (h.d_hidden && rows != std::min(p.rows, s.R)) shared_rows(s, rows, shared, grid);          // a shorter last piece
     if (few && h.d_hidden && h.d_weight) {
-      rc = few_grads<DT>(ga, gw, st);
+      rc = few_grads<DT>(ga, gw, shared, grid, st);
       continue;
     }
-    if (h.d_hidden) rc = few ? d_hidden<DT, Few>(ga, st) : mid_h ? d_hidden<DT, Mid>(ga, st) : d_hidden<DT, Big>(ga, st);
-    if (h.d_weight && rc == PT_OK) rc = mid_w ? d_weight<DT, Mid>(gw, st) : d_weight<DT, Big>(gw, st);
+    if (h.d_hidden)
+      rc = few                  ? d_hidden<DT, Few>(ga, shared, grid, st)
+           : mid_hidden(s, rows) ? d_hidden<DT, Mid>(ga, shared, grid, st)
+                                 : d_hidden<DT, Big>(ga, shared, grid, st);
+    gw.share = wt.share;
+    if (h.d_weight && rc == PT_OK) rc = wt.mid ? d_weight<DT, Mid>(gw, st) : d_weight<DT, Big>(gw, st);
   }
   return rc;
 }
@@ -899,8 +968,13 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
 
 extern "C" int pt_head_workspace(const pt_head* head, uint64_t* least_bytes, uint64_t* best_bytes) {
   if (int rc = check(head, "pt_head_workspace"); rc != PT_OK) return rc;
-  if (least_bytes) *least_bytes = head->rows ? make_plan(*head, PIECE_STEP).total : 0;
-  if (best_bytes) *best_bytes = head->rows ? make_plan(*head, PIECE_BEST).total : 0;
+  if (least_bytes) {
+    // the smallest pieces as a rule, but one piece needs no sums of pieces
+    uint64_t least = head->rows ? ~0ull : 0;
+    for (uint64_t rows = PIECE_STEP; head->rows && rows <= best_rows(*head); rows += PIECE_STEP) least = std::min(least, make_plan(*head, rows).total);
+    *least_bytes = least;
+  }
+  if (best_bytes) *best_bytes = head->rows ? make_plan(*head, best_rows(*head)).total : 0;
   return PT_OK;
 }
 
@@ -917,11 +991,10 @@ extern "C" int pt_head_loss(const pt_head* head, void* workspace, uint64_t works
   if (!workspace) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_head_loss: workspace is NULL");
   if ((uintptr_t)workspace % 256 != 0) return pt_fail(nullptr, PT_ERR_ALIGNMENT, "pt_head_loss: the workspace is not 256-byte aligned");
   // the largest pieces that fit
-  uint64_t rows = PIECE_BEST;
-  while (rows > PIECE_STEP && make_plan(*head, rows).total > workspace_bytes) rows -= PIECE_STEP;
-  const Plan p = make_plan(*head, rows);
+  uint64_t rows = best_rows(*head);
+  Plan p = make_plan(*head, rows);
+  while (p.total > workspace_bytes && rows > PIECE_STEP) p = make_plan(*head, rows -= PIECE_STEP);
   if (p.total > workspace_bytes)
-    return pt_fail(nullptr, PT_ERR_NOMEM, "pt_head_loss: a workspace of %llu bytes, at least %llu are needed", (unsigned long long)workspace_bytes,
-                   (unsigned long long)p.total);
+    return pt_fail(nullptr, PT_ERR_NOMEM, "pt_head_loss: a workspace of %llu bytes is too small (pt_head_workspace)", (unsigned long long)workspace_bytes);
   return head->dtype == PT_BF16 ? run<PT_BF16>(*head, p, (char*)workspace, st) : run<PT_FP16>(*head, p, (char*)workspace, st);
 }

@@ -136,6 +136,41 @@ def test_large_tiles(rows, width, vocab, workspace, dtype):
     check(call(c, workspace=workspace), expected(c, "cuda"))
 
 
+# a small vocabulary: workgroups that share the rows of a tile of the weight's gradient, in either kind of tile, one piece of more rows than usual, widths
+# whose sums end inside four numbers
+SHARED = [(8192, 512, 1000), (3000, 203, 700), (9000, 64, 40), (20000, 130, 300), (1500, 1100, 2100), (33000, 16, 17)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,vocab", SHARED)
+def test_small_vocabularies(rows, width, vocab, dtype):
+    c = case(rows, width, vocab, dtype, ignored=0.3)
+    want = expected(c, "cuda")
+    check(call(c), want)
+    check(call(c, grads="weight"), want)
+
+
+def test_a_small_vocabulary_without_a_row():
+    c = case(3000, 128, 200, "bf16")
+    c["target"][:] = -1
+    loss, dh, dw = call(c)
+    assert not bool(loss.any()) and not bool(dh.any()) and not bool(dw.any())
+
+
+@pytest.mark.parametrize("rows", [1, 9, 40, 64])
+def test_rows_without_a_target_that_are_multiplied_all_the_same(rows):
+    """Few rows whose hidden states are taken where they lie: those without a target hold what must not reach a result."""
+    c = case(rows, 128, 500, "bf16", ignored=0.4)
+    off = c["target"] < 0
+    c["hidden"][off] = float("nan")
+    c["hidden"][off, ::2] = float("inf")
+    want = expected(c)
+    for grads in ("both", "hidden", "weight"):
+        got = call(c, grads=grads)
+        check(got, want)
+        assert not bool(got[0][off].any()) and (got[1] is None or not bool(got[1][off].any()))
+
+
 def test_logits_beyond_32_bits():
     """What is kept of a piece's logits is 4.3 GB: rows whose place passes 2^32 bytes."""
     c = case(8192, 64, 131072, "fp16")
