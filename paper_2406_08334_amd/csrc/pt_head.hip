@@ -21,6 +21,7 @@ using namespace pt_mfma;
 namespace {
 
 typedef u32x4 u32x4_a __attribute__((aligned(2)));
+typedef u32x2 u32x2_a __attribute__((aligned(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t PIECE_STEP = 256;       // pieces are multiples of this many rows
@@ -194,27 +195,60 @@ typedef Cfg<256, 256, 2, 4, 256, 2970> Big;
 typedef Cfg<128, 128, 2, 2, 512, 1910> Mid;
 typedef Cfg<128, 64, 4, 1, 256, 1700> Few;     // up to 64 rows: 256 of them read at the rate of the memory
 
-// Workgroups that share the k of a tile: as many as finish first, the sums that they leave to be added counted in; and when that is, in ns.
-struct Shares { uint32_t n; uint64_t ns; };
-template <class C> __host__ __device__ inline Shares shares(uint32_t tiles, uint32_t twos) {
-  Shares best = {1, ~0ull};
-  for (uint32_t n : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
-    if (n > 1 && n * 2 > twos) break;
-    const uint64_t rounds = (tiles * n + C::SLOTS - 1) / C::SLOTS, parts = n > 1 ? tiles * n : 0;
-    const uint64_t ns = rounds * ((twos + n - 1) / n * C::TWO_NS + 3000) + parts * C::PART_NS + (n > 1 ? 4000 : 0);
-    if (ns < best.ns) best = {n, ns};
+// How the tiles of a gradient are done: `whole` by one workgroup each, and `tail`, those of the last round, by `n` each, which share its k and leave sums to
+// be added; and when they are done, in ns.
+struct Split { uint32_t whole, tail, n; uint64_t ns; };
+template <class C> __host__ __device__ inline Split split(uint32_t tiles, uint32_t twos) {
+  const uint64_t round = uint64_t(twos) * C::TWO_NS + 3000;
+  Split best = {tiles, 0, 1, (tiles + C::SLOTS - 1) / C::SLOTS * round};
+  const uint32_t tail = tiles % C::SLOTS, whole = tiles - tail;
+  if (!tail) return best;
+  for (uint32_t n : {2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u, std::min(32u, uint32_t(C::SLOTS) / tail)}) {
+    if (n < 2 || n * 2 > twos) continue;
+    const uint64_t ns = whole / C::SLOTS * round + (tail * n + C::SLOTS - 1) / C::SLOTS * (uint64_t((twos + n - 1) / n) * C::TWO_NS + 3000) +
+                        uint64_t(tail) * n * C::PART_NS + 4000;
+    if (ns < best.ns) best = {whole, tail, n, ns};
   }
   return best;
 }
 
-// Tile `id` of tm x tn: the XCDs, which workgroups go to in turn, get tiles next to each other, in patches of a few n.
-__device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
+// Tile i of tm x tn: those next to each other lie in patches of a few n.
+__device__ __forceinline__ void tile_at(uint32_t i, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
   constexpr uint32_t GROUP = 8;
-  const uint32_t total = tm * tn, per = (total + 7) / 8, at = (id >> 3), i = (id & 7) * per + at;
-  if (at >= per || i >= total) return false;
   const uint32_t g = i / (GROUP * tm), n0 = g * GROUP, gn = min(GROUP, tn - n0), r = i - g * GROUP * tm;
   n = n0 + r % gn;
   m = r / gn;
+}
+// The XCDs, which workgroups go to in turn, get numbers next to each other: of `total` that of workgroup `id`, if there is one.
+__device__ __forceinline__ bool xcd_of(uint32_t id, uint32_t total, uint32_t& i) {
+  const uint32_t per = (total + 7) / 8;
+  i = (id & 7) * per + (id >> 3);
+  return (id >> 3) < per && i < total;
+}
+__device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
+  uint32_t i;
+  if (!xcd_of(id, tm * tn, i)) return false;
+  tile_at(i, tm, tn, m, n);
+  return true;
+}
+// Tile and part of a workgroup of a split product; sums: where its sums go, or NULL: they are all there is.
+__host__ __device__ inline uint32_t split_grid(const Split& s) { return (s.whole + 7) / 8 * 8 + (s.tail * s.n + 7) / 8 * 8; }
+template <class C>
+__device__ __forceinline__ bool part_of(const Split& s, uint32_t id, uint32_t tm, uint32_t tn, float* room, uint32_t& m, uint32_t& n, uint32_t& part,
+                                        PT_GLOBAL float*& sums) {
+  uint32_t i;
+  const uint32_t first = (s.whole + 7) / 8 * 8;
+  part = 0;
+  sums = nullptr;
+  if (id < first) {
+    if (!xcd_of(id, s.whole, i)) return false;
+  } else {
+    if (!xcd_of(id - first, s.tail * s.n, i)) return false;
+    sums = (PT_GLOBAL float*)room + size_t(i) * (C::BM * C::BN);
+    part = i / s.tail;
+    i = s.whole + i % s.tail;
+  }
+  tile_at(i, tm, tn, m, n);
   return true;
 }
 inline uint32_t tile_grid(uint64_t tm, uint64_t tn) { return uint32_t((tm * tn + 7) / 8 * 8); }
@@ -501,17 +535,17 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   }
 }
 
-// Of a row of d 16-bit numbers the eight from m on; wide: whole ones may be stored at once.
-__device__ __forceinline__ void store8(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, bool wide, u32x4 w) {
-  if (wide && m + 8 <= d) *(PT_GLOBAL u32x4*)(row + m) = w;
+// Of a row of d 16-bit numbers, at any address, the eight from m on.
+__device__ __forceinline__ void store8(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, u32x4 w) {
+  if (m + 8 <= d) *(PT_GLOBAL u32x4_a*)(row + m) = w;
   else
 #pragma unroll
     for (uint32_t q = 0; q < 8; ++q)
       if (m + q < d) row[m + q] = uint16_t(w[q / 2] >> (16 * (q & 1)));
 }
 
-__device__ __forceinline__ void store4(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, bool wide, u32x2 w) {
-  if (wide && m + 4 <= d) *(PT_GLOBAL u32x2*)(row + m) = w;
+__device__ __forceinline__ void store4(PT_GLOBAL uint16_t* row, uint32_t m, uint32_t d, u32x2 w) {
+  if (m + 4 <= d) *(PT_GLOBAL u32x2_a*)(row + m) = w;
   else
 #pragma unroll
     for (uint32_t q = 0; q < 4; ++q)
@@ -526,14 +560,13 @@ struct GradArgs {
   const uint32_t *row_of, *target_of;      // of the piece
   uint16_t* out;
   uint64_t stride;
-  bool wide;                 // eight results may be stored at once
-  uint32_t pitch;            // of the sums below
-  float* part;               // sums of several workgroups a tile: [shares][rows or words][pitch]
-  uint32_t share;            // of d_weight: workgroups a tile
+  float* part;               // sums of several workgroups a tile: [n][tail][BN][BM]
+  Split split;               // of d_weight
   const float* rest;
   const uint16_t* weight;
   uint64_t weight_stride;
   float* acc;                // d_weight over several pieces: sums so far [V][pitch]
+  uint32_t pitch;
   bool read_acc, write_acc;
 };
 
@@ -560,16 +593,25 @@ __device__ __forceinline__ void with_tile(uint32_t left, F&& f) {
   f(typename C::template Of<DT, PK, QK>{});
 }
 
+// A lane's sums of rows j of a tile, into the tile's place among those of several workgroups.
+template <class C, class T>
+__device__ __forceinline__ void leave(const T& t, int j, PT_GLOBAL float* sums) {
+  const uint32_t lane = threadIdx.x & 63;
+  PT_GLOBAL float* row = sums + (t.wave_n() + j * 16 + (lane & 15)) * C::BM + t.wave_m() + (lane >> 4) * 4;
+#pragma unroll
+  for (int i = 0; i < T::FM; ++i) *(PT_GLOBAL f32x4*)(row + i * 16) = t.acc[i][j];
+}
+
 // d_hidden of a piece: m runs over the width, n over rows, k over the vocabulary.
 template <int DT, class C>
 __device__ __forceinline__ void d_hidden_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM, tiles_n = (n_rows + C::BN - 1) / C::BN, twos = a.s.Vp / TWO;
-  const uint32_t share = shares<C>(tiles_m * tiles_n, twos).n;
-  uint32_t tm, tn;
-  if (!tile_of(block, tiles_m * share, tiles_n, tm, tn)) return;
-  const uint32_t part = tm / tiles_m, t0 = uint32_t(uint64_t(twos) * part / share), t1 = uint32_t(uint64_t(twos) * (part + 1) / share);
-  tm -= part * tiles_m;
+  const Split sp = split<C>(tiles_m * tiles_n, twos);
+  uint32_t tm, tn, part;
+  PT_GLOBAL float* sums;
+  if (!part_of<C>(sp, block, tiles_m, tiles_n, a.part, tm, tn, part, sums)) return;
+  const uint32_t t0 = sums ? uint32_t(uint64_t(twos) * part / sp.n) : 0, t1 = sums ? uint32_t(uint64_t(twos) * (part + 1) / sp.n) : twos;
   Operand q = a.q;
   q.extent = n_rows;
   const float down = a.meta->down;
@@ -581,12 +623,8 @@ __device__ __forceinline__ void d_hidden_tile(const GradArgs& a, lds_char* even,
     for (int j = 0; j < T::FN; ++j) {
       const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
       const bool live = n < n_rows;
-      if (share > 1) {
-        if (!live) continue;
-        PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.rows + n) * a.pitch;
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i)
-          if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
+      if (sums) {
+        leave<C>(t, j, sums);
         continue;
       }
       const uint32_t at = live ? n : 0;                    // lanes without a row take part in the exchange
@@ -600,7 +638,7 @@ __device__ __forceinline__ void d_hidden_tile(const GradArgs& a, lds_char* even,
         u32x4 x = eight(encode16x4<DT>(add_rest<DT>(t.acc[i][j], rest, w, m, a.s.d) * down),
                         encode16x4<DT>(add_rest<DT>(t.acc[i + 1][j], rest, w, m + 16, a.s.d) * down));
         if (y == NO_TARGET) x = u32x4{0, 0, 0, 0};         // whatever the weight holds
-        if (live) store8(row, mw + i * 16 + eight_at(), a.s.d, a.wide, x);
+        if (live) store8(row, mw + i * 16 + eight_at(), a.s.d, x);
       }
     }
   });
@@ -613,25 +651,40 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_hidden(const GradArgs a) 
   d_hidden_tile<DT, C>(a, (lds_char*)even, (lds_char*)odd, blockIdx.x);
 }
 
-// Adds up what several workgroups a tile have left: a lane four results of a row.
+// Adds up what several workgroups a tile have left, four results of a row at a time, by JOINERS workgroups at most: that many at once, and few if the rows
+// turn out to need none.  f: called with place (m, n) and sum.
+constexpr uint32_t JOINERS = 2048;
+template <class C> uint32_t joiners(uint32_t tail) { return std::min<uint32_t>(JOINERS, tail * (C::BM * C::BN / 1024)); }
+template <class C, class F>
+__device__ __forceinline__ void join_tiles(const float* room, const Split& s, uint32_t tm, uint32_t tn, F&& f) {
+  constexpr uint32_t TILE = C::BM * C::BN;
+  const size_t next = size_t(s.tail) * TILE;
+  for (uint32_t i = blockIdx.x; i < s.tail * (TILE / 1024); i += gridDim.x) {
+    const uint32_t j = i / (TILE / 1024), e = i % (TILE / 1024) * 1024 + threadIdx.x * 4;
+    uint32_t m, n;
+    tile_at(s.whole + j, tm, tn, m, n);
+    const PT_GLOBAL float* sums = (const PT_GLOBAL float*)room + size_t(j) * TILE + e;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (uint32_t k = 0; k < s.n; ++k) x += *(const PT_GLOBAL f32x4*)(sums + k * next);
+    f(m * C::BM + e % C::BM, n * C::BN + e / C::BM, x);
+  }
+}
+
 template <int DT, class C>
 __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
-  const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows), n = blockIdx.x, m = (blockIdx.y * 256 + threadIdx.x) * 4;
-  if (n >= n_rows || m >= a.s.d) return;
-  const uint32_t share = shares<C>((a.s.d + C::BM - 1) / C::BM * ((n_rows + C::BN - 1) / C::BN), a.s.Vp / TWO).n;
-  if (share == 1) return;
-  const PT_GLOBAL float* part = (const PT_GLOBAL float*)a.part + size_t(n) * a.pitch + m;
-  const size_t next = size_t(a.rows) * a.pitch;
-  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-  for (uint32_t k = 0; k < share; ++k) x += *(const PT_GLOBAL f32x4*)(part + k * next);
-  const uint32_t target = a.target_of[n];
-  u32x2 y = {0, 0};
-  if (target != NO_TARGET) {
-    const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + target * a.weight_stride;
-    y = encode16x4<DT>(add_rest<DT>(x, a.rest[n], w, m, a.s.d) * a.meta->down);
-  }
-  store4((PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride, m, a.s.d, a.wide, y);
+  const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows), tiles_m = (a.s.d + C::BM - 1) / C::BM, tiles_n = (n_rows + C::BN - 1) / C::BN;
+  const float down = a.meta->down;
+  join_tiles<C>(a.part, split<C>(tiles_m * tiles_n, a.s.Vp / TWO), tiles_m, tiles_n, [&](uint32_t m, uint32_t n, f32x4 x) {
+    if (n >= n_rows || m >= a.s.d) return;
+    const uint32_t target = a.target_of[n];
+    u32x2 y = {0, 0};
+    if (target != NO_TARGET) {
+      const PT_GLOBAL uint16_t* w = (const PT_GLOBAL uint16_t*)a.weight + target * a.weight_stride;
+      y = encode16x4<DT>(add_rest<DT>(x, a.rest[n], w, m, a.s.d) * down);
+    }
+    store4((PT_GLOBAL uint16_t*)a.out + a.row_of[n] * a.stride, m, a.s.d, y);
+  });
 }
 
 // d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
@@ -639,14 +692,12 @@ template <int DT, class C>
 __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
   if (!n_rows && a.read_acc && a.write_acc) return;
-  uint32_t tm, tn;
-  const uint32_t tiles_m = (a.s.d + C::BM - 1) / C::BM;
-  if (!tile_of(block, tiles_m * a.share, (a.s.V + C::BN - 1) / C::BN, tm, tn)) return;
-  const uint32_t part = tm / tiles_m;
-  tm -= part * tiles_m;
+  uint32_t tm, tn, part;
+  PT_GLOBAL float* left;
+  if (!part_of<C>(a.split, block, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, a.part, tm, tn, part, left)) return;
   Operand p = a.p, q = a.q;
   p.k = q.k = !n_rows ? 0 : a.s.low ? 2 * a.s.low : (n_rows + TWO - 1) / TWO * TWO;
-  const uint32_t twos = p.k / TWO, t0 = uint32_t(uint64_t(twos) * part / a.share), t1 = uint32_t(uint64_t(twos) * (part + 1) / a.share);
+  const uint32_t twos = p.k / TWO, t0 = left ? twos * part / a.split.n : 0, t1 = left ? twos * (part + 1) / a.split.n : twos;
   const float down = a.meta->down;
   with_tile<DT, C, false, false>(a.s.d - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
@@ -656,12 +707,8 @@ __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even,
     for (int j = 0; j < T::FN; ++j) {
       const uint32_t n = tn * C::BN + t.wave_n() + j * 16 + (lane & 15);
       const bool live = n < a.s.V;
-      if (a.share > 1) {
-        if (!live) continue;
-        PT_GLOBAL float* row = (PT_GLOBAL float*)a.part + (size_t(part) * a.s.V + n) * a.pitch;
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i)
-          if (mb + i * 16 < a.s.d) *(PT_GLOBAL f32x4*)(row + mb + i * 16) = t.acc[i][j];
+      if (left) {
+        leave<C>(t, j, left);
         continue;
       }
       const uint32_t at = live ? n : 0;                    // lanes without a row take part in the exchange
@@ -679,7 +726,7 @@ __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even,
           w[h] = encode16x4<DT>(x);
         }
         const u32x4 x = eight(w[0], w[1]);
-        if (live && !a.write_acc) store8(row, mw + i * 16 + eight_at(), a.s.d, a.wide, x);
+        if (live && !a.write_acc) store8(row, mw + i * 16 + eight_at(), a.s.d, x);
       }
     }
   });
@@ -692,16 +739,12 @@ __global__ void __launch_bounds__(C::THREADS) k_head_d_weight(const GradArgs a) 
   d_weight_tile<DT, C>(a, (lds_char*)even, (lds_char*)odd, blockIdx.x);
 }
 
-template <int DT>
+template <int DT, class C>
 __global__ void __launch_bounds__(256) k_head_join_weight(const GradArgs a) {
-  const uint32_t n = blockIdx.x, m = (blockIdx.y * 256 + threadIdx.x) * 4;
-  if (m >= a.s.d) return;
-  const PT_GLOBAL float* part = (const PT_GLOBAL float*)a.part + size_t(n) * a.pitch + m;
-  const size_t next = size_t(a.s.V) * a.pitch;
-  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-  for (uint32_t k = 0; k < a.share; ++k) x += *(const PT_GLOBAL f32x4*)(part + k * next);
-  store4((PT_GLOBAL uint16_t*)a.out + n * a.stride, m, a.s.d, a.wide, encode16x4<DT>(x * a.meta->down));
+  const float down = a.meta->down;
+  join_tiles<C>(a.part, a.split, (a.s.d + C::BM - 1) / C::BM, (a.s.V + C::BN - 1) / C::BN, [&](uint32_t m, uint32_t n, f32x4 x) {
+    if (n < a.s.V && m < a.s.d) store4((PT_GLOBAL uint16_t*)a.out + n * a.stride, m, a.s.d, encode16x4<DT>(x * down));
+  });
 }
 
 // Both gradients of few rows in one launch: neither fills the chip for long.
@@ -726,54 +769,60 @@ inline bool mid_tiles(uint64_t m, uint64_t n) {
 }
 uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
+// Of d_hidden of any number of rows up to `rows` that turns out to have a target: the most workgroups, tiles that several share, and bytes of their sums.
+struct Most { uint32_t grid, tail; uint64_t bytes; };
+
 // Where everything lies in the workspace, for pieces of `rows` rows.
 struct Plan {
   Shape s;
   uint32_t parts, pitch, pieces, rows;
   bool grads, direct, as_is;               // direct: the weight is taken where it lies; as_is: so are the hidden states
-  uint32_t hidden_shared, hidden_grid;     // most_shared of a whole piece
-  uint32_t shared;                         // rows (or words) times workgroups a tile of a gradient, at most
+  Most hidden;                             // of a whole piece
   uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, g, g_pitch, sums, acc, total;
 };
 
 // Partial sums of a row's exponentials.
 template <class C> uint32_t parts(uint32_t vocab) { return (vocab + C::BM - 1) / C::BM * C::WM; }
 
-// The most rows times workgroups, and the most workgroups, of d_hidden for any number of rows up to `rows` that turns out to have a target.
-template <class C> void most_shared(const Shape& s, uint32_t rows, uint32_t& shared, uint32_t& grid) {
-  shared = grid = 0;
+template <class C> Most most(const Shape& s, uint32_t rows) {
+  Most x = {0, 0, 0};
   const uint32_t tm = (s.d + C::BM - 1) / C::BM;
   for (uint32_t tn = 1; tn <= (rows + C::BN - 1) / C::BN; ++tn) {
-    const uint32_t n = shares<C>(tm * tn, s.Vp / TWO).n;
-    if (n > 1) shared = std::max(shared, n * rows);
-    grid = std::max(grid, tile_grid(uint64_t(tm) * n, tn));
+    const Split sp = split<C>(tm * tn, s.Vp / TWO);
+    x.grid = std::max(x.grid, split_grid(sp));
+    x.tail = std::max(x.tail, sp.tail);
+    x.bytes = std::max<uint64_t>(x.bytes, 4ull * sp.tail * sp.n * C::BM * C::BN);
   }
+  return x;
 }
 
 // Whether d_hidden is sooner done in tiles of Mid.
 inline bool mid_hidden(const Shape& s, uint32_t rows) {
   const auto ns = [&](auto c) {
     typedef decltype(c) C;
-    return shares<C>((s.d + C::BM - 1) / C::BM * ((rows + C::BN - 1) / C::BN), s.Vp / TWO).ns;
+    return split<C>((s.d + C::BM - 1) / C::BM * ((rows + C::BN - 1) / C::BN), s.Vp / TWO).ns;
   };
   return ns(Mid{}) < ns(Big{});
 }
 
 // d_weight of `rows` rows: whether it is sooner done in tiles of Mid, whose width ends at multiples of 128 (of Big's the last tile may be a narrower one),
-// and by how many workgroups a tile; it is shared in one piece alone, which needs no sums of pieces.
-struct WeightTiles { bool mid; uint32_t share; };
+// and how they are split; in one piece alone, which needs no sums of pieces.
+struct WeightTiles { bool mid; Split split; uint64_t bytes; };
 inline WeightTiles weight_tiles(const Shape& s, uint32_t rows, bool one_piece) {
-  const uint32_t left = s.d % 256, tenths = s.d / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
-  const uint32_t twos = (rows + TWO - 1) / TWO;
-  const Shares big = shares<Big>(std::max(1u, (tenths * ((s.V + Big::BN - 1) / Big::BN) + 9) / 10), one_piece ? twos : 1);
-  const Shares mid = shares<Mid>((s.d + Mid::BM - 1) / Mid::BM * ((s.V + Mid::BN - 1) / Mid::BN), one_piece ? twos : 1);
-  return mid.ns < big.ns ? WeightTiles{true, mid.n} : WeightTiles{false, big.n};
+  const uint32_t twos = (rows + TWO - 1) / TWO, left = s.d % 256, tenths = s.d / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
+  const auto tiles = [&](auto c) {
+    typedef decltype(c) C;
+    const uint32_t n = (s.d + C::BM - 1) / C::BM * ((s.V + C::BN - 1) / C::BN);
+    const Split sp = split<C>(n, one_piece ? twos : 1);
+    return WeightTiles{C::BM == Mid::BM, sp, 4ull * sp.tail * sp.n * C::BM * C::BN};
+  };
+  const WeightTiles big = tiles(Big{}), mid = tiles(Mid{});
+  const uint64_t big_ns = big.split.ns * tenths / ((s.d + 255) / 256 * 10);
+  return mid.split.ns < big_ns ? mid : big;
 }
 
-void shared_rows(const Shape& s, uint32_t rows, uint32_t& shared, uint32_t& grid) {
-  if (rows <= FEW_ROWS) most_shared<Few>(s, rows, shared, grid);
-  else if (mid_hidden(s, rows)) most_shared<Mid>(s, rows, shared, grid);
-  else most_shared<Big>(s, rows, shared, grid);
+Most most_hidden(const Shape& s, uint32_t rows) {
+  return rows <= FEW_ROWS ? most<Few>(s, rows) : mid_hidden(s, rows) ? most<Mid>(s, rows) : most<Big>(s, rows);
 }
 
 Plan make_plan(const pt_head& h, uint64_t rows) {
@@ -807,20 +856,14 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
     p.g_pitch = 2ull * p.s.Vp;
     p.g = take(p.g_pitch * (up(h.rows, TWO) + p.s.low));
   }
+  uint64_t sums = 0;                       // of the gradients, which come one after the other
   if (h.d_hidden) {
-    shared_rows(p.s, std::min(p.rows, h.rows), p.hidden_shared, p.hidden_grid);
-    p.shared = p.hidden_shared;
-    if (p.pieces > 1) {
-      uint32_t shared, grid;
-      shared_rows(p.s, h.rows - (p.pieces - 1) * p.rows, shared, grid);
-      p.shared = std::max(p.shared, shared);
-    }
+    p.hidden = most_hidden(p.s, std::min(p.rows, h.rows));
+    sums = p.hidden.bytes;
+    if (p.pieces > 1) sums = std::max(sums, most_hidden(p.s, h.rows - (p.pieces - 1) * p.rows).bytes);
   }
-  if (h.d_weight && p.pieces == 1 && h.rows > FEW_ROWS) {
-    const uint32_t share = weight_tiles(p.s, h.rows, true).share;
-    if (share > 1) p.shared = std::max(p.shared, share * h.vocab);     // one after the other: the same room
-  }
-  p.sums = take(4ull * p.shared * p.pitch);
+  if (h.d_weight && p.pieces == 1 && h.rows > FEW_ROWS) sums = std::max(sums, weight_tiles(p.s, h.rows, true).bytes);
+  p.sums = take(sums);
   p.acc = take(h.d_weight && p.pieces > 1 ? 4ull * h.vocab * p.pitch : 0);
   p.total = at;
   return p;
@@ -855,29 +898,27 @@ template <int DT, class C> int logits(const LogitArgs& a, hipStream_t st) {
   PT_LAUNCH_CHECK(nullptr, "k_head_logits");
   return PT_OK;
 }
-template <int DT, class C> int join_hidden(const GradArgs& a, uint32_t shared, hipStream_t st) {
-  if (!shared) return PT_OK;
-  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(a.rows, (a.s.d + 1023) / 1024), dim3(256), 0, st, a);
+template <int DT, class C> int join_hidden(const GradArgs& a, const Most& x, hipStream_t st) {
+  if (!x.tail) return PT_OK;
+  hipLaunchKernelGGL((k_head_join<DT, C>), dim3(joiners<C>(x.tail)), dim3(256), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_join");
   return PT_OK;
 }
-template <int DT, class C> int d_hidden(const GradArgs& a, uint32_t shared, uint32_t grid, hipStream_t st) {
-  hipLaunchKernelGGL((k_head_d_hidden<DT, C>), dim3(grid), dim3(C::THREADS), 0, st, a);
+template <int DT, class C> int d_hidden(const GradArgs& a, const Most& x, hipStream_t st) {
+  hipLaunchKernelGGL((k_head_d_hidden<DT, C>), dim3(x.grid), dim3(C::THREADS), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_d_hidden");
-  return join_hidden<DT, C>(a, shared, st);
+  return join_hidden<DT, C>(a, x, st);
 }
-template <int DT> int few_grads(const GradArgs& h, const GradArgs& w, uint32_t shared, uint32_t grid, hipStream_t st) {
-  hipLaunchKernelGGL(k_head_few_grads<DT>, dim3(grid + tile_grid((w.s.d + Mid::BM - 1) / Mid::BM, (w.s.V + Mid::BN - 1) / Mid::BN)), dim3(256), 0, st, h, w,
-                     grid);
+template <int DT> int few_grads(const GradArgs& h, const GradArgs& w, const Most& x, hipStream_t st) {
+  hipLaunchKernelGGL(k_head_few_grads<DT>, dim3(x.grid + split_grid(w.split)), dim3(256), 0, st, h, w, x.grid);
   PT_LAUNCH_CHECK(nullptr, "k_head_few_grads");
-  return join_hidden<DT, Few>(h, shared, st);
+  return join_hidden<DT, Few>(h, x, st);
 }
 template <int DT, class C> int d_weight(const GradArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_head_d_weight<DT, C>), dim3(tile_grid((a.s.d + C::BM - 1) / C::BM * a.share, (a.s.V + C::BN - 1) / C::BN)), dim3(C::THREADS), 0, st,
-                     a);
+  hipLaunchKernelGGL((k_head_d_weight<DT, C>), dim3(split_grid(a.split)), dim3(C::THREADS), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_d_weight");
-  if (a.share == 1) return PT_OK;
-  hipLaunchKernelGGL(k_head_join_weight<DT>, dim3(a.s.V, (a.s.d + 1023) / 1024), dim3(256), 0, st, a);
+  if (!a.split.tail) return PT_OK;
+  hipLaunchKernelGGL((k_head_join_weight<DT, C>), dim3(joiners<C>(a.split.tail)), dim3(256), 0, st, a);
   PT_LAUNCH_CHECK(nullptr, "k_head_join_weight");
   return PT_OK;
 }
@@ -917,7 +958,8 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     const uint32_t first = i * p.rows, rows = std::min(p.rows, s.R - first);
     uint16_t* hid = packed + size_t(first) * s.Kd;
     const bool few = rows <= FEW_ROWS, mid = mid_tiles(s.V, rows);
-    const WeightTiles wt = weight_tiles(s, rows, p.pieces == 1);
+    WeightTiles wt = weight_tiles(s, rows, p.pieces == 1);
+    if (few) wt = {true, {(s.d + Mid::BM - 1) / Mid::BM * ((s.V + Mid::BN - 1) / Mid::BN), 0, 1, 0}, 0};          // together with d_hidden
     const Operand hidden = p.as_is ? Operand{h.hidden, h.hidden_stride * 2, 0, s.d} : Operand{hid, 2ull * s.Kd, 0, s.Kd};
     const LogitArgs la = {s, {weight, stride * 2, s.V, width}, hidden, meta, first, rows, target_of + first, p.as_is ? h.target : nullptr, (f32x2*)(ws + p.part),
                           few ? parts<Few>(s.V) : mid ? parts<Mid>(s.V) : parts<Big>(s.V), (float*)(ws + p.at_target),
@@ -937,28 +979,22 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO)) + (p.as_is ? s.low : 0), slices), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
     const GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.g, p.g_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
-                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (uintptr_t)h.d_hidden % 16 == 0 && h.d_hidden_stride % 8 == 0, p.pitch,
-                   (float*)(ws + p.sums), 1, sa.rest, weight, stride, nullptr, false, false};
+                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (float*)(ws + p.sums), wt.split, sa.rest, weight, stride, (float*)(ws + p.acc), p.pitch,
+                   i > 0, i + 1 < p.pieces};
     GradArgs gw = ga;
     gw.p = {hid, 2ull * s.Kd, s.Kd, 0};
     gw.q = {ws + p.g, p.g_pitch, s.Vp, 0};
     gw.out = (uint16_t*)h.d_weight;
     gw.stride = h.d_weight_stride;
-    gw.wide = (uintptr_t)h.d_weight % 16 == 0 && h.d_weight_stride % 8 == 0;
-    gw.acc = (float*)(ws + p.acc);
-    gw.read_acc = i > 0;
-    gw.write_acc = i + 1 < p.pieces;
-    uint32_t shared = p.hidden_shared, grid = p.hidden_grid;
-    if (h.d_hidden && rows != std::min(p.rows, s.R)) shared_rows(s, rows, shared, grid);          // a shorter last piece
+    const Most most = h.d_hidden && rows != std::min(p.rows, s.R) ? most_hidden(s, rows) : p.hidden;          // a shorter last piece
     if (few && h.d_hidden && h.d_weight) {
-      rc = few_grads<DT>(ga, gw, shared, grid, st);
+      rc = few_grads<DT>(ga, gw, most, st);
       continue;
     }
     if (h.d_hidden)
-      rc = few                  ? d_hidden<DT, Few>(ga, shared, grid, st)
-           : mid_hidden(s, rows) ? d_hidden<DT, Mid>(ga, shared, grid, st)
-                                 : d_hidden<DT, Big>(ga, shared, grid, st);
-    gw.share = wt.share;
+      rc = few                  ? d_hidden<DT, Few>(ga, most, st)
+           : mid_hidden(s, rows) ? d_hidden<DT, Mid>(ga, most, st)
+                                 : d_hidden<DT, Big>(ga, most, st);
     if (h.d_weight && rc == PT_OK) rc = wt.mid ? d_weight<DT, Mid>(gw, st) : d_weight<DT, Big>(gw, st);
   }
   return rc;
@@ -984,7 +1020,7 @@ extern "C" int pt_head_loss(const pt_head* head, void* workspace, uint64_t works
   if (!head->rows) {
     if (!head->d_weight) return PT_OK;
     hipLaunchKernelGGL(k_head_zero, dim3(head->vocab), dim3(256), 0, st, (uint16_t*)head->d_weight, head->d_weight_stride,
-                       Shape{0, head->vocab, head->width, 0, 0});
+                       Shape{0, head->vocab, head->width, 0, 0, 0});
     PT_LAUNCH_CHECK(nullptr, "k_head_zero");
     return PT_OK;
   }
