@@ -887,8 +887,8 @@ int check(const pt_head* h, const char* who) {
       ((uintptr_t)h->row_scale | (uintptr_t)h->loss) % 4 != 0 || (uintptr_t)h->target % 8 != 0)
     return pt_fail(nullptr, PT_ERR_ALIGNMENT, "%s: an array is not aligned to its elements", who);
   // a step's loads reach 256 rows or 64 from a 64-bit address on by 32-bit offsets
-  if (h->rows > (1u << 30) || h->vocab > (1u << 21) || h->width > (1u << 20) || h->weight_stride > (1u << 21))
-    return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: more than 2^30 rows, 2^21 words, a width over 2^20 or a weight stride over 2^21", who);
+  if (h->rows > (1u << 25) || h->vocab > (1u << 21) || h->width > (1u << 20) || h->weight_stride > (1u << 21))
+    return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: more than 2^25 rows, 2^21 words, a width over 2^20 or a weight stride over 2^21", who);
   return PT_OK;
 }
 

@@ -409,6 +409,9 @@ struct Block {
   }
 };
 
+// Blocks along x of a launch at most: its threads along x have to be less than 2^32.  More lie in rows of one length: workgroups without a block cost too.
+constexpr uint32_t LAUNCH = 1u << 22;
+
 // A wave a block, in the order of the list: as for the chunks, few bytes in flight that lie next to each other are moved fastest
 // (unused LDS keeps 11 waves on a compute unit).  With states in 8 bits a wave has little more than half the bytes and the arithmetic counts:
 // as many waves as there is room for.
@@ -416,11 +419,13 @@ template <int DT, int BITS>
 __global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
   const PT_SCALAR ListState* st = (const PT_SCALAR ListState*)a.st;
   Block<DT, BITS> x;
-  x.load(a, blockIdx.x);                       // a skipped step reads in vain
+  const uint32_t b = blockIdx.y * gridDim.x + blockIdx.x;
+  if (b >= a.blocks.n) return;
+  x.load(a, b);                                // a skipped step reads in vain
   asm volatile("" ::: "memory");
   double clip;
   const Consts k = list_consts(a, clip);
-  if (blockIdx.x == 0 && threadIdx.x == 0) {   // what no other workgroup reads
+  if (b == 0 && threadIdx.x == 0) {            // what no other workgroup reads
     a.st->applied = 1;
     a.st->s.clip_coef = clip;
     const float c[9] = {k.b1, k.b2, k.omb1, k.omb2, k.decay, k.step_size, k.rsb2, k.eps, k.gm};
@@ -428,13 +433,11 @@ __global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
     for (int j = 0; j < 9; ++j) a.st->s.c[j] = c[j];
   }
   if (st->s.skip) return;
-  x.finish(k, st->key + PHI * (uint64_t(blockIdx.x) * (BLOCK / 2) + 2 * threadIdx.x + 1));
+  x.finish(k, st->key + PHI * (uint64_t(b) * (BLOCK / 2) + 2 * threadIdx.x + 1));
 }
 
 // The update of a list without an element: its step has happened.
 __global__ void k_list_applied(ListState* st) { st->applied = 1; st->s.clip_coef = 1.0; }
-
-constexpr uint32_t UPDATE_LDS8 = 0, UPDATE_LDS32 = PT_ADAMW_LDS;
 
 // Tables of an Index over `counts` pieces of every tensor.
 void build_index(const std::vector<uint64_t>& counts, std::vector<uint32_t>& first, std::vector<uint32_t>& coarse) {
@@ -451,7 +454,7 @@ void build_index(const std::vector<uint64_t>& counts, std::vector<uint32_t>& fir
 }  // namespace
 
 struct pt_tensors {
-  int device = 0, dtype = PT_BF16, bits = 32;
+  int dtype = PT_BF16, bits = 32;
   bool scaler = false;
   uint64_t seed = 0;
   Index units{}, blocks{};
@@ -520,7 +523,6 @@ int create(pt_tensors* l, const pt_tensor* list, uint32_t n, const pt_scaler_cfg
   std::memcpy(host.data() + o_bc, bc.data(), bc.size() * 4);
   std::memcpy(host.data() + o_uf, uf.data(), uf.size() * 4);
   std::memcpy(host.data() + o_uc, uc.data(), uc.size() * 4);
-  PT_HIP(nullptr, hipGetDevice(&l->device));
   PT_HIP(nullptr, hipMalloc((void**)&l->mem, total));
   PT_HIP(nullptr, hipMemcpy(l->mem, host.data(), total, hipMemcpyHostToDevice));
   l->st = (ListState*)l->mem;
@@ -611,7 +613,8 @@ extern "C" int pt_tensors_adamw_step(pt_tensors* l, const pt_hparams* hp, void* 
                          float(1.0 - hp->lr * hp->weight_decay), 0.0f, 0.0f, float(hp->eps)}};
   const auto kernel = l->dtype == PT_BF16 ? (l->bits == 8 ? k_list_adamw<PT_BF16, 8> : k_list_adamw<PT_BF16, 32>)
                                           : (l->bits == 8 ? k_list_adamw<PT_FP16, 8> : k_list_adamw<PT_FP16, 32>);
-  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3(l->blocks.n), dim3(64), l->bits == 8 ? UPDATE_LDS8 : UPDATE_LDS32, (hipStream_t)stream, a);
+  const uint32_t rows = (l->blocks.n + LAUNCH - 1) / LAUNCH;
+  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3((l->blocks.n + rows - 1) / rows, rows), dim3(64), l->bits == 8 ? 0 : PT_ADAMW_LDS, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(k_list_applied, dim3(1), dim3(1), 0, (hipStream_t)stream, l->st);
   PT_LAUNCH_CHECK(nullptr, "k_list_adamw");
   l->open = false;
