@@ -94,7 +94,9 @@ struct NormArgs {
 };
 
 // Sum of squares of every gradient in a fixed order: waves take units in turn, the last workgroup to finish adds the workgroups' sums up in
-// order, ends the step before and opens this one.
+// order, ends the step before and opens this one.  Reading bounds it (667e6 fp16 gradients: 205 us, 6.5 TB/s), of short lists the round trips of the hand-over
+// (0.8e6: 6.7 us).  Two workgroups a compute unit: with one, or four, a step of 667e6 takes 3.12 - 3.25 or 3.07 - 3.20 ms instead of 3.05, of 67e6 334 or 333 us
+// instead of 326; that many sums are also all the last one adds up.
 template <int DT>
 __global__ void __launch_bounds__(NORM_THREADS) k_list_norm(const NormArgs a) {
   const uint32_t lane = threadIdx.x & 63;
@@ -412,9 +414,12 @@ struct Block {
 // Blocks along x of a launch at most: its threads along x have to be less than 2^32.  More lie in rows of one length: workgroups without a block cost too.
 constexpr uint32_t LAUNCH = 1u << 22;
 
-// A wave a block, in the order of the list: as for the chunks, few bytes in flight that lie next to each other are moved fastest
-// (unused LDS keeps 11 waves on a compute unit).  With states in 8 bits a wave has little more than half the bytes and the arithmetic counts:
-// as many waves as there is room for.
+// A wave a block, in the order of the list.  The bytes of memory bound it.  States in 32 bits: as for the chunks, few bytes in flight that lie next to each
+// other are moved fastest, so unused LDS keeps a compute unit to 11 waves (2.46e8 parameters 1183 -> 1156 us, 6.3e6 42.2 -> 41.0) but for a short list, most
+// of which is under way at once (0.8e6 13.6 -> 12.5 us without, 3.1e6 25.5 -> 24.8).  States in 8 bits have little more than half the bytes to an update and
+// their own arithmetic: as many waves as there is room for (1.56e9: 4.47 ms; kept to 11 waves 7.0).  Rates: 667e6 fp16, 32 bits: 2.86 - 2.98 ms, 6.3 - 6.5 TB/s; 1.56e9
+// bf16, 8 bits: 4.0 ms, 6.2 TB/s.
+constexpr uint32_t SHORT = 16384;
 template <int DT, int BITS>
 __global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
   const PT_SCALAR ListState* st = (const PT_SCALAR ListState*)a.st;
@@ -614,7 +619,7 @@ extern "C" int pt_tensors_adamw_step(pt_tensors* l, const pt_hparams* hp, void* 
   const auto kernel = l->dtype == PT_BF16 ? (l->bits == 8 ? k_list_adamw<PT_BF16, 8> : k_list_adamw<PT_BF16, 32>)
                                           : (l->bits == 8 ? k_list_adamw<PT_FP16, 8> : k_list_adamw<PT_FP16, 32>);
   const uint32_t rows = (l->blocks.n + LAUNCH - 1) / LAUNCH;
-  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3((l->blocks.n + rows - 1) / rows, rows), dim3(64), l->bits == 8 ? 0 : PT_ADAMW_LDS, (hipStream_t)stream, a);
+  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3((l->blocks.n + rows - 1) / rows, rows), dim3(64), l->bits == 8 || l->blocks.n <= SHORT ? 0 : PT_ADAMW_LDS, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(k_list_applied, dim3(1), dim3(1), 0, (hipStream_t)stream, l->st);
   PT_LAUNCH_CHECK(nullptr, "k_list_adamw");
   l->open = false;
