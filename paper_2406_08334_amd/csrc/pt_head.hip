@@ -10,6 +10,9 @@
 // Three products of 2 rows vocab width operations each are what it costs.  Gradients want lse of a whole row before the first of them: pieces of the
 // vocabulary would take the first product twice, so the pieces are rows, of which as many are taken at a time as the workspace has room for.
 // The loss alone never stores a logit.
+//
+// 8192 rows, width 1600, vocabulary 50257, bf16: 3.8 ms, of which the products 3.45 (1.2, 1.15, 1.05; 3.95 TFLOP: 1150 TFLOP/s, where a large library
+// product reaches 1270 at this width) and soft 0.34; 6144 of 8192 rows, width 4096, vocabulary 32000: 3.95 ms, 1220 TFLOP/s.
 #include "pt_common.h"
 #include "pt_mfma.h"
 #include "pt_update.h"
@@ -25,12 +28,14 @@ typedef u32x2 u32x2_a __attribute__((aligned(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t PIECE_STEP = 256;       // pieces are multiples of this many rows
-// Of a piece at best: this many rows, or, of a small vocabulary, as many as keep this many bytes of logits.
+// Of a piece at best: this many rows, or, of a small vocabulary, as many as keep this many bytes of logits (16384 x 256 x 600 in one piece of 16384 rows
+// instead of two: d_weight, which then needs no sums of pieces, and may be shared, 2 x 86 -> 17 + 5 us).
 constexpr uint64_t PIECE_BEST = 8192, PIECE_BYTES = 1ull << 30, PIECE_MOST = 32768;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // What is kept of the logits of a piece.  bf16 inputs: exp(z - the largest of the wave's part of the row) as an fp16 number, 2^15 being 1: a rounding of 2^-12
-// ahead of G's own of 2^-9.  fp16 inputs, whose G is rounded by 2^-12 itself: z in fp32.
+// ahead of G's own of 2^-9.  fp16 inputs, whose G is rounded by 2^-12 itself: z in fp32 (exponentials in fp16 would save a tenth of the time at most, but
+// make the gradients' error half as large again).
 template <int DT> constexpr bool KEEP_EXP = DT == PT_BF16;
 template <int DT> constexpr uint32_t KEPT_BYTES = KEEP_EXP<DT> ? 2 : 4;
 constexpr float ONE_EXP = 15.0f;
@@ -113,7 +118,7 @@ __device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& eac
   found = found_rows(n, big);
 }
 
-// One workgroup lists the rows of a call.
+// One workgroup lists the rows of a call, in order: no count of another has to be waited for.  Bound by the round trips of its turns: 8192 rows in 10 us.
 __global__ void __launch_bounds__(1024) k_head_rows(const RowArgs a) {
   Meta m;
   list_rows<1024>(a, m, [&](uint32_t at, uint32_t r, uint32_t y) { a.row_of[at] = r; a.target_of[at] = y; });
@@ -135,7 +140,8 @@ __device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOB
 }
 
 // A wave a row: the hidden states of the rows with a target, zero rows up to a whole step behind them, and nothing for those without one.
-// LIST: every workgroup lists the rows by itself, of which there are LISTED at most: a launch less, 4 us.
+// LIST: every workgroup lists the rows by itself, of which there are LISTED at most: a launch less (1000 x 1024 x 8000 105 -> 101 us).
+// Bound by memory: 8192 rows of 4096 in 22 us, 5.2 TB/s.
 constexpr uint32_t LISTED = 1024;
 template <bool LIST>
 __global__ void __launch_bounds__(256) k_head_gather(const RowArgs a, const uint16_t* __restrict__ hidden, uint64_t stride, uint16_t* __restrict__ packed,
@@ -172,7 +178,8 @@ __global__ void __launch_bounds__(256) k_head_gather(const RowArgs a, const uint
   }
 }
 
-// A weight whose rows do not all begin at multiples of 16 bytes.
+// A weight whose rows do not all begin at multiples of 16 bytes, or end inside a step: the products load 16 bytes a lane past registers, which want that.
+// Bound by memory: 50257 rows of 771 in 34 us, 4.9 TB/s.
 __global__ void __launch_bounds__(256) k_head_weight(const uint16_t* __restrict__ weight, uint64_t stride, Shape s, uint16_t* __restrict__ padded) {
   const uint32_t v = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (v < s.V)
@@ -187,16 +194,20 @@ __global__ void __launch_bounds__(256) k_head_zero(uint16_t* __restrict__ d_weig
 
 // Tiles of the products and how their waves lie in them.  `SLOTS` of them run at a time, TWO_NS is what two steps of them take then (measured), and
 // PART_NS what a tile of partial sums costs that is written and read once more.
+//   Big   the fewest reads of LDS a product: 1440 TFLOP/s while all 256 run.  4096 x 1600 x 32000: 1.24 ms; in Mid alone 1.57
+//   Mid   where that few tiles of Big would leave the chip idle.  300 x 1024 x 2000: 55 us; in Big alone 78.  8192 x 512 x 1000: 95; 121
+//   Few   up to FEW_ROWS rows, which take as long as the weight takes to read.  64 x 1600 x 50257: 137 us; in Mid alone 156; 64 x 4096 x 32000, the loss: 53; 67
+// Which is taken is a matter of what each would need by these figures (mid_tiles, mid_hidden, weight_tiles).
 template <int BM_, int BN_, int WM_, int WN_, int SLOTS_, int TWO_NS_> struct Cfg {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, THREADS = 64 * WM_ * WN_, SLOTS = SLOTS_, TWO_NS = TWO_NS_, PART_NS = BM_ * BN_ / 625;
   template <int DT, bool PK, bool QK> using Of = Tile<DT, PK, QK, BM_, BN_, WM_, WN_>;
 };
 typedef Cfg<256, 256, 2, 4, 256, 2970> Big;
 typedef Cfg<128, 128, 2, 2, 512, 1910> Mid;
-typedef Cfg<128, 64, 4, 1, 256, 1700> Few;     // up to 64 rows: 256 of them read at the rate of the memory
+typedef Cfg<128, 64, 4, 1, 256, 1700> Few;
 
 // How the tiles of a gradient are done: `whole` by one workgroup each, and `tail`, those of the last round, by `n` each, which share its k and leave sums to
-// be added; and when they are done, in ns.
+// be added; and when they are done, in ns.  (512 x 4096 x 32000: 690 us without, 450 with; 1000 x 768 x 5000: 112, 76.)
 struct Split { uint32_t whole, tail, n; uint64_t ns; };
 template <class C> __host__ __device__ inline Split split(uint32_t tiles, uint32_t twos) {
   const uint64_t round = uint64_t(twos) * C::TWO_NS + 3000;
@@ -272,6 +283,9 @@ struct LogitArgs {
   void* z;                   // [rows][Vp], or NULL: what is kept of the logits
 };
 
+// z of a tile and what becomes of it (above).  m runs over the vocabulary, so that a lane has four z of a row next to each other, n over the rows.
+// Products bound it: 8192 x 1600 x 50257 1.2 ms, 1100 TFLOP/s, what is kept being written (0.8 GB) while other workgroups multiply; the loss alone of
+// 4096 x 4096 x 32000 0.79 ms, 1360 TFLOP/s.  Of few rows reading the weight: one of 1600 x 50257 26 us, 6.2 TB/s.
 template <int DT, class C>
 __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
   typedef typename C::template Of<DT, true, true> T;
@@ -396,7 +410,7 @@ __device__ __forceinline__ f32x2 join_row(const f32x2* part, uint32_t parts) {
   return join(join(s_x[0], s_x[1]), join(s_x[2], s_x[3]));
 }
 
-// The loss alone: a workgroup a row.
+// The loss alone: a workgroup a row.  4096 rows, 250 parts each: 9 us.
 __global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
   const uint32_t r = blockIdx.x;
   if (r >= (a.target ? a.rows : piece_rows(a.meta, a.first, a.rows))) return;
@@ -421,7 +435,7 @@ __device__ __forceinline__ u32x4 pack8_rest(const float (&x)[8], const u32x4& q)
 }
 
 // Loss and G of a row by a workgroup, G where what is kept of the row's logits lies.  Of few rows G has a place of its own, and several workgroups
-// (gridDim.y) share a row.
+// (gridDim.y) share a row.  Bound by memory: 6144 x 32000 bf16 in 132 us, 6.0 TB/s; 8192 x 50257 bf16 338 us, 4.9; 8192 x 32000 fp16 348, 4.5.
 // Of z in fp32, which are twice as long, a round takes 2048: a lane has its own of the next round under way while it stores those of this one,
 // and stores when every lane has this round's.
 // Rows as they are (few; SoftArgs::target): every one has its place, those without a target a G of zero, and the workgroups behind those of G do what
@@ -583,7 +597,7 @@ __device__ __forceinline__ f32x4 add_rest(f32x4 x, float rest, const PT_GLOBAL u
 }
 
 // Tiles of the gradients at the end of the width: of Big's, 256 wide, what is left of the width is often a small part (width 1600: 64 of it), and takes a
-// narrower tile.  f: called with the tile.
+// narrower tile (4096 x 1600 x 32000: 1258 us without, 1238 with).  f: called with the tile.
 template <int DT, class C, bool PK, bool QK, class F>
 __device__ __forceinline__ void with_tile(uint32_t left, F&& f) {
   if constexpr (C::BM == 256) {
@@ -602,7 +616,9 @@ __device__ __forceinline__ void leave(const T& t, int j, PT_GLOBAL float* sums) 
   for (int i = 0; i < T::FM; ++i) *(PT_GLOBAL f32x4*)(row + i * 16) = t.acc[i][j];
 }
 
-// d_hidden of a piece: m runs over the width, n over rows, k over the vocabulary.
+// d_hidden of a piece: m runs over the width, n over rows, k over the vocabulary.  Products bound it: 6144 x 4096 x 32000 1.23 ms, 1310 TFLOP/s;
+// 8192 x 1600 x 50257 1.15 ms, 1150: 224 tiles, a round that leaves 32 compute units idle (by eight workgroups each they would be 1792, seven rounds of an
+// eighth, but their sums cost more than the idle units).
 template <int DT, class C>
 __device__ __forceinline__ void d_hidden_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
@@ -687,7 +703,8 @@ __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
   });
 }
 
-// d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.
+// d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.  Products bound it: 6144 x 4096 x 32000 1.21 ms, 1330 TFLOP/s;
+// 8192 x 1600 x 50257 1.05 ms, 1250.
 template <int DT, class C>
 __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
@@ -747,7 +764,8 @@ __global__ void __launch_bounds__(256) k_head_join_weight(const GradArgs a) {
   });
 }
 
-// Both gradients of few rows in one launch: neither fills the chip for long.
+// Both gradients of few rows in one launch: neither fills the chip for long.  Bound by memory, which the weight is read from and its gradient written to:
+// 64 x 1600 x 50257 in 87 us, 3.7 TB/s (d_weight in tiles of 128 x 64 89, of 64 x 128 91, of 64 x 64 114).
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_few_grads(const GradArgs h, const GradArgs w, uint32_t blocks_h) {
   static_assert(Few::THREADS == 256 && Mid::THREADS == 256, "one launch");
@@ -759,7 +777,8 @@ __global__ void __launch_bounds__(256) k_head_few_grads(const GradArgs h, const 
 
 // ---- host -----------------------------------------------------------------------------------------------
 
-// Up to this many rows the gradient of the weight is a matter of writing it: what rounding G has left is multiplied as well, as rows of its own.
+// Up to LOW_ROWS rows the gradient of the weight is a matter of writing it: what rounding G has left is multiplied as well, as rows of its own.  It is of few
+// rows that a result has few terms whose roundings could cancel.  (100 x 1600 x 50257: 168 us without, 180 with; 256 x 4096 x 32000: 330, 379.)
 constexpr uint32_t LOW_ROWS = 128, FEW_ROWS = 64;
 
 // Whether a product of m x n is sooner done in tiles of Mid.

@@ -414,11 +414,11 @@ struct Block {
 // Blocks along x of a launch at most: its threads along x have to be less than 2^32.  More lie in rows of one length: workgroups without a block cost too.
 constexpr uint32_t LAUNCH = 1u << 22;
 
-// A wave a block, in the order of the list.  The bytes of memory bound it.  States in 32 bits: as for the chunks, few bytes in flight that lie next to each
-// other are moved fastest, so unused LDS keeps a compute unit to 11 waves (2.46e8 parameters 1183 -> 1156 us, 6.3e6 42.2 -> 41.0) but for a short list, most
-// of which is under way at once (0.8e6 13.6 -> 12.5 us without, 3.1e6 25.5 -> 24.8).  States in 8 bits have little more than half the bytes to an update and
-// their own arithmetic: as many waves as there is room for (1.56e9: 4.47 ms; kept to 11 waves 7.0).  Rates: 667e6 fp16, 32 bits: 2.86 - 2.98 ms, 6.3 - 6.5 TB/s; 1.56e9
-// bf16, 8 bits: 4.0 ms, 6.2 TB/s.
+// A wave a block, in the order of the list.  The bytes of memory bound it: 667e6 parameters, fp16, states in 32 bits 2.86 - 2.98 ms, 6.3 - 6.5 TB/s; 1.56e9,
+// bf16, states in 8 bits 4.0 ms, 6.2 TB/s.  States in 32 bits: as for the chunks, few bytes in flight that lie next to each other are moved fastest, so
+// unused LDS keeps a compute unit to 11 waves (2.46e8 parameters 1183 -> 1156 us, 6.3e6 42.2 -> 41.0) but for a short list, most of which is under way
+// at once (without: 0.8e6 13.6 -> 12.5 us, 3.1e6 25.5 -> 24.8).  States in 8 bits have little more than half the bytes to an update and their own
+// arithmetic: as many waves as there is room for (1.56e9, step with its norm: 4.47 ms; kept to 11 waves 7.0).
 constexpr uint32_t SHORT = 16384;
 template <int DT, int BITS>
 __global__ void __launch_bounds__(64) k_list_adamw(const UpdateArgs a) {
@@ -619,7 +619,8 @@ extern "C" int pt_tensors_adamw_step(pt_tensors* l, const pt_hparams* hp, void* 
   const auto kernel = l->dtype == PT_BF16 ? (l->bits == 8 ? k_list_adamw<PT_BF16, 8> : k_list_adamw<PT_BF16, 32>)
                                           : (l->bits == 8 ? k_list_adamw<PT_FP16, 8> : k_list_adamw<PT_FP16, 32>);
   const uint32_t rows = (l->blocks.n + LAUNCH - 1) / LAUNCH;
-  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3((l->blocks.n + rows - 1) / rows, rows), dim3(64), l->bits == 8 || l->blocks.n <= SHORT ? 0 : PT_ADAMW_LDS, (hipStream_t)stream, a);
+  const uint32_t lds = l->bits == 8 || l->blocks.n <= SHORT ? 0 : PT_ADAMW_LDS;
+  if (l->blocks.n) hipLaunchKernelGGL(kernel, dim3((l->blocks.n + rows - 1) / rows, rows), dim3(64), lds, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(k_list_applied, dim3(1), dim3(1), 0, (hipStream_t)stream, l->st);
   PT_LAUNCH_CHECK(nullptr, "k_list_adamw");
   l->open = false;
