@@ -456,8 +456,9 @@ typedef struct {
 /* Describes n_tensors tensors to the device.  state_bits 32: m and v as in chunks, results bit-identical to theirs.
  * state_bits 8: m and sqrt(v) in blocks of 256 consecutive elements of a tensor, OCP e4m3 codes times the block's largest
  * magnitude / 448 (blocks whose largest is below 2^-100 become zero); all zero bytes and scales are m = v = 0.  The update computes
- * in fp32 (each product rounded before it is added) and rounds the states up or down at random with the odds that keep their mean (rounding to nearest would
- * hold an average in place that moves by less than half a code a step); a variance that is not zero keeps one code at least.
+ * in fp32 (each product rounded before it is added) and rounds the states up or down at random with the odds that keep their mean
+ * (rounding to nearest would hold an average in place that moves by less than half a code a step); a variance that is not zero keeps
+ * one code at least.
  * The random numbers are a function of `seed`, the step counter and the element's place in the list: the same calls give the same
  * bits.  scaler as for pt_ctx_create.  Allocates and synchronises; not a hot call.
  * At most 2^31 blocks of 256 elements (each tensor's last one counted whole). */
@@ -485,8 +486,10 @@ int pt_tensors_report_read(pt_tensors* list, pt_step_report* out, void* stream);
  *     z_rv = sum_k h_rk W_vk      loss_r = log sum_v exp(z_rv) - z_r,y_r
  *     G_rv = s_r (exp(z_rv) / sum_u exp(z_ru) - [v = y_r])      d_hidden = G W      d_weight = G^T h
  * A row whose target lies outside [0, vocab) is ignored: its loss and its row of d_hidden are 0, it adds nothing to d_weight,
- * and nothing of its hidden state is looked at.  16-bit inputs, fp32 sums of their exact products; G is rounded to the 16-bit
- * type once, between the two products it takes part in, and so are the results.
+ * and whatever its hidden state holds (inf and NaN too) reaches no result.  16-bit inputs, fp32 sums of their exact products; G is
+ * rounded to the 16-bit type between the two products it takes part in (of bf16 inputs its exponentials to fp16 before; what the
+ * rounding has left at the target goes into d_hidden, and of up to 128 rows all that it has left into d_weight), and so are the results.
+ * No array that is written may overlap another one.
  * d_hidden and d_weight may each be NULL: then that gradient is not taken; with both NULL only the loss is, and nothing of the
  * size of the logits is written at all. */
 typedef struct {
@@ -502,15 +505,17 @@ typedef struct {
   int32_t dtype;           /* pt_dtype                                                             */
 } pt_head;
 
-/* Bytes of workspace that pt_head_loss needs at least, and that it is fastest with (0 for an argument that is NULL is not
- * written).  With gradients the rows are taken in pieces: fewer bytes, more pieces, each of which reads and writes the sums of
- * d_weight once.  Host only. */
+/* Bytes of workspace that pt_head_loss needs at least, and those that it is fastest with; either pointer may be NULL.  With gradients
+ * the rows are taken in pieces, at best of 8192 rows or 1 GiB of logits, whichever is more: fewer bytes, smaller pieces, each of which
+ * reads and writes the sums of d_weight once.  Host only.  PT_ERR_UNSUPPORTED: more than 2^25 rows, 2^21 words, a width over 2^20 or a
+ * weight stride over 2^21. */
 int pt_head_workspace(const pt_head* head, uint64_t* least_bytes, uint64_t* best_bytes);
 
 /* Enqueues the whole computation on `stream`; allocates nothing, does not synchronise, may be captured into a graph.
  * workspace: device, 256-byte aligned, of workspace_bytes >= least_bytes (else PT_ERR_NOMEM); its contents are of no use afterwards.
- * Widths, strides and addresses that are multiples of 8 elements take the weight where it lies; others are copied into the
- * workspace first.  rows == 0 does nothing but clear d_weight.  Errors: text in pt_last_error(NULL). */
+ * A weight whose width is a multiple of 64, stride a multiple of 8 elements and address one of 16 bytes is taken where it lies; any
+ * other is copied into the workspace first.  rows == 0 does nothing but clear d_weight.  The same call gives the same bits again.
+ * Errors: text in pt_last_error(NULL). */
 int pt_head_loss(const pt_head* head, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* ---- OPTIM-phase cost model (host only) -------------------------------------------------

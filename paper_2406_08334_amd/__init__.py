@@ -5,6 +5,7 @@ Sub-modules:
   build    - hipcc build of the library for gfx950
   shapes   - tensor-size tables of the synthetic model states (integers only)
   synth    - seeded, counter-based input generators (no arithmetic of the method)
+  train_head - example: embedding and head of a bigram model trained with pt_head_loss and a list of tensors
 
 Nothing is loaded at import time; `binding` raises if the HIP library is missing.
 """
