@@ -322,7 +322,8 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
       for (int q = 0; q < 4; ++q) big = fmaxf(big, t.acc[i][j][q]);
     big = fmaxf(big, __shfl_xor(big, 16, 64));
     big = fmaxf(big, __shfl_xor(big, 32, 64));
-    const float top = (big == -__builtin_inff() ? 0.0f : big * LOG2E) - ONE_EXP;          // of nothing but -inf the sum is 0
+    // The difference first: the largest adds 1 exactly, so no sum is below 1 and no loss below 0.  Of nothing but -inf the sum is 0.
+    const float top = big == -__builtin_inff() ? 0.0f : big;
     float sum = 0.0f;
     if (KEEP_EXP<DT> && a.z) {
       typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
           f32x4 e;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            e[q] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i + h][j][q], LOG2E, -top));
+            e[q] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i + h][j][q] - top, LOG2E, ONE_EXP));
             sum += e[q];
           }
           w[h] = __builtin_bit_cast(u32x2, __builtin_convertvector(e, f16x4));
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(C::THREADS) k_head_logits(const LogitArgs a) {
       for (int i = 0; i < T::FM; ++i) {
         if (a.z && live) *(PT_GLOBAL f32x4*)((PT_GLOBAL float*)a.z + size_t(n) * a.s.Vp + mb + i * 16) = t.acc[i][j];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][q], LOG2E, -top));
+        for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][q] - top, LOG2E, ONE_EXP));
       }
     }
     sum *= 0x1p-15f;
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
   const uint32_t row = a.target ? r : a.row_of[r];
   const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * up;
-  const float off = lse * LOG2E, gy = s * expm1f(zy - lse);
+  const float gy = s * expm1f(zy - lse);
   if (tid == 0 && blockIdx.y == 0) {
     a.loss[row] = lse - zy;
     a.rest[r] = gy - decode16<DT>(encode16<DT>(gy));
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
 #pragma unroll 4
     for (uint32_t c = first; c < a.s.Vp; c += turn) {
       const f16x8 e = __builtin_bit_cast(f16x8, *(const PT_GLOBAL u32x4*)((const PT_GLOBAL uint16_t*)a.z + size_t(r) * a.s.Vp + c));
-      const float f = s * __builtin_amdgcn_exp2f(__builtin_fmaf(part[min(c / a.part_width, a.parts - 1)][0], LOG2E, -off - ONE_EXP));
+      const float f = s * __builtin_amdgcn_exp2f(__builtin_fmaf(part[min(c / a.part_width, a.parts - 1)][0] - lse, LOG2E, -ONE_EXP));
       float p[8];
 #pragma unroll
       for (uint32_t j = 0; j < 8; ++j) {
@@ -535,7 +536,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     float p[8];
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
-      p[j] = s * __builtin_amdgcn_exp2f(__builtin_fmaf(q[j / 4][j % 4], LOG2E, -off));
+      p[j] = s * __builtin_amdgcn_exp2f((q[j / 4][j % 4] - lse) * LOG2E);
       if (c + j == y) p[j] = gy;
       if (c + j >= a.s.V) p[j] = 0.0f;
     }

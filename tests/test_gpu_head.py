@@ -199,6 +199,47 @@ def test_one_gradient(grads):
     check(call(c, grads=grads), expected(c))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("grads", ["hidden", "weight"])
+def test_one_gradient_in_pieces_the_last_of_few_rows(grads, dtype):
+    c = case(1300, 96, 700, dtype, ignored=0.2)
+    check(call(c, grads=grads, workspace="least"), expected(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_a_vocabulary_of_one_word(rows, dtype):
+    """The word is certain: no loss, no gradient."""
+    c = case(rows, 72, 1, dtype, scale="none")
+    loss, dh, dw = call(c)
+    assert not bool(loss.any()) and not bool(dh.any()) and not bool(dw.any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [50, 600])
+def test_no_loss_is_below_zero(rows, dtype):
+    """The target's z is the largest by far, and far from 0: nothing but roundings is left of the loss."""
+    c = case(rows, 64, 500, dtype)
+    w = c["weight"].float()
+    c["hidden"].copy_(100.0 * w[c["target"]] / w[c["target"]].square().sum(1, keepdim=True))
+    for grads in ("none", "both"):
+        loss = call(c, grads=grads)[0]
+        assert bool((loss >= 0).all()) and float(loss.max()) < 1e-3
+    check(call(c), expected(c))
+
+
+@pytest.mark.parametrize("rows", [30, 200])
+def test_scales_of_zero(rows):
+    """Rows whose gradient is wanted zero times, and none but such."""
+    c = case(rows, 64, 300, "bf16")
+    c["scale"][::3] = 0.0
+    check(call(c), expected(c))
+    c["scale"][:] = 0.0
+    loss, dh, dw = call(c)
+    check((loss, None, None), expected(c))
+    assert not bool(dh.any()) and not bool(dw.any())
+
+
 @pytest.mark.parametrize("scale", ["none", "mixed"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_scales_of_rows(dtype, scale):
