@@ -1,0 +1,82 @@
+"""Lists of tensors with states in 8 bits over several steps, against a plain evaluation in fp32 that goes its own way.
+
+The plain evaluation takes the multiplier of the gradients (clip over loss scale) from the list and nothing else: states, codes and weights are its own from
+the first step on.  Products, sums and codes are then the same fp32 operations on the same numbers, so the codes have to be equal, all of them; the
+weight's quotient may be two units in the last place off, so each step may add 16 e of the magnitudes that enter it (e = 2^-24)."""
+import pytest
+import torch
+
+from paper_2406_08334_amd import binding as B
+from test_gpu_tensors import E, HP, SIZES, List, randoms
+
+gpu = pytest.mark.gpu
+
+
+class Plain:
+    """The update of a list in elementary fp32 operations, from a copy of its arrays."""
+
+    def __init__(self, l):
+        self.l, self.w = l, [w.clone() for w in l.w]
+        value = lambda c, s: c.clone().view(torch.float8_e4m3fn).float() * s.repeat_interleave(256)[:len(c)]  # noqa: E731
+        self.codes = [(m.clone(), v.clone()) for m, v in zip(l.m, l.v)]
+        self.m = [value(c, s) for c, s in zip(l.m, l.ms)]
+        self.v = [value(c, s).square() for c, s in zip(l.v, l.vs)]
+        self.off = [torch.zeros(n, dtype=torch.float64, device="cuda") for n in l.sizes]         # how far the weights may be off by now
+
+    def step(self, t, mult, **hp):
+        hp = {**HP, **hp}
+        for i, (n, u) in enumerate(zip(self.l.sizes, randoms(self.l.sizes, self.l.seed, t))):
+            if not n:
+                continue
+            g = self.l.g[i].float() * mult
+            m = self.m[i] * hp["beta1"] + g * (1.0 - hp["beta1"])
+            v = self.v[i] * hp["beta2"] + g * (1.0 - hp["beta2"]) * g
+            d = v.sqrt() / (1.0 - hp["beta2"] ** t) ** 0.5 + hp["eps"]
+            rate = hp["lr"] / (1.0 - hp["beta1"] ** t)
+            keep = 1.0 if i in self.l.no_decay else 1.0 - hp["lr"] * hp["weight_decay"]
+            size = self.w[i].abs().double() * keep + rate * (self.m[i].abs() * hp["beta1"] + g.abs() * (1.0 - hp["beta1"])).double() / d.double()
+            self.off[i] += 16 * E * size
+            self.w[i] = self.w[i] * keep - rate * (m / d)
+            (cm, self.m[i]), (cv, r) = (to8(x, torch.from_numpy(k).float().cuda(), lift) for x, k, lift in ((m, u[0], False), (v.sqrt(), u[1], True)))
+            self.v[i] = r.square()
+            self.codes[i] = cm, cv
+
+
+def to8(x, u, lift):
+    """Codes of x, 256 that share a scale, and the values they stand for."""
+    n = len(x)
+    x = torch.nn.functional.pad(x, (0, -n % 256)).view(-1, 256)
+    u = torch.nn.functional.pad(u, (0, -n % 256)).view(-1, 256)
+    big = x.abs().amax(1, keepdim=True)
+    there = big >= 2.0 ** -100
+    y = x.abs() * torch.where(there, big.reciprocal() * 448.0, 0.0)
+    _, e = torch.frexp(y.clamp(min=2.0 ** -6))
+    step = torch.exp2((e - 4).float())
+    q = (torch.floor(y / step + u) * step).clamp(max=448.0)
+    if lift:
+        q = torch.where(y > 0, q.clamp(min=2.0 ** -9), q)
+    q = torch.where(x < 0, -q, q).to(torch.float8_e4m3fn)
+    scale = torch.where(there, big * (1.0 / 448.0), 0.0)
+    return q.view(-1)[:n].view(torch.uint8), (q.float() * scale).view(-1)[:n]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("zero", [True, False])
+def test_steps_that_go_on_from_each_other(zero, dtype):
+    """From states of zero, which only reach what a run can, and from momentum and variance that know nothing of each other: momenta up to hundreds of
+    times the root of the variance beside them, where a code of it decides over the weight's next step."""
+    l = List(SIZES + [200_000], 8, dtype, zero=zero, no_decay=(1, 5))
+    plain = Plain(l)
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    for t in range(1, 9):
+        for g in l.g:
+            g.copy_(torch.randn(g.shape, generator=gen, device="cuda") * 1e-2)
+        l.step()
+        plain.step(t, B.pt_tensors_report_read(l.list).grad_mult)
+        for i, n in enumerate(l.sizes):
+            for name, code, want in (("m", l.m[i], plain.codes[i][0]), ("v", l.v[i], plain.codes[i][1])):
+                same = (code == want) | ((code | want) & 0x7F == 0)                   # zero has two signs
+                assert bool(same.all()), (t, i, name, int((~same).sum()))
+            assert bool(((l.w[i].double() - plain.w[i].double()).abs() <= plain.off[i]).all()), (t, i)
+    l.close()
