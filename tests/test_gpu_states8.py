@@ -80,3 +80,58 @@ def test_steps_that_go_on_from_each_other(zero, dtype):
                 assert bool(same.all()), (t, i, name, int((~same).sum()))
             assert bool(((l.w[i].double() - plain.w[i].double()).abs() <= plain.off[i]).all()), (t, i)
     l.close()
+
+
+# ---- rounding that keeps the mean ----------------------------------------------------------------------
+
+N, SCALE, CODE, UP = 1 << 18, 1e-4, 288.0, 320.0          # elements; a block's scale; their code, and the next one
+PULL, SMALL, STEPS = 12.6, 0.4, 20                        # one pull by 0.39 of the distance; many by 0.0125 of it
+
+
+def mean_is_kept(values, want, steps):
+    """values: in codes.  Each step leaves an element one of two codes 32 apart, their spread at most half of that; so the mean of N is off by 16 / sqrt(N) times the root of
+    the steps, of which six times are allowed, and 1e-6 for the fp32 operations."""
+    return abs(float(values.mean()) - want) <= 6 * 16 * (steps / N) ** 0.5 + 1e-6 * want * steps
+
+
+@pytest.mark.parametrize("rounding", ["random", "nearest"])
+def test_what_the_mean_tells(rounding):
+    """On the host: the two tests below hold for rounding at random and fail by ten times their bound for rounding to nearest."""
+    gen = torch.Generator().manual_seed(1)
+
+    def one(y):
+        return (torch.floor(y / 32 + (torch.rand(N, generator=gen) if rounding == "random" else 0.5))) * 32
+    once, many = one(torch.full((N,), CODE + PULL)), torch.full((N,), CODE)
+    for _ in range(STEPS):
+        many = one(many + SMALL)
+    for values, want, steps in ((once, CODE + PULL, 1), (many, CODE + STEPS * SMALL, STEPS)):
+        assert mean_is_kept(values, want, steps) == (rounding == "random")
+        if rounding == "nearest":
+            assert abs(float(values.mean()) - want) > 6 * 1.5 * 16 * (steps / N) ** 0.5
+
+
+@gpu
+@pytest.mark.parametrize("pull,steps", [(PULL, 1), (SMALL, STEPS)])
+def test_the_mean_of_what_moves_by_part_of_a_code(pull, steps):
+    """Momenta of code 288 beside a block's largest of 448 that stays what it is: beta1 next to 1 and a gradient that pulls each by `pull` codes a step."""
+    l = List([N], 8, zero=True, dtype=torch.bfloat16, grad32=True)
+    code = lambda x: torch.tensor(x).to(torch.float8_e4m3fn).view(torch.uint8)  # noqa: E731
+    l.m[0].copy_(code(CODE).expand(N))
+    l.m[0][::256] = code(448.0)
+    l.ms[0].fill_(SCALE)
+    beta1 = 1.0 - 2.0 ** -9
+    # the largest's gradient is its own value: it stays; the others' is theirs and the pull over 1 - beta1
+    rest = torch.arange(N, device="cuda") % 256 != 0
+    B.pt_tensors_set_state(l.list, 10, 1.0, 0)
+    for t in range(steps):
+        torch.cuda.synchronize()
+        m = l.m[0].view(torch.float8_e4m3fn).float() * l.ms[0].repeat_interleave(256)
+        l.g[0].copy_(torch.where(rest, m + pull * SCALE * 2.0 ** 9, m))
+        l.step(beta1=beta1, max_norm=0.0)
+    torch.cuda.synchronize()
+    q = l.m[0].view(torch.float8_e4m3fn).float()[rest].double()
+    assert bool((l.ms[0] - SCALE).abs().max() <= 1e-6 * SCALE * steps)
+    if steps == 1:
+        assert sorted(q.unique().tolist()) == [CODE, UP]
+    assert mean_is_kept(q, CODE + steps * pull, steps)
+    l.close()
