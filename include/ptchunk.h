@@ -458,7 +458,7 @@ typedef struct {
  * magnitude / 448 (blocks whose largest is below 2^-100 become zero); all zero bytes and scales are m = v = 0.  The update computes
  * in fp32 (each product rounded before it is added) and rounds the states up or down at random with the odds that keep their mean
  * (rounding to nearest would hold an average in place that moves by less than half a code a step); a variance that is not zero keeps
- * one code at least.
+ * one code at least, and one that passes fp32's range is kept as fp32's largest, but for a part in 2^16.
  * The random numbers are a function of `seed`, the step counter and the element's place in the list: the same calls give the same
  * bits.  scaler as for pt_ctx_create.  Allocates and synchronises; not a hot call.
  * At most 2^31 blocks of 256 elements (each tensor's last one counted whole). */

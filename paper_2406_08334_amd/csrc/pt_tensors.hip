@@ -216,6 +216,9 @@ __device__ __forceinline__ Consts list_consts(const UpdateArgs& a, double& clip)
 }
 
 constexpr float TOP8 = 448.0f, TINY8 = 0x1p-100f, LOW8 = 0x1p-9f;        // largest and smallest number of the format; blocks of less than TINY8 are zero
+// An r is kept up to here: its square, a last place or two off by its scale, is an fp32 number still.  Were it inf, its block's others, one code at least
+// of a scale as large, would have squares of inf too, for good.
+constexpr float MOST_R = 0x1.ffffp63f;
 
 // Largest of x over the wave (of numbers >= 0), in every lane: in four steps over the 16 lanes of a row, then over the rows.
 template <int CTRL> __device__ __forceinline__ float dpp_max(float x) {
@@ -233,11 +236,11 @@ __device__ __forceinline__ float wave_max(float x) {
 }
 
 // sqrt of a number >= 0, rounded to the nearest but for one in some millions (x of normal size): the reciprocal root is right to its last
-// place, one step on the remainder.
+// place, one step on the remainder.  Of inf, a variance that no fp32 number holds, inf: the step would have inf times 0 in it.
 __device__ __forceinline__ float root(float x) {
   const float y = __builtin_amdgcn_rsqf(x), s = x * y;
   const float r = __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
-  return x > 0x1p-100f ? r : __builtin_sqrtf(x);
+  return x > 0x1p-100f ? (x < __builtin_inff() ? r : x) : __builtin_sqrtf(x);
 }
 
 // The update with states in 8 bits: as update_element, but every product is rounded before it is added.  A code is a threshold on m and r, and a
@@ -347,7 +350,7 @@ struct Block {
     if constexpr (BITS == 8) {
       const float bm = fminf(wave_max(fmaxf(fmaxf(__builtin_fabsf(m[0]), __builtin_fabsf(m[1])), fmaxf(__builtin_fabsf(m[2]), __builtin_fabsf(m[3])))),
                              3.402823466e38f);
-      const float bv = fminf(wave_max(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]))), 3.402823466e38f);
+      const float bv = fminf(wave_max(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]))), MOST_R);
       const bool hm = bm >= TINY8, hv = bv >= TINY8;
       const float im = hm ? 1.0f / bm * TOP8 : 0.0f, iv = hv ? 1.0f / bv * TOP8 : 0.0f;
       uint32_t z[4];

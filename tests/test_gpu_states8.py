@@ -135,3 +135,42 @@ def test_the_mean_of_what_moves_by_part_of_a_code(pull, steps):
         assert sorted(q.unique().tolist()) == [CODE, UP]
     assert mean_is_kept(q, CODE + steps * pull, steps)
     l.close()
+
+
+# ---- a gradient whose square is no fp32 number -----------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("grad32", [False, True])
+def test_a_variance_beyond_fp32(grad32):
+    """Finite gradients of 1e20 without a clip: the norm is finite, so the step is taken, and the variance is inf in 32 bits.  The weight gets its decay and
+    nothing else, as with states in 32 bits; in 8 bits the state stays finite, so that its block comes back."""
+    sizes = [700, 300]
+    lists = [List(sizes, bits, zero=True, grad32=grad32) for bits in (8, 32)]
+    for l in lists:
+        l.g[0][5], l.g[0][600], l.g[1][299] = 1e20, -1e20, 3e38
+    start = [w.double() for w in lists[0].w]
+    for l in lists:
+        l.step(max_norm=0.0)
+        torch.cuda.synchronize()
+        assert B.pt_tensors_report_read(l.list).step == 1
+    small, large = lists
+    keep = 1.0 - HP["lr"] * HP["weight_decay"]
+    for i in range(2):
+        assert bool(small.w[i].isfinite().all()) and bool(small.p[i].float().isfinite().all())
+        size = start[i].abs() * keep + HP["lr"] * 1.1            # of a first step, which moves a weight by lr at most
+        assert bool(((small.w[i].double() - large.w[i].double()).abs() <= 16 * E * size).all())
+    for i, k in ((0, 5), (0, 600), (1, 299)):
+        assert abs(float(small.w[i][k]) - float(start[i][k]) * keep) <= 2 * E * abs(float(start[i][k]))
+    assert bool(large.v[0][5].isinf())
+    for _ in range(3):                                           # gradients as usual again
+        for l in lists:
+            for g in l.g:
+                g.fill_(1e-2)
+        small.step()
+        for i in range(2):
+            r = small.v[i].view(torch.float8_e4m3fn).float() * small.vs[i].repeat_interleave(256)[:sizes[i]]
+            assert bool(r.square().isfinite().all()) and bool(small.ms[i].isfinite().all())
+            assert bool(small.w[i].isfinite().all())
+    for l in lists:
+        l.check_guards()
+        l.close()
