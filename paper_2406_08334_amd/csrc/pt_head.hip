@@ -4,7 +4,7 @@
 //   gather   their hidden states next to each other, zero-padded to whole steps of the products
 //   logits   z = W h^T on the matrix cores, tile by tile; of each wave's part of a tile the largest z and the sum of exp(z - that) of every row, and, for
 //            gradients, exp(z - that) (fp16 inputs: z in fp32)
-//   soft     from those lse and loss of a row; G = s (exp(z - lse) - [target]) in 16 bits, in place
+//   soft     from those largest z, log of the sum (lse in two parts) and loss of a row; G = s (exp(z - lse) - [target]) in 16 bits, in place
 //   d_hidden = G W, d_weight = G^T h on the matrix cores
 //
 // Three products of 2 rows vocab width operations each are what it costs.  Gradients want lse of a whole row before the first of them: pieces of the
@@ -413,14 +413,18 @@ __device__ __forceinline__ f32x2 join_row(const f32x2* part, uint32_t parts) {
   return join(join(s_x[0], s_x[1]), join(s_x[2], s_x[3]));
 }
 
+// A row's loss from its largest z, the sum of exp(z - that) and the target's z.  The difference of two z first: lse as one number would be rounded at the
+// size of the logits, and a small loss beside large ones is less than that (z of 4000: 1e-4).
+__device__ __forceinline__ float loss_of(f32x2 x, float zy) { return (x[0] - zy) + logf(x[1]); }
+
 // The loss alone: a workgroup a row.  4096 rows, 250 parts each: 9 us.
 __global__ void __launch_bounds__(256) k_head_loss(const SoftArgs a) {
   const uint32_t r = blockIdx.x;
   if (r >= (a.target ? a.rows : piece_rows(a.meta, a.first, a.rows))) return;
   const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
   if (threadIdx.x != 0) return;
-  if (a.target) a.loss[r] = uint64_t(a.target[r]) < a.s.V ? x[0] + logf(x[1]) - a.at_target[r] : 0.0f;
-  else a.loss[a.row_of[r]] = x[0] + logf(x[1]) - a.at_target[r];
+  if (a.target) a.loss[r] = uint64_t(a.target[r]) < a.s.V ? loss_of(x, a.at_target[r]) : 0.0f;
+  else a.loss[a.row_of[r]] = loss_of(x, a.at_target[r]);
 }
 
 // Eight numbers in 16 bits, and what is left of them.
@@ -499,10 +503,10 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
   }
   const f32x2 x = join_row(a.part + size_t(r) * a.parts, a.parts);
   const uint32_t row = a.target ? r : a.row_of[r];
-  const float zy = a.at_target[r], lse = x[0] + logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * up;
-  const float gy = s * expm1f(zy - lse);
+  const float top = x[0], log_sum = logf(x[1]), s = (a.scale ? a.scale[row] : 1.0f) * up, loss = loss_of(x, a.at_target[r]);
+  const float gy = s * expm1f(-loss);
   if (tid == 0 && blockIdx.y == 0) {
-    a.loss[row] = lse - zy;
+    a.loss[row] = loss;
     a.rest[r] = gy - decode16<DT>(encode16<DT>(gy));
   }
   if constexpr (KEEP_EXP<DT>) {
@@ -511,7 +515,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
 #pragma unroll 4
     for (uint32_t c = first; c < a.s.Vp; c += turn) {
       const f16x8 e = __builtin_bit_cast(f16x8, *(const PT_GLOBAL u32x4*)((const PT_GLOBAL uint16_t*)a.z + size_t(r) * a.s.Vp + c));
-      const float f = s * __builtin_amdgcn_exp2f(__builtin_fmaf(part[min(c / a.part_width, a.parts - 1)][0] - lse, LOG2E, -ONE_EXP));
+      const float f = s * __builtin_amdgcn_exp2f(__builtin_fmaf((part[min(c / a.part_width, a.parts - 1)][0] - top) - log_sum, LOG2E, -ONE_EXP));
       float p[8];
 #pragma unroll
       for (uint32_t j = 0; j < 8; ++j) {
@@ -536,7 +540,7 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     float p[8];
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
-      p[j] = s * __builtin_amdgcn_exp2f((q[j / 4][j % 4] - lse) * LOG2E);
+      p[j] = s * __builtin_amdgcn_exp2f(((q[j / 4][j % 4] - top) - log_sum) * LOG2E);
       if (c + j == y) p[j] = gy;
       if (c + j >= a.s.V) p[j] = 0.0f;
     }
