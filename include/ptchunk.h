@@ -488,7 +488,7 @@ int pt_tensors_report_read(pt_tensors* list, pt_step_report* out, void* stream);
  * A row whose target lies outside [0, vocab) is ignored: its loss and its row of d_hidden are 0, it adds nothing to d_weight,
  * and whatever its hidden state holds (inf and NaN too) reaches no result.  16-bit inputs, fp32 sums of their exact products; G is
  * rounded to the 16-bit type between the two products it takes part in (of bf16 inputs its exponentials to fp16 before; what the
- * rounding has left at the target goes into d_hidden, and of up to 128 rows all that it has left into d_weight), and so are the results.
+ * rounding has left at the target takes part in both, and of up to 128 rows all that it has left in d_weight's), and so are the results.
  * No loss is below 0.  No array that is written may overlap another one.
  * d_hidden and d_weight may each be NULL: then that gradient is not taken; with both NULL only the loss is, and nothing of the
  * size of the logits is written at all. */

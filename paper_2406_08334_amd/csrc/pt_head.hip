@@ -1,11 +1,12 @@
 // Loss of a language model's head: softmax cross entropy from hidden states and weight, with gradients, logits of a piece of the rows at a time.
 //
-//   rows     the rows with a target, counted and listed on the device (ignored ones take no part in anything that follows)
+//   rows     the rows with a target, counted and listed on the device (ignored ones take no part in anything that follows); for the gradient of the
+//            weight in the order of their targets, 128 words at a time
 //   gather   their hidden states next to each other, zero-padded to whole steps of the products
 //   logits   z = W h^T on the matrix cores, tile by tile; of each wave's part of a tile the largest z and the sum of exp(z - that) of every row, and, for
 //            gradients, exp(z - that) (fp16 inputs: z in fp32)
 //   soft     from those largest z, log of the sum (lse in two parts) and loss of a row; G = s (exp(z - lse) - [target]) in 16 bits, in place
-//   d_hidden = G W, d_weight = G^T h on the matrix cores
+//   d_hidden = G W, d_weight = G^T h on the matrix cores, and with them what rounding G has left at the targets
 //
 // Three products of 2 rows vocab width operations each are what it costs.  Gradients want lse of a whole row before the first of them: pieces of the
 // vocabulary would take the first product twice, so the pieces are rows, of which as many are taken at a time as the workspace has room for.
@@ -50,7 +51,9 @@ struct Shape {
   uint32_t R, V, d;
   uint32_t Kd, Vp;           // width and vocabulary rounded up to whole steps and tiles
   uint32_t low;              // 0, or, of few rows, how far behind a row of G what its rounding has left lies (and h once more)
+  uint32_t groups;           // of GROUP words, which the rows are ordered by; 1: they are in the call's order
 };
+constexpr uint32_t GROUP = 128;            // what the smaller tiles of d_weight have of the vocabulary
 
 // ---- rows ---------------------------------------------------------------------------------------------
 
@@ -64,21 +67,48 @@ __device__ __forceinline__ Meta found_rows(uint32_t n, float big) {
   return {n, ldexpf(1.0f, e), ldexpf(1.0f, -e)};
 }
 
-// The rows that have a target, in order, by a workgroup of THREADS.
 struct RowArgs {
   const int64_t* target;
   const float* scale;
   Shape s;
   Meta* meta;
   uint32_t *row_of, *target_of;
+  uint32_t* starts;          // [groups + 1]: where the rows of a group begin
 };
+
+// How many rows have a target below `word`, by a workgroup of THREADS.
+template <int THREADS>
+__device__ __forceinline__ uint32_t rows_below(const RowArgs& a, uint32_t word) {
+  constexpr uint32_t WAVES = THREADS / 64, TURN = 8;
+  __shared__ uint32_t s_below[WAVES];
+  uint32_t n = 0;
+  for (uint32_t r0 = 0; r0 < a.s.R; r0 += TURN * THREADS) {
+    int64_t y[TURN];
+#pragma unroll
+    for (uint32_t q = 0; q < TURN; ++q) {
+      const uint32_t r = r0 + q * THREADS + threadIdx.x;
+      y[q] = r < a.s.R ? a.target[r] : -1;
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < TURN; ++q) n += uint64_t(y[q]) < word ? 1u : 0u;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+  if ((threadIdx.x & 63) == 0) s_below[threadIdx.x >> 6] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < WAVES; ++w) n += s_below[w];
+  return n;
+}
+
+// The rows whose target is one of `words` from `word` on, in order, by a workgroup of THREADS; n: how many lie before them.  found: of all rows up to those.
 template <int THREADS, class F>
-__device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& each) {
+__device__ __forceinline__ void list_rows(const RowArgs& a, uint32_t word, uint32_t words, uint32_t n, Meta& found, F&& each) {
   constexpr uint32_t WAVES = THREADS / 64, TURN = 4;       // rows of a lane at a time: their loads are under way together
   __shared__ uint32_t s_n[TURN * WAVES];
   __shared__ float s_big[WAVES];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t n = 0;
   float big = 0.0f;
   for (uint32_t r0 = 0; r0 < a.s.R; r0 += TURN * THREADS) {
     int64_t y[TURN];
@@ -92,9 +122,8 @@ __device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& eac
     }
 #pragma unroll
     for (uint32_t q = 0; q < TURN; ++q) {
-      const bool has = uint64_t(y[q]) < a.s.V;
-      if (has) big = fmaxf(big, scale[q]);
-      mask[q] = __ballot(has);
+      if (uint64_t(y[q]) < a.s.V) big = fmaxf(big, scale[q]);
+      mask[q] = __ballot(uint64_t(y[q]) - word < words);
       if (lane == 0) s_n[q * WAVES + wave] = uint32_t(__popcll(mask[q]));
     }
     __syncthreads();
@@ -103,7 +132,7 @@ __device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& eac
       uint32_t before = 0, all = 0;
 #pragma unroll
       for (uint32_t w = 0; w < WAVES; ++w) { const uint32_t k = s_n[q * WAVES + w]; before += w < wave ? k : 0; all += k; }
-      if (uint64_t(y[q]) < a.s.V)
+      if (uint64_t(y[q]) - word < words)
         each(n + before + uint32_t(__popcll(mask[q] & ((uint64_t(1) << lane) - 1))), r0 + q * THREADS + threadIdx.x, uint32_t(y[q]));
       n += all;
     }
@@ -118,11 +147,18 @@ __device__ __forceinline__ void list_rows(const RowArgs& a, Meta& found, F&& eac
   found = found_rows(n, big);
 }
 
-// One workgroup lists the rows of a call, in order: no count of another has to be waited for.  Bound by the round trips of its turns: 8192 rows in 10 us.
+// A workgroup lists the rows of a group: each goes through all targets, twice, so that no count of another has to be waited for.  Bound by the round trips
+// of its turns: 8192 rows in 11 us by 8 workgroups (1000 words), 13 by 393 (50257 words), 22 by 1024 (131072, two rounds of them); in the call's order, by
+// one that goes through them once, 10.
 __global__ void __launch_bounds__(1024) k_head_rows(const RowArgs a) {
+  const uint32_t g = blockIdx.x, word = a.s.groups > 1 ? g * GROUP : 0, n = g ? rows_below<1024>(a, word) : 0;
   Meta m;
-  list_rows<1024>(a, m, [&](uint32_t at, uint32_t r, uint32_t y) { a.row_of[at] = r; a.target_of[at] = y; });
-  if (threadIdx.x == 0) *a.meta = m;
+  list_rows<1024>(a, word, a.s.groups > 1 ? min(GROUP, a.s.V - word) : a.s.V, n, m, [&](uint32_t at, uint32_t r, uint32_t y) { a.row_of[at] = r; a.target_of[at] = y; });
+  if (threadIdx.x != 0) return;
+  a.starts[g] = n;
+  if (g + 1 < a.s.groups) return;
+  a.starts[g + 1] = m.count;
+  *a.meta = m;
 }
 
 // One row of 16-bit words, at any address, into one of Kd words that begins at a multiple of 16 bytes; zero behind its end.
@@ -140,31 +176,52 @@ __device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOB
 }
 
 // A wave a row: the hidden states of the rows with a target, zero rows up to a whole step behind them, and nothing for those without one.
-// LIST: every workgroup lists the rows by itself, of which there are LISTED at most: a launch less (1000 x 1024 x 8000 105 -> 101 us).
+// LIST: every workgroup lists the rows by itself, of which there are LISTED at most: a launch less (1000 x 1024 x 8000 105 -> 101 us); a wave counts the rows
+// that its own comes behind.
 // Bound by memory: 8192 rows of 4096 in 22 us, 5.2 TB/s.
 constexpr uint32_t LISTED = 1024;
 template <bool LIST>
 __global__ void __launch_bounds__(256) k_head_gather(const RowArgs a, const uint16_t* __restrict__ hidden, uint64_t stride, uint16_t* __restrict__ packed,
                                                      float* __restrict__ loss, uint16_t* __restrict__ d_hidden, uint64_t d_stride) {
-  __shared__ uint32_t s_row[LIST ? LISTED : 1];
+  __shared__ uint32_t s_row[LIST ? LISTED : 1], s_target[LIST ? LISTED : 1];
   const uint32_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const Shape& s = a.s;
-  uint32_t n, from = 0;
+  uint32_t n, from = 0, place = r;
   if constexpr (LIST) {
     Meta m;
-    list_rows<256>(a, m, [&](uint32_t at, uint32_t row, uint32_t y) {
-      s_row[at] = row;
-      if (blockIdx.x == 0) { a.row_of[at] = row; a.target_of[at] = y; }
-    });
+    list_rows<256>(a, 0, s.V, 0, m, [&](uint32_t at, uint32_t row, uint32_t y) { s_row[at] = row; s_target[at] = y; });
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.meta = m;
     n = m.count;
-    if (r < n) from = s_row[r];
+    if (r < n) {
+      from = s_row[r];
+      const uint32_t y = s_target[r];
+      if (s.groups > 1) {
+        const uint32_t g = y / GROUP;
+        uint32_t begun = 0;                                // the groups up to that of the row before
+        place = 0;
+        for (uint32_t i = lane; i < n; i += 64) {
+          const uint32_t h = s_target[i] / GROUP;
+          const bool before = h < g || (h == g && i < r);
+          place += before ? 1 : 0;
+          begun = max(begun, before ? h + 1 : 0);
+        }
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) { place += __shfl_xor(place, off, 64); begun = max(begun, uint32_t(__shfl_xor(begun, off, 64))); }
+        place = __builtin_amdgcn_readfirstlane(place);
+        for (uint32_t i = begun + lane; i <= g; i += 64) a.starts[i] = place;
+        if (place + 1 == n)
+          for (uint32_t i = g + 1 + lane; i <= s.groups; i += 64) a.starts[i] = n;
+      }
+      if (lane == 0) { a.row_of[place] = from; a.target_of[place] = y; }
+    } else if (n == 0 && r == 0) {
+      for (uint32_t i = lane; i <= s.groups; i += 64) a.starts[i] = 0;
+    }
   } else {
     n = a.meta->count;
     if (r < n) from = a.row_of[r];
   }
   const uint32_t zeros = s.low ? s.low : (n + TWO - 1) / TWO * TWO;
-  for (uint32_t at = r; at < zeros + s.low && r < zeros; at += s.low) {          // once, or twice
+  for (uint32_t at = place; at < zeros + s.low && r < zeros; at += s.low) {      // once, or twice
     PT_GLOBAL uint16_t* to = (PT_GLOBAL uint16_t*)packed + size_t(at) * s.Kd;
     if (r < n) copy_row((const PT_GLOBAL uint16_t*)hidden + from * stride, to, s.d, s.Kd, lane, 64);
     else
@@ -226,8 +283,8 @@ template <class C> __host__ __device__ inline Split split(uint32_t tiles, uint32
 // Tile i of tm x tn: the 32 of an XCD that run at a time make patches of about 4 n x 8 m, which share what they read.  (Patches of 8 n: 8192 (6144) x 4096 x
 // 32000 3870 us instead of 3800, 4096 x 4096 x 32000 835, 827; 16 n: 3940, 855; 2 n: 3850, 832.)
 __device__ __forceinline__ void tile_at(uint32_t i, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
-  constexpr uint32_t GROUP = 4;
-  const uint32_t g = i / (GROUP * tm), n0 = g * GROUP, gn = min(GROUP, tn - n0), r = i - g * GROUP * tm;
+  constexpr uint32_t PATCH = 4;
+  const uint32_t g = i / (PATCH * tm), n0 = g * PATCH, gn = min(PATCH, tn - n0), r = i - g * PATCH * tm;
   n = n0 + r % gn;
   m = r / gn;
 }
@@ -400,6 +457,7 @@ struct SoftArgs {
   uint16_t* g;               // G; where z lies, or, of few rows, elsewhere
   uint64_t g_pitch;          // bytes
   float* rest;               // [rows]: of G at the target, what its rounding has left
+  uint16_t* rests;           // [rows][2 GROUP]: the same as a row of a matrix over two groups of words, zero at all others; or NULL
 };
 
 // Of the workgroup, in all its lanes.
@@ -509,6 +567,13 @@ __global__ void __launch_bounds__(256) k_head_soft(const SoftArgs a) {
     a.loss[row] = loss;
     a.rest[r] = gy - decode16<DT>(encode16<DT>(gy));
   }
+  if (a.rests && tid < 2 * GROUP / 8) {
+    const uint32_t rest = encode16<DT>(gy - decode16<DT>(encode16<DT>(gy))), at = y % (2 * GROUP);
+    u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) w[j] = at / 2 == tid * 4 + j ? rest << (16 * (at & 1)) : 0;
+    *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.rests + size_t(r) * (2 * GROUP) + tid * 8) = w;
+  }
   if constexpr (KEEP_EXP<DT>) {
     typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
     const PT_GLOBAL f32x2* part = (const PT_GLOBAL f32x2*)a.part + size_t(r) * a.parts;
@@ -584,6 +649,8 @@ struct GradArgs {
   float* part;               // sums of several workgroups a tile: [n][tail][BN][BM]
   Split split;               // of d_weight
   const float* rest;
+  const uint16_t* rests;     // of the piece, for d_weight, and where the groups' rows begin; or NULL
+  const uint32_t* starts;
   const uint16_t* weight;
   uint64_t weight_stride;
   float* acc;                // d_weight over several pieces: sums so far [V][pitch]
@@ -592,7 +659,7 @@ struct GradArgs {
 };
 
 // G at the target has been rounded like the rest of its row, of which it can be the only number that counts: what that has left, times the target's
-// row of the weight, goes into the sum in fp32.
+// row of the weight, goes into the sum in fp32.  (Into d_weight: d_weight_tile.)
 template <int DT>
 __device__ __forceinline__ f32x4 add_rest(f32x4 x, float rest, const PT_GLOBAL uint16_t* w, uint32_t m, uint32_t d) {
   if (m >= d) return x;
@@ -710,8 +777,12 @@ __global__ void __launch_bounds__(256) k_head_join(const GradArgs a) {
   });
 }
 
-// d_weight: m runs over the width, n over the vocabulary, k over the piece's rows.  Products bound it: 6144 x 4096 x 32000 1.21 ms, 1330 TFLOP/s;
-// 8192 x 1600 x 50257 1.05 ms, 1250.
+// d_weight: m runs over the width, n over the vocabulary, k over the piece's rows, and once more over those whose target is a word of the tile: what is left
+// of their G there, a matrix with one number a row, so that a word with a thousand rows takes no longer than a thousand with one.  A tile's rows lie next to
+// each other, as they are ordered by target: of 8192 rows and 50257 words 42, one round of two steps behind 64.  (8192 x 1600 x 50257 3.66 -> 3.69 ms for the whole
+// call, 1531 x 771 x 50257 604 -> 619 us, 8192 x 512 x 1000 97 -> 104; the error against 64 bits of 6144 x 4096 x 32000, bf16: 2.2e-3 to 2.4e-3 -> 1.66e-3, what
+// rounding the result costs.)
+// Products bound it: 6144 x 4096 x 32000 1.21 ms, 1330 TFLOP/s; 8192 x 1600 x 50257 1.05 ms, 1250.
 template <int DT, class C>
 __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even, lds_char* odd, uint32_t block) {
   const uint32_t n_rows = piece_rows(a.meta, a.first, a.rows);
@@ -726,6 +797,17 @@ __device__ __forceinline__ void d_weight_tile(const GradArgs& a, lds_char* even,
   with_tile<DT, C, false, false>(a.s.d - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
     t.run(even, odd, p, q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+    if (a.rests) {
+      const uint32_t g = tn * (C::BN / GROUP), end = a.first + piece_rows(a.meta, a.first, a.rows);
+      const uint32_t r0 = max(a.starts[g], a.first) - a.first, r1 = min(max(a.starts[min(g + C::BN / GROUP, a.s.groups)], a.first), end) - a.first;
+      if (r0 < r1) {
+        const uint32_t more = (r1 - r0 + TWO - 1) / TWO, m0 = left ? more * part / a.split.n : 0, m1 = left ? more * (part + 1) / a.split.n : more;
+        __builtin_amdgcn_s_barrier();
+        Operand h = a.p;
+        h.k = min(r0 + m1 * TWO, r1);
+        t.add(even, odd, h, {a.rests + tn * C::BN % (2 * GROUP), 2 * (2 * GROUP), C::BN, h.k}, tm * C::BM, 0, r0 + m0 * TWO, m1 - m0);
+      }
+    }
     const uint32_t lane = threadIdx.x & 63, mw = tm * C::BM + t.wave_m(), mb = mw + (lane >> 4) * 4;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -803,8 +885,9 @@ struct Plan {
   Shape s;
   uint32_t parts, pitch, pieces, rows;
   bool grads, direct, as_is;               // direct: the weight is taken where it lies; as_is: so are the hidden states
+  bool ordered;                            // rows by target, for d_weight
   Most hidden;                             // of a whole piece
-  uint64_t meta, row_of, target_of, at_target, rest, packed, weight, part, z, g, g_pitch, sums, acc, total;
+  uint64_t meta, row_of, target_of, starts, at_target, rest, rests, packed, weight, part, z, g, g_pitch, sums, acc, total;
 };
 
 // Partial sums of a row's exponentials.
@@ -853,8 +936,10 @@ Most most_hidden(const Shape& s, uint32_t rows) {
 
 Plan make_plan(const pt_head& h, uint64_t rows) {
   Plan p{};
-  p.s = {h.rows, h.vocab, h.width, uint32_t(up(h.width, TWO)), uint32_t(up(h.vocab, 256)), 0};
+  p.s = {h.rows, h.vocab, h.width, uint32_t(up(h.width, TWO)), uint32_t(up(h.vocab, 256)), 0, 1};
   if (h.d_weight && h.rows <= LOW_ROWS) p.s.low = uint32_t(up(h.rows, BK));
+  p.ordered = h.d_weight && h.rows > LOW_ROWS;
+  if (p.ordered) p.s.groups = (h.vocab + GROUP - 1) / GROUP;
   p.grads = h.d_hidden || h.d_weight;
   p.direct = h.width % BK == 0 && h.weight_stride % 8 == 0 && (uintptr_t)h.weight % 16 == 0;
   p.as_is = p.direct && h.rows <= FEW_ROWS && h.hidden_stride % 8 == 0 && h.hidden_stride <= (1u << 21) && (uintptr_t)h.hidden % 16 == 0;
@@ -869,8 +954,10 @@ Plan make_plan(const pt_head& h, uint64_t rows) {
   p.meta = take(sizeof(Meta));
   p.row_of = take(4ull * h.rows);
   p.target_of = take(4ull * h.rows);
+  p.starts = take(4ull * (p.s.groups + 1));
   p.at_target = take(4ull * p.rows);
   p.rest = take(p.grads ? 4ull * p.rows : 0);
+  p.rests = take(p.ordered ? 2ull * (2 * GROUP) * p.rows : 0);
   p.packed = take(2ull * (up(h.rows, TWO) + p.s.low) * p.s.Kd);
   p.weight = take(p.direct ? 0 : 2ull * h.vocab * p.s.Kd);
   p.part = take(8ull * p.rows * p.parts);
@@ -955,7 +1042,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
   Meta* meta = (Meta*)(ws + p.meta);
   uint32_t *row_of = (uint32_t*)(ws + p.row_of), *target_of = (uint32_t*)(ws + p.target_of);
   uint16_t* packed = (uint16_t*)(ws + p.packed);
-  const RowArgs ra = {h.target, h.row_scale, s, meta, row_of, target_of};
+  const RowArgs ra = {h.target, h.row_scale, s, meta, row_of, target_of, (uint32_t*)(ws + p.starts)};
   const dim3 gather(uint32_t(up(s.R, TWO) / 4));
   if (p.as_is) {
     // few rows: those without a target are multiplied too, and what else gathering does is done with G
@@ -963,7 +1050,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     hipLaunchKernelGGL(k_head_gather<true>, gather, dim3(256), 0, st, ra, (const uint16_t*)h.hidden, h.hidden_stride, packed, h.loss, (uint16_t*)h.d_hidden,
                        h.d_hidden_stride);
   } else {
-    hipLaunchKernelGGL(k_head_rows, dim3(1), dim3(1024), 0, st, ra);
+    hipLaunchKernelGGL(k_head_rows, dim3(s.groups), dim3(1024), 0, st, ra);
     PT_LAUNCH_CHECK(nullptr, "k_head_rows");
     hipLaunchKernelGGL(k_head_gather<false>, gather, dim3(256), 0, st, ra, (const uint16_t*)h.hidden, h.hidden_stride, packed, h.loss,
                        (uint16_t*)h.d_hidden, h.d_hidden_stride);
@@ -995,7 +1082,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     const SoftArgs sa = {s, meta, first, rows, row_of + first, target_of + first, la.target, (const uint16_t*)h.hidden,
                          h.hidden_stride, packed, la.part, la.parts,
                          uint32_t(few ? Few::BM / Few::WM : mid ? Mid::BM / Mid::WM : Big::BM / Big::WM), la.at_target, h.row_scale, h.loss, ws + p.z,
-                         (uint16_t*)(ws + p.g), p.g_pitch, (float*)(ws + p.rest)};
+                         (uint16_t*)(ws + p.g), p.g_pitch, (float*)(ws + p.rest), p.ordered ? (uint16_t*)(ws + p.rests) : nullptr};
     if (!p.grads) {
       hipLaunchKernelGGL(k_head_loss, dim3(rows), dim3(256), 0, st, sa);
       PT_LAUNCH_CHECK(nullptr, "k_head_loss");
@@ -1005,7 +1092,7 @@ int run(const pt_head& h, const Plan& p, char* ws, hipStream_t st) {
     hipLaunchKernelGGL(k_head_soft<DT>, dim3(uint32_t(up(rows, TWO)) + (p.as_is ? s.low : 0), slices), dim3(256), 0, st, sa);
     PT_LAUNCH_CHECK(nullptr, "k_head_soft");
     const GradArgs ga = {s, {weight, stride * 2, width, s.V}, {ws + p.g, p.g_pitch, 0, s.Vp}, meta, first, rows, row_of + first, target_of + first,
-                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (float*)(ws + p.sums), wt.split, sa.rest, weight, stride, (float*)(ws + p.acc), p.pitch,
+                   (uint16_t*)h.d_hidden, h.d_hidden_stride, (float*)(ws + p.sums), wt.split, sa.rest, sa.rests, ra.starts, weight, stride, (float*)(ws + p.acc), p.pitch,
                    i > 0, i + 1 < p.pieces};
     GradArgs gw = ga;
     gw.p = {hid, 2ull * s.Kd, s.Kd, 0};
@@ -1046,7 +1133,7 @@ extern "C" int pt_head_loss(const pt_head* head, void* workspace, uint64_t works
   if (!head->rows) {
     if (!head->d_weight) return PT_OK;
     hipLaunchKernelGGL(k_head_zero, dim3(head->vocab), dim3(256), 0, st, (uint16_t*)head->d_weight, head->d_weight_stride,
-                       Shape{0, head->vocab, head->width, 0, 0, 0});
+                       Shape{0, head->vocab, head->width, 0, 0, 0, 1});
     PT_LAUNCH_CHECK(nullptr, "k_head_zero");
     return PT_OK;
   }

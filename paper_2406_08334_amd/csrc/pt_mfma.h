@@ -168,10 +168,18 @@ struct Tile {
   // cannot tell from what it reads.
   __device__ __forceinline__ void run(lds_char* even, lds_char* odd, const Operand& p, const Operand& q, uint32_t m0, uint32_t n0, uint32_t k0,
                                       uint32_t twos) {
+    clear();
+    add(even, odd, p, q, m0, n0, k0, twos);
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // To the sums so far.  Between two of them the workgroup has to meet.
+  __device__ __forceinline__ void add(lds_char* even, lds_char* odd, const Operand& p, const Operand& q, uint32_t m0, uint32_t n0, uint32_t k0,
+                                      uint32_t twos) {
     if (!twos) return;
     sp.init(p, m0, k0, wave_m());
     sq.init(q, n0, k0, wave_n());

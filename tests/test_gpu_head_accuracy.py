@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2406_08334_amd import binding as B
-from test_gpu_head import DTYPES, E, call
+from test_gpu_head import DTYPES, E, call, case
 
 pytestmark = pytest.mark.gpu
 C = 8.0                                                    # the first element of every row of the weight
@@ -65,3 +65,64 @@ def test_small_losses_beside_large_logits(rows, offset, dtype):
         bound = bound * (1 + u) + u * want.abs().clamp(min=tiny)
         off = (got.double().cpu() - want).abs()
         assert bool((off <= bound).all()), f"{name}: {float((off / bound).max()):.3g} of the bound"
+
+
+# ---- what rounding G leaves at the target ----------------------------------------------------------------
+
+def expected(c, where="cuda"):
+    """Gradients in 64 bits and their bounds.  D: what z can be off by (sums of `width` exact products in fp32, any order); G is rounded by u away from the target, where bf16's
+    exponentials are rounded to 11 bits before; at the target what the rounding leaves is multiplied too, rounded by u itself: u^2."""
+    dt = c["hidden"].dtype
+    u, tiny = next((u, t) for d, u, t in DTYPES.values() if d == dt)
+    w, y = c["weight"].double().to(where), c["target"].to(where)
+    rows, width = c["hidden"].shape
+    on = ((y >= 0) & (y < w.shape[0])).nonzero()[:, 0]
+    h, s, yy = c["hidden"].double().to(where)[on], c["scale"].double().to(where)[on], y[on]
+    D = 2 * (width + 64) * E * (h.abs() @ w.abs().t()).amax(1) + 2e-5
+    logp = torch.log_softmax(h @ w.t(), 1)
+    i = torch.arange(len(on), device=where)
+    p = logp.exp()
+    g = p.clone()
+    g[i, yy] = torch.expm1(logp[i, yy])
+    dg = g.abs() * (u + (2.0 ** -11 if dt == torch.bfloat16 else 0.0))
+    dg[i, yy] = g[i, yy].abs() * (u * u + 8 * E)
+    dg = s.abs()[:, None] * (dg + D[:, None] * p) + float(s.abs().max()) * 2.0 ** -38
+    g = g * s[:, None]
+    dh, dh_b = (torch.zeros(rows, width, dtype=torch.float64, device=where) for _ in range(2))
+    dh[on], dh_b[on] = g @ w, dg @ w.abs() + (w.shape[0] + 64) * E * (g.abs() @ w.abs())
+    dw, dw_b = g.t() @ h, dg.t() @ h.abs() + (2 * len(on) + 64) * E * (g.abs().t() @ h.abs())
+    return [(x, b * (1 + u) + u * x.abs().clamp(min=tiny)) for x, b in ((dh, dh_b), (dw, dw_b))]
+
+
+def check(got, want):
+    for name, x, (w, b) in zip(("d_hidden", "d_weight"), got[1:], want):
+        if x is None:
+            continue
+        off = (x.double().to(w.device) - w).abs()
+        assert bool((off <= b).all()), f"{name}: {float((off / b.clamp(min=1e-300)).max()):.3g} of the bound"
+
+
+# few rows and many, listed by one workgroup and by all; tiles of both kinds, shared and not; widths that end inside one; a vocabulary inside one
+# tile, and one word
+ROWS = [(64, 128, 900, None), (128, 200, 900, None), (129, 200, 900, None), (300, 771, 1500, None), (1024, 320, 12800, None), (1025, 96, 700, "least"),
+        (2100, 640, 9000, None), (2600, 64, 3000, "least"), (3000, 203, 700, None), (9000, 64, 40, None), (5000, 130, 300, "least"), (700, 72, 2, None)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,vocab,workspace", ROWS)
+def test_the_target_takes_part_unrounded(rows, width, vocab, workspace, dtype):
+    c = case(rows, width, vocab, dtype, ignored=0.2)
+    want = expected(c)
+    check(call(c, workspace=workspace), want)
+    check(call(c, grads="weight", workspace=workspace), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,workspace", [(400, None), (5000, "least"), (9000, None)])
+def test_targets_that_repeat(rows, workspace, dtype):
+    """Half of the rows have one word, a quarter the last one, some words none."""
+    c = case(rows, 96, 2000, dtype, ignored=0.1)
+    at = torch.arange(rows, device="cuda")
+    c["target"][(at % 2 == 0) & (c["target"] >= 0)] = 1234
+    c["target"][(at % 4 == 1) & (c["target"] >= 0)] = 1999
+    check(call(c, workspace=workspace), expected(c))
