@@ -464,6 +464,7 @@ void build_index(const std::vector<uint64_t>& counts, std::vector<uint32_t>& fir
 struct pt_tensors {
   int dtype = PT_BF16, bits = 32;
   bool scaler = false;
+  int device = 0;
   uint64_t seed = 0;
   Index units{}, blocks{};
   uint32_t norm_grid = 0;
@@ -531,6 +532,7 @@ int create(pt_tensors* l, const pt_tensor* list, uint32_t n, const pt_scaler_cfg
   std::memcpy(host.data() + o_bc, bc.data(), bc.size() * 4);
   std::memcpy(host.data() + o_uf, uf.data(), uf.size() * 4);
   std::memcpy(host.data() + o_uc, uc.data(), uc.size() * 4);
+  PT_HIP(nullptr, hipGetDevice(&l->device));
   PT_HIP(nullptr, hipMalloc((void**)&l->mem, total));
   PT_HIP(nullptr, hipMemcpy(l->mem, host.data(), total, hipMemcpyHostToDevice));
   l->st = (ListState*)l->mem;
@@ -576,8 +578,13 @@ extern "C" int pt_tensors_create(pt_tensors** out, int dtype, const pt_tensor* l
 
 extern "C" int pt_tensors_destroy(pt_tensors* l) {
   if (!l) return PT_OK;
+  // its own device's work, whichever is current
+  int current = l->device;
+  (void)hipGetDevice(&current);
+  if (current != l->device) (void)hipSetDevice(l->device);
   (void)hipDeviceSynchronize();
   if (l->mem) (void)hipFree(l->mem);
+  if (current != l->device) (void)hipSetDevice(current);
   delete l;
   return PT_OK;
 }

@@ -1,0 +1,46 @@
+// What lists of tensors ask of the HIP runtime, on the stand-in for it (fake_hip.h).
+#include "fake_hip.h"
+#include "ptchunk.h"
+
+extern "C" hipError_t hipSetDevice(int d) {
+  fake::device = d;
+  fake::note(d ? "device 1" : "device 0");
+  return hipSuccess;
+}
+
+#define EXPECT(c) do { if (!(c)) { fprintf(stderr, "line %d: %s\n%s", __LINE__, #c, fake::text().c_str()); return 1; } } while (0)
+
+// A list belongs to the device that was current when it was made: that one's work is waited for before its memory goes, whichever is current then.
+static int destroyed_from_another_device() {
+  for (int own = 0; own < 2; ++own)
+    for (int current = 0; current < 2; ++current) {
+      fake::device = own;
+      pt_tensor t = {};
+      float* a = nullptr;
+      EXPECT(hipMalloc((void**)&a, 4096) == hipSuccess);
+      t.grad = a; t.master = a + 64; t.m = a + 128; t.v = a + 192; t.elems = 10;
+      pt_tensors* l = nullptr;
+      EXPECT(pt_tensors_create(&l, PT_BF16, &t, 1, 32, nullptr, 0) == PT_OK);
+      const size_t held = fake::memory.size();
+      fake::device = current;
+      const size_t from = fake::ops.size();
+      EXPECT(pt_tensors_destroy(l) == PT_OK);
+      EXPECT(fake::memory.size() == held - 1);
+      EXPECT(fake::device == current);                       // as the caller left it
+      int at = current;
+      bool waited = false;
+      for (size_t i = from; i < fake::ops.size(); ++i) {
+        const std::string& what = fake::ops[i].what;
+        if (what.rfind("device ", 0) == 0) at = what.back() - '0';
+        if (what == "sync device" && at == own) waited = true;
+      }
+      EXPECT(waited);
+    }
+  return 0;
+}
+
+int main() {
+  const int rc = destroyed_from_another_device();
+  if (rc == 0) puts("held");
+  return rc;
+}
