@@ -1,0 +1,22 @@
+"""What the helpers and entry points of the head's loss and of lists of tensors refuse before anything reaches a device, and where their limits lie."""
+import pytest
+import torch
+
+from paper_2406_08334_amd import binding as B
+from test_head_host import good
+
+
+def tensor8(grad_dtype=torch.bfloat16, param_dtype=torch.bfloat16):
+    f, c = torch.zeros(300), torch.zeros(300, dtype=torch.uint8)
+    return B.tensor(torch.zeros(300, dtype=grad_dtype), f, c, c.clone(), torch.zeros(300, dtype=param_dtype), m_scale=f[:2], v_scale=f[2:4])
+
+
+def test_states_of_one_width_are_no_list_of_the_other():
+    """Codes of a byte read and written as fp32 numbers would pass their arrays' ends."""
+    f = torch.zeros(300)
+    with pytest.raises(ValueError):
+        B.pt_tensors_create(B.PT_BF16, [tensor8()], 32)
+    with pytest.raises(ValueError):
+        B.pt_tensors_create(B.PT_BF16, [B.tensor(f, f, f, f)], 8)
+    with pytest.raises(ValueError):
+        B.pt_tensors_create(B.PT_BF16, [B.tensor(f, f, f, f), tensor8()], 32)
