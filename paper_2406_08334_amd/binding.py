@@ -505,14 +505,19 @@ def tensor(grad, master, m, v, param16=None, m_scale=None, v_scale=None, no_deca
     flags = (PT_TENSOR_NO_DECAY if no_decay else 0) | (PT_TENSOR_GRAD_F32 if grad.dtype == torch.float32 else 0)
     t = pt_tensor(_addr(grad), _addr(master), _addr(param16), _addr(m), _addr(v), _addr(m_scale), _addr(v_scale), n, flags, 0)
     t.state_bits = 8 * size
+    t.types = {x.dtype for x in (grad, param16) if x is not None}
     return t
 
 
 def pt_tensors_create(dtype: int, tensors, state_bits: int, scaler: pt_scaler_cfg | None = None, seed: int = 0):
     """tensors: list of `tensor(...)`; state_bits: 8 or 32, what their states have."""
-    for i, t in enumerate(tensors):
-        if getattr(t, "state_bits", state_bits) != state_bits:       # unknown of one that `tensor` has not made
+    import torch
+    other = {PT_BF16: torch.float16, PT_FP16: torch.bfloat16}.get(int(dtype))
+    for i, t in enumerate(tensors):                                  # neither is known of one that `tensor` has not made
+        if getattr(t, "state_bits", state_bits) != state_bits:
             raise ValueError(f"pt_tensors_create: the states of tensor {i} have {t.state_bits} bits, not {state_bits}")
+        if other in getattr(t, "types", ()):
+            raise ValueError(f"pt_tensors_create: tensor {i} has arrays of {other}, not of the list's type")
     arr = (pt_tensor * max(len(tensors), 1))(*tensors)
     out = C.c_void_p()
     _check(lib().pt_tensors_create(C.byref(out), int(dtype), arr, len(tensors), int(state_bits),

@@ -20,3 +20,11 @@ def test_states_of_one_width_are_no_list_of_the_other():
         B.pt_tensors_create(B.PT_BF16, [B.tensor(f, f, f, f)], 8)
     with pytest.raises(ValueError):
         B.pt_tensors_create(B.PT_BF16, [B.tensor(f, f, f, f), tensor8()], 32)
+
+
+@pytest.mark.parametrize("own,other", [((B.PT_BF16, torch.bfloat16), torch.float16), ((B.PT_FP16, torch.float16), torch.bfloat16)])
+def test_arrays_of_the_other_16_bit_type(own, other):
+    """Both have two bytes an element: read as the list's own they are other numbers."""
+    for types in ((other, other), (own[1], other), (other, own[1])):
+        with pytest.raises(ValueError):
+            B.pt_tensors_create(own[0], [tensor8(*types)], 8)
