@@ -583,7 +583,9 @@ def pt_head_workspace(head: pt_head):
 
 
 def pt_head_loss(head: pt_head, workspace, stream=None):
-    """workspace: a device tensor of pt_head_workspace(head) bytes."""
+    """workspace: a device tensor of pt_head_workspace(head) bytes, back to back."""
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("pt_head_loss: the workspace's elements are not back to back")
     rc = lib().pt_head_loss(C.byref(head), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                             _stream(stream))
     if rc:

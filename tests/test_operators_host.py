@@ -28,3 +28,11 @@ def test_arrays_of_the_other_16_bit_type(own, other):
     for types in ((other, other), (own[1], other), (other, own[1])):
         with pytest.raises(ValueError):
             B.pt_tensors_create(own[0], [tensor8(*types)], 8)
+
+
+@pytest.mark.parametrize("workspace", [torch.empty(1, dtype=torch.uint8).expand(1 << 24), torch.empty(1 << 16, 256, dtype=torch.uint8)[:, :128],
+                                       torch.empty(1 << 24, dtype=torch.uint8)[::2]])
+def test_a_workspace_with_gaps(workspace):
+    """Its elements say nothing about the bytes behind its address: one byte expanded to 16 MiB passed for 16 MiB."""
+    with pytest.raises(ValueError):
+        B.pt_head_loss(good(), workspace, 0)
