@@ -36,3 +36,20 @@ def test_a_workspace_with_gaps(workspace):
     """Its elements say nothing about the bytes behind its address: one byte expanded to 16 MiB passed for 16 MiB."""
     with pytest.raises(ValueError):
         B.pt_head_loss(good(), workspace, 0)
+
+
+@pytest.mark.parametrize("limit,beyond", [(dict(rows=1 << 25), dict(rows=(1 << 25) + 1)),
+                                          (dict(vocab=1 << 21), dict(vocab=(1 << 21) + 1)),
+                                          (dict(width=1 << 20, hidden_stride=1 << 20, weight_stride=1 << 20),
+                                           dict(width=(1 << 20) + 1, hidden_stride=1 << 21, weight_stride=1 << 21)),
+                                          (dict(weight_stride=1 << 21), dict(weight_stride=(1 << 21) + 1))])
+def test_the_limits_themselves(limit, beyond):
+    """As the header names them: the last that is taken, the first that is not."""
+    least, best = B.pt_head_workspace(good(**limit))
+    assert 0 < least <= best
+    for grads in (dict(d_hidden=0x10000, d_hidden_stride=1 << 21), dict(d_weight=0x20000, d_weight_stride=1 << 21)):
+        least, best = B.pt_head_workspace(good(**limit, **grads))
+        assert 0 < least <= best
+        with pytest.raises(B.PtError) as e:
+            B.pt_head_workspace(good(**beyond, **grads))
+        assert e.value.status == B.PT_ERR_UNSUPPORTED
