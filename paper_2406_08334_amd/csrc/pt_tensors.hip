@@ -469,7 +469,7 @@ struct pt_tensors {
   Index units{}, blocks{};
   uint32_t norm_grid = 0;
   bool open = false;                      // a norm has been taken that no update has used
-  double beta1 = 0.9, beta2 = 0.95;       // those the last norm was taken with
+  double beta1 = 0.9, beta2 = 0.95;       // those whose powers the device has
   double next_beta1 = 0.9, next_beta2 = 0.95;
   uint8_t* mem = nullptr;                 // everything below lies in it
   ListState* st = nullptr;
@@ -620,8 +620,8 @@ extern "C" int pt_tensors_adamw_step(pt_tensors* l, const pt_hparams* hp, void* 
   if (hp->beta1 != l->beta1 || hp->beta2 != l->beta2) {
     hipLaunchKernelGGL(k_list_betas, dim3(1), dim3(64), 0, (hipStream_t)stream, l->st, hp->beta1, hp->beta2);
     PT_LAUNCH_CHECK(nullptr, "k_list_betas");
-    l->next_beta1 = hp->beta1;
-    l->next_beta2 = hp->beta2;
+    l->beta1 = l->next_beta1 = hp->beta1;
+    l->beta2 = l->next_beta2 = hp->beta2;
   }
   const UpdateArgs a = {l->blocks, l->desc, l->st, hp->lr, hp->max_norm,
                         {float(hp->beta1), float(hp->beta2), float(1.0 - hp->beta1), float(1.0 - hp->beta2),

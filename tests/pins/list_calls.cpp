@@ -39,8 +39,37 @@ static int destroyed_from_another_device() {
   return 0;
 }
 
-int main() {
-  const int rc = destroyed_from_another_device();
+// The powers of beta are those of the update that is launched, also behind one with other betas whose launch has failed.
+static int betas_behind_an_update_that_failed() {
+  fake::device = 0;
+  float* a = nullptr;
+  EXPECT(hipMalloc((void**)&a, 4096) == hipSuccess);
+  pt_tensor t = {};
+  t.grad = a; t.master = a + 64; t.m = a + 128; t.v = a + 192; t.elems = 10;
+  pt_tensors* l = nullptr;
+  EXPECT(pt_tensors_create(&l, PT_BF16, &t, 1, 32, nullptr, 0) == PT_OK);
+  pt_hparams first = {1e-3, 0.9, 0.95, 1e-8, 0.0, 1.0}, other = first;
+  other.beta1 = 0.8;
+  EXPECT(pt_tensors_grad_sqnorm(l, nullptr) == PT_OK);       // with the first ones' powers
+  fake::fail_kernel = "k_list_adamw";
+  fake::fail_after = 0;
+  EXPECT(pt_tensors_adamw_step(l, &other, nullptr) == PT_ERR_HIP);
+  fake::fail_kernel = "";
+  EXPECT(fake::launches("k_list_betas").size() == 1);
+  EXPECT(pt_tensors_adamw_step(l, &first, nullptr) == PT_OK);
+  EXPECT(fake::launches("k_list_betas").size() == 2);        // theirs again
+  EXPECT(pt_tensors_grad_sqnorm(l, nullptr) == PT_OK);
+  EXPECT(pt_tensors_adamw_step(l, &first, nullptr) == PT_OK);
+  EXPECT(fake::launches("k_list_betas").size() == 2 && fake::launches("k_list_adamw").size() == 2);
+  EXPECT(pt_tensors_destroy(l) == PT_OK);
+  return 0;
+}
+
+int main(int argc, char** argv) {
+  const std::string check = argc == 2 ? argv[1] : "";
+  const int rc = check == "destroyed_from_another_device"        ? destroyed_from_another_device()
+                 : check == "betas_behind_an_update_that_failed" ? betas_behind_an_update_that_failed()
+                                                                 : 2;
   if (rc == 0) puts("held");
   return rc;
 }
