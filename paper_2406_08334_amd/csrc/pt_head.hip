@@ -62,8 +62,8 @@ constexpr uint32_t NO_TARGET = ~0u;
 // big: the largest scale.
 __device__ __forceinline__ Meta found_rows(uint32_t n, float big) {
   int e = 0;
-  if (big > 0.0f && big < 3.4e38f) (void)frexpf(big, &e);       // big < 2^e
-  e = max(-100, min(100, 14 - e));
+  if (big > 0.0f && big < __builtin_inff()) (void)frexpf(big, &e);       // big < 2^e, e up to 128
+  e = min(100, 14 - e);                                        // no less than -114: the power and 1 / it are numbers of normal size
   return {n, ldexpf(1.0f, e), ldexpf(1.0f, -e)};
 }
 

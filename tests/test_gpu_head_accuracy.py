@@ -126,3 +126,19 @@ def test_targets_that_repeat(rows, workspace, dtype):
     c["target"][(at % 2 == 0) & (c["target"] >= 0)] = 1234
     c["target"][(at % 4 == 1) & (c["target"] >= 0)] = 1999
     check(call(c, workspace=workspace), expected(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [40, 200])
+@pytest.mark.parametrize("big", [2.0 ** 120, 2.0 ** 127, 2.0 ** -120])
+def test_scales_at_the_ends_of_their_range(rows, big, dtype):
+    """Any finite scale: right where the results are in the type's range; where they are not, inf and no NaN, and zero where the weight or h is."""
+    c = case(rows, 64, 300, dtype)
+    c["scale"] = torch.full((rows,), big, device="cuda")
+    c["weight"][:, 5:9] = 0.0
+    c["hidden"][:, 5:9] = 0.0
+    loss, dh, dw = call(c)
+    assert not bool(dh.isnan().any()) and not bool(dw.isnan().any())
+    assert bool((dh[:, 5:9] == 0).all()) and bool((dw[:, 5:9] == 0).all())
+    if dtype == "bf16" and big < 2.0 ** 127:
+        check((loss, dh, dw), expected(c))
