@@ -12,8 +12,8 @@
 // vocabulary would take the first product twice, so the pieces are rows, of which as many are taken at a time as the workspace has room for.
 // The loss alone never stores a logit.
 //
-// 8192 rows, width 1600, vocabulary 50257, bf16: 3.8 ms, of which the products 3.45 (1.2, 1.15, 1.05; 3.95 TFLOP: 1150 TFLOP/s, where a large library
-// product reaches 1270 at this width) and soft 0.34; 6144 of 8192 rows, width 4096, vocabulary 32000: 3.95 ms, 1220 TFLOP/s.
+// 8192 rows, width 1600, vocabulary 50257, bf16: 3.7 - 3.8 ms, of which the products 3.4 (1.21, 1.14, 1.03; 3.95 TFLOP: 1160 TFLOP/s, where a large library
+// product reaches 1270 at this width) and soft 0.35; 6144 of 8192 rows, width 4096, vocabulary 32000: 3.85 - 4.0 ms, 1200 - 1250 TFLOP/s.
 #include "pt_common.h"
 #include "pt_mfma.h"
 #include "pt_update.h"
@@ -34,9 +34,9 @@ constexpr uint32_t PIECE_STEP = 256;       // pieces are multiples of this many 
 constexpr uint64_t PIECE_BEST = 8192, PIECE_BYTES = 1ull << 30, PIECE_MOST = 32768;
 constexpr float LOG2E = 1.44269504088896340736f;
 
-// What is kept of the logits of a piece.  bf16 inputs: exp(z - the largest of the wave's part of the row) as an fp16 number, 2^15 being 1: a rounding of 2^-12
-// ahead of G's own of 2^-9.  fp16 inputs, whose G is rounded by 2^-12 itself: z in fp32 (exponentials in fp16 would save a tenth of the time at most, but
-// make the gradients' error half as large again).
+// What is kept of the logits of a piece.  bf16 inputs: exp(z - the largest of the wave's part of the row) as an fp16 number, 2^15 being 1: a rounding of up to
+// 2^-11 ahead of G's own of up to 2^-8.  fp16 inputs, whose G is rounded by up to 2^-11 itself: z in fp32 (exponentials in fp16 would save a tenth of the
+// time at most, and round every word but the target twice by as much).
 template <int DT> constexpr bool KEEP_EXP = DT == PT_BF16;
 template <int DT> constexpr uint32_t KEPT_BYTES = KEEP_EXP<DT> ? 2 : 4;
 constexpr float ONE_EXP = 15.0f;

@@ -351,6 +351,7 @@ struct Block {
       const float bm = fminf(wave_max(fmaxf(fmaxf(__builtin_fabsf(m[0]), __builtin_fabsf(m[1])), fmaxf(__builtin_fabsf(m[2]), __builtin_fabsf(m[3])))),
                              3.402823466e38f);
       const float bv = fminf(wave_max(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]))), MOST_R);
+      // the reciprocal first, and the scale by a product: what an elementwise evaluation of top / largest and largest / top makes of them
       const bool hm = bm >= TINY8, hv = bv >= TINY8;
       const float im = hm ? 1.0f / bm * TOP8 : 0.0f, iv = hv ? 1.0f / bv * TOP8 : 0.0f;
       uint32_t z[4];
