@@ -518,6 +518,122 @@ int pt_head_workspace(const pt_head* head, uint64_t* least_bytes, uint64_t* best
  * Errors: text in pt_last_error(NULL). */
 int pt_head_loss(const pt_head* head, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* ---- layers before the head ------------------------------------------------------------------
+ * What lies between an embedding and the head's loss: a matrix product with what follows it, a normalisation, dropout, and rows in
+ * 8 bits.  Every call enqueues on `stream` only, allocates nothing and may be captured into a graph; the same call gives the same bits
+ * again; device arrays belong to the current device and to `stream`'s.  16-bit arrays need 2-byte alignment, fp32 ones 4-byte; rows may lie
+ * at any stride >= their width (elements).  No array that is written may overlap another one, but for what is said at a call.  Errors:
+ * text in pt_last_error(NULL).
+ *
+ * 8 BITS: rows of OCP e4m3 codes with one scale each; code times scale is the value, and a row's largest magnitude becomes 448.  A
+ * row whose largest is below 2^-100 becomes zero (scale 0); one that holds +-inf or NaN becomes NaN (codes and scale). */
+
+/* Dropout.  off = p in whole 65536ths (to the nearest, 65535 at most).  Element c of row r of an array of `width` is dropped if its 16
+ * bits are < off: bits 16 (c % 4) on of mix(key + (r ceil(width / 4) + c / 4 + 1) phi), key = mix(seed + step phi), mix being
+ * splitmix64's output function and phi 0x9E3779B97F4A7C15.  Others are multiplied by 65536 / (65536 - off).  No mask is stored: a gradient
+ * finds the same one by the same seed and step.  A dropped element adds nothing, whatever it holds. */
+typedef struct {
+  double p;              /* in [0, 1); 0: no dropout                                                  */
+  uint64_t seed;
+  const uint64_t* step;  /* device, read when a call runs (so a captured graph sees a new one); NULL: 0 */
+} pt_drop;
+
+typedef enum { PT_ACT_NONE = 0, PT_ACT_RELU = 1, PT_ACT_GELU = 2 /* by erf */, PT_ACT_GELU_TANH = 3, PT_ACT_SILU = 4 } pt_act;
+
+/* Matrix product with its epilogue.  With D dropout:
+ *     z_rn = sum_k x_rk W_nk + bias_n         pre = z        out = residual + D(act(z) gate)
+ * computed in fp32 from exact products, each output rounded once.  Gradients, from d_out, x, W, pre (as rounded) and gate:
+ *     e = D(d_out)    d_gate = e act(pre)    dz = e gate act'(pre)    d_bias = sum_r dz    d_x = dz W    d_weight = dz^T x
+ * dz is rounded to the 16-bit type between the products (d_bias is not of rounded ones); d_residual is d_out itself. */
+typedef struct {
+  const void* x;             /* device, [rows, width] 16-bit elements; with x_scale e4m3 codes            */
+  const void* weight;        /* device, [outs, width], as x                                               */
+  const float* x_scale;      /* device, [rows]; NULL: 16 bits                                             */
+  const float* weight_scale; /* device, [outs]; both scales or neither.  8 bits: no gradients             */
+  const void* bias;          /* device, [outs] 16-bit, or NULL                                            */
+  const void* gate;          /* device, [rows, outs], or NULL: 1                                          */
+  const void* residual;      /* device, [rows, outs], or NULL: 0.  May be `out` itself                    */
+  void* pre;                 /* device, [rows, outs]: written by pt_linear_out, read by pt_linear_grads (which needs it if there is an */
+                             /* activation or a gate); or NULL                                            */
+  void* out;                 /* device, [rows, outs], written by pt_linear_out                            */
+  const void* d_out;         /* device, [rows, outs]: the gradients' input, and what they are, each or NULL: */
+  void *d_x, *d_weight, *d_bias, *d_gate; /* [rows, width], [outs, width], [outs], [rows, outs]           */
+  uint64_t x_stride, weight_stride, gate_stride, residual_stride, pre_stride, out_stride, d_out_stride, d_x_stride, d_weight_stride,
+      d_gate_stride;
+  pt_drop drop;
+  uint32_t rows, outs, width;
+  int32_t dtype;             /* pt_dtype, of everything that is not in 8 bits                             */
+  int32_t act;               /* pt_act                                                                    */
+  int32_t reserved;
+} pt_linear;
+
+/* Bytes of workspace of the two calls (for arrays as they are given: operands that do not begin at multiples of 16 bytes, lie at odd strides
+ * or have widths that are no multiple of 64 are copied into it first); either pointer may be NULL.  Host only.  PT_ERR_UNSUPPORTED: more than
+ * 2^25 rows, 2^21 outs or a width over 2^20, or more than 2^30 tiles of 128 x 128 in a product. */
+int pt_linear_workspace(const pt_linear* layer, uint64_t* out_bytes, uint64_t* grads_bytes);
+
+/* workspace: device, 256-byte aligned, of at least those bytes (else PT_ERR_NOMEM); its contents are of no use afterwards; may be NULL where
+ * none are needed.  rows == 0: pt_linear_out does nothing, pt_linear_grads clears d_weight and d_bias. */
+int pt_linear_out(const pt_linear* layer, void* workspace, uint64_t workspace_bytes, void* stream);
+int pt_linear_grads(const pt_linear* layer, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* RMS norm with the residual's addition:
+ *     s = x + residual       sum = s in 16 bits       rstd = 1 / sqrt(mean_k s^2 + eps)       y = s rstd gain
+ * in fp32, s unrounded.  Gradients, from sum (x where there is no residual), rstd, gain, d_y and d_sum, the gradient that reaches the sum
+ * on its other ways:
+ *     t = d_y gain     d_x = d_sum + rstd (t - sum rstd^2 mean_k(t sum))  (x's and residual's)     d_gain_k = sum_r d_y sum rstd
+ * An output in 8 bits has the gradient of one in 16. */
+typedef struct {
+  const void* x;         /* device, [rows, width] 16-bit elements                                      */
+  const void* residual;  /* device, [rows, width], or NULL: 0                                          */
+  const void* gain;      /* device, [width] 16-bit, or NULL: 1                                         */
+  void* sum;             /* device, [rows, width], or NULL: not kept.  May be x or residual itself     */
+  float* rstd;           /* device, [rows], or NULL: not kept                                          */
+  void* y;               /* device, [rows, width] 16-bit, or with y_scale e4m3 codes                   */
+  float* y_scale;        /* device, [rows]; NULL: 16 bits                                              */
+  const void* d_y;       /* device, [rows, width] 16-bit                                               */
+  const void* d_sum;     /* device, [rows, width] 16-bit, or NULL: 0.  May be d_x itself               */
+  void* d_x;             /* device, [rows, width] 16-bit, or NULL                                      */
+  void* d_gain;          /* device, [width] 16-bit, or NULL                                            */
+  uint64_t x_stride, residual_stride, sum_stride, y_stride, d_y_stride, d_sum_stride, d_x_stride;
+  double eps;            /* >= 0                                                                       */
+  uint32_t rows, width;  /* width up to 32768                                                          */
+  int32_t dtype;         /* pt_dtype                                                                   */
+  int32_t reserved;
+} pt_rms;
+
+/* Bytes of workspace of pt_rms_grads (0 without d_gain).  Host only. */
+int pt_rms_workspace(const pt_rms* norm, uint64_t* grads_bytes);
+int pt_rms_norm(const pt_rms* norm, void* stream);
+/* workspace as for pt_linear_grads.  rows == 0 clears d_gain.  The sum that the gradients read is `sum` if that is given, else x. */
+int pt_rms_grads(const pt_rms* norm, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Rows to 8 bits. */
+#define PT_FP32 2            /* as pt_rows.type, beside pt_dtype's */
+typedef struct {
+  const void* x;             /* device, [rows, width]                    */
+  void* codes;               /* device, [rows, width] bytes, written     */
+  float* scale;              /* device, [rows], written                  */
+  uint64_t x_stride, codes_stride;
+  uint32_t rows, width;      /* width up to 32768                        */
+  int32_t type;              /* PT_BF16, PT_FP16 or PT_FP32              */
+  int32_t reserved;
+} pt_rows;
+int pt_rows8(const pt_rows* rows, void* stream);
+
+/* out = residual + D(x); the gradient of x is the same call on that of out, without a residual. */
+typedef struct {
+  const void* x;             /* device, [rows, width] 16-bit elements.  May be `out` itself  */
+  const void* residual;      /* device, [rows, width], or NULL: 0.  May be `out` itself      */
+  void* out;                 /* device, [rows, width], written                               */
+  uint64_t x_stride, residual_stride, out_stride;
+  pt_drop drop;
+  uint32_t rows, width;      /* rows times ceil(width / 8) up to 2^32 - 1                    */
+  int32_t dtype;
+  int32_t reserved;
+} pt_dropped;
+int pt_dropout(const pt_dropped* dropped, void* stream);
+
 /* ---- OPTIM-phase cost model (host only) -------------------------------------------------
  * The paper's runtime model restricted to the optimizer phase (Appendix A.1, Eq. 2: the part
  * that runs on the GPU and the part that does not run side by side, the longer one decides;

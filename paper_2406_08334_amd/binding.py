@@ -28,6 +28,7 @@ EXPORTS = [
     "pt_chunk_grad_sqnorm_noalloc", "pt_calib_adamw_pattern", "pt_stream_status",
     "pt_tensors_create", "pt_tensors_destroy", "pt_tensors_set_state", "pt_tensors_grad_sqnorm", "pt_tensors_adamw_step",
     "pt_tensors_report_read", "pt_head_workspace", "pt_head_loss",
+    "pt_linear_workspace", "pt_linear_out", "pt_linear_grads", "pt_rms_workspace", "pt_rms_norm", "pt_rms_grads", "pt_rows8", "pt_dropout",
 ]
 
 
@@ -79,6 +80,36 @@ class pt_head(C.Structure):
                 ("width", C.c_uint32), ("dtype", C.c_int32)]
 
 
+class pt_drop(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_void_p)]
+
+
+class pt_linear(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "weight", "x_scale", "weight_scale", "bias", "gate", "residual", "pre", "out", "d_out", "d_x", "d_weight",
+                                          "d_bias", "d_gate")] + \
+               [(n + "_stride", C.c_uint64) for n in ("x", "weight", "gate", "residual", "pre", "out", "d_out", "d_x", "d_weight", "d_gate")] + \
+               [("drop", pt_drop), ("rows", C.c_uint32), ("outs", C.c_uint32), ("width", C.c_uint32), ("dtype", C.c_int32), ("act", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class pt_rms(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "residual", "gain", "sum", "rstd", "y", "y_scale", "d_y", "d_sum", "d_x", "d_gain")] + \
+               [(n + "_stride", C.c_uint64) for n in ("x", "residual", "sum", "y", "d_y", "d_sum", "d_x")] + \
+               [("eps", C.c_double), ("rows", C.c_uint32), ("width", C.c_uint32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class pt_rows(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("codes", C.c_void_p), ("scale", C.c_void_p), ("x_stride", C.c_uint64), ("codes_stride", C.c_uint64),
+                ("rows", C.c_uint32), ("width", C.c_uint32), ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class pt_dropped(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p), ("x_stride", C.c_uint64), ("residual_stride", C.c_uint64),
+                ("out_stride", C.c_uint64), ("drop", pt_drop), ("rows", C.c_uint32), ("width", C.c_uint32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+PT_ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+PT_FP32 = 2
 PT_TENSOR_NO_DECAY, PT_TENSOR_GRAD_F32 = 1, 2
 PT_OPTIM_STREAM, PT_OPTIM_HOST = 0, 1
 
@@ -158,6 +189,13 @@ def lib():
         L.pt_tensors_report_read.argtypes = [vp, C.POINTER(pt_step_report), vp]
         L.pt_head_workspace.argtypes = [C.POINTER(pt_head), C.POINTER(u64), C.POINTER(u64)]
         L.pt_head_loss.argtypes = [C.POINTER(pt_head), vp, u64, vp]
+        L.pt_linear_workspace.argtypes = [C.POINTER(pt_linear), C.POINTER(u64), C.POINTER(u64)]
+        L.pt_linear_out.argtypes = L.pt_linear_grads.argtypes = [C.POINTER(pt_linear), vp, u64, vp]
+        L.pt_rms_workspace.argtypes = [C.POINTER(pt_rms), C.POINTER(u64)]
+        L.pt_rms_norm.argtypes = [C.POINTER(pt_rms), vp]
+        L.pt_rms_grads.argtypes = [C.POINTER(pt_rms), vp, u64, vp]
+        L.pt_rows8.argtypes = [C.POINTER(pt_rows), vp]
+        L.pt_dropout.argtypes = [C.POINTER(pt_dropped), vp]
         for name in EXPORTS:
             if name not in ("pt_version", "pt_status_string", "pt_last_error"):
                 getattr(L, name).restype = C.c_int
@@ -590,3 +628,164 @@ def pt_head_loss(head: pt_head, workspace, stream=None):
                             _stream(stream))
     if rc:
         _check(rc, "pt_head_loss")
+
+
+# ---- layers before the head -------------------------------------------------------------
+
+def _rows_of(who: str, arrays):
+    """arrays: (name, tensor or None, shape, dtype).  -> their strides; the elements of a row lie back to back, rows at any stride."""
+    strides = {}
+    for name, x, shape, dtype in arrays:
+        if x is None:
+            strides[name] = 0
+            continue
+        if x.dtype != dtype or tuple(x.shape) != shape or (x.stride(-1) != 1 and shape[-1] > 1):
+            raise ValueError(f"{who}: {name} is not {shape} of {dtype} with the elements of a row back to back")
+        strides[name] = max(x.stride(0), shape[1]) if len(shape) == 2 and shape[0] <= 1 else x.stride(0)
+    return strides
+
+
+def _type_of(who: str, x) -> int:
+    import torch
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"{who}: {x.dtype} is neither bfloat16 nor float16")
+    return PT_BF16 if x.dtype == torch.bfloat16 else PT_FP16
+
+
+def _codes(who: str, name: str, x):
+    """The array's own type, one of those that a byte of codes may have in torch."""
+    import torch
+    if x.dtype not in (torch.uint8, torch.float8_e4m3fn):
+        raise ValueError(f"{who}: {name} is neither uint8 nor float8_e4m3fn")
+    return x.dtype
+
+
+def _drop(who: str, p: float, seed: int, step) -> pt_drop:
+    import torch
+    if step is not None and not (step.dtype in (torch.int64, torch.uint64) and step.numel() == 1):
+        raise ValueError(f"{who}: step is not one 64-bit number")
+    return pt_drop(float(p), int(seed) & (2 ** 64 - 1), _addr(step))
+
+
+def _work(who: str, workspace):
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError(f"{who}: the workspace's elements are not back to back")
+    return _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def linear(x, weight, out=None, bias=None, gate=None, residual=None, pre=None, act: str = "none", drop: float = 0.0, seed: int = 0, step=None,
+           x_scale=None, weight_scale=None, d_out=None, d_x=None, d_weight=None, d_bias=None, d_gate=None) -> pt_linear:
+    """Describes a product with its epilogue from torch tensors: x [rows, width] and weight [outs, width] of one 16-bit type, or bytes of codes with
+    x_scale [rows] and weight_scale [outs] in fp32; out, gate, residual, pre, d_out, d_gate [rows, outs], bias, d_bias [outs], d_x and d_weight as what they
+    belong to, all of the 16-bit type.  step: one int64 on the device.  Rows may lie at any stride.  The caller keeps the tensors."""
+    import torch
+    rows, width = x.shape
+    outs = weight.shape[0]
+    if x_scale is not None or weight_scale is not None:
+        kinds = _codes("linear", "x", x), _codes("linear", "weight", weight)
+        first = next((t for t in (out, pre, residual, gate, bias) if t is not None), None)
+        dt = torch.bfloat16 if first is None else first.dtype
+    else:
+        kinds = x.dtype, x.dtype
+        dt = x.dtype
+    dtype = PT_BF16 if dt == torch.bfloat16 else PT_FP16
+    if dt not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"linear: {dt} is neither bfloat16 nor float16")
+    st = _rows_of("linear", [("x", x, (rows, width), kinds[0]), ("weight", weight, (outs, width), kinds[1])] +
+                  [(n, t, (rows, outs), dt) for n, t in (("gate", gate), ("residual", residual), ("pre", pre), ("out", out), ("d_out", d_out),
+                                                         ("d_gate", d_gate))] +
+                  [("d_x", d_x, (rows, width), dt), ("d_weight", d_weight, (outs, width), dt)])
+    _rows_of("linear", [("bias", bias, (outs,), dt), ("d_bias", d_bias, (outs,), dt), ("x_scale", x_scale, (rows,), torch.float32),
+                        ("weight_scale", weight_scale, (outs,), torch.float32)])
+    if act not in PT_ACT:
+        raise ValueError(f"linear: act is none of {', '.join(PT_ACT)}")
+    return pt_linear(_addr(x), _addr(weight), _addr(x_scale), _addr(weight_scale), _addr(bias), _addr(gate), _addr(residual), _addr(pre), _addr(out),
+                     _addr(d_out), _addr(d_x), _addr(d_weight), _addr(d_bias), _addr(d_gate),
+                     *(st[n] for n in ("x", "weight", "gate", "residual", "pre", "out", "d_out", "d_x", "d_weight", "d_gate")),
+                     _drop("linear", drop, seed, step), rows, outs, width, dtype, PT_ACT[act], 0)
+
+
+def pt_linear_workspace(layer: pt_linear):
+    """-> bytes of the workspace of (pt_linear_out, pt_linear_grads).  Host only."""
+    a, b = C.c_uint64(), C.c_uint64()
+    _check(lib().pt_linear_workspace(C.byref(layer), C.byref(a), C.byref(b)), "pt_linear_workspace")
+    return int(a.value), int(b.value)
+
+
+def pt_linear_out(layer: pt_linear, workspace=None, stream=None):
+    """workspace: a device tensor of pt_linear_workspace(layer)[0] bytes, back to back."""
+    rc = lib().pt_linear_out(C.byref(layer), *_work("pt_linear_out", workspace), _stream(stream))
+    if rc:
+        _check(rc, "pt_linear_out")
+
+
+def pt_linear_grads(layer: pt_linear, workspace=None, stream=None):
+    """workspace: a device tensor of pt_linear_workspace(layer)[1] bytes, back to back."""
+    rc = lib().pt_linear_grads(C.byref(layer), *_work("pt_linear_grads", workspace), _stream(stream))
+    if rc:
+        _check(rc, "pt_linear_grads")
+
+
+def rms(x, y=None, gain=None, residual=None, sum=None, rstd=None, y_scale=None, eps: float = 1e-5, d_y=None, d_sum=None, d_x=None, d_gain=None) -> pt_rms:
+    """Describes an RMS norm from torch tensors: x, residual, sum, y, d_y, d_sum, d_x [rows, width] and gain, d_gain [width] of one 16-bit type; with y_scale
+    [rows] in fp32 y has bytes of codes; rstd [rows] in fp32.  Rows may lie at any stride.  The caller keeps the tensors."""
+    import torch
+    rows, width = x.shape
+    dtype, dt = _type_of("rms", x), x.dtype
+    kind = dt if y_scale is None or y is None else _codes("rms", "y", y)
+    st = _rows_of("rms", [(n, t, (rows, width), k) for n, t, k in (("x", x, dt), ("residual", residual, dt), ("sum", sum, dt), ("y", y, kind), ("d_y", d_y, dt),
+                                                                   ("d_sum", d_sum, dt), ("d_x", d_x, dt))])
+    _rows_of("rms", [("gain", gain, (width,), dt), ("d_gain", d_gain, (width,), dt), ("rstd", rstd, (rows,), torch.float32),
+                     ("y_scale", y_scale, (rows,), torch.float32)])
+    return pt_rms(_addr(x), _addr(residual), _addr(gain), _addr(sum), _addr(rstd), _addr(y), _addr(y_scale), _addr(d_y), _addr(d_sum), _addr(d_x), _addr(d_gain),
+                  *(st[n] for n in ("x", "residual", "sum", "y", "d_y", "d_sum", "d_x")), float(eps), rows, width, dtype, 0)
+
+
+def pt_rms_workspace(norm: pt_rms) -> int:
+    """-> bytes of the workspace of pt_rms_grads.  Host only."""
+    a = C.c_uint64()
+    _check(lib().pt_rms_workspace(C.byref(norm), C.byref(a)), "pt_rms_workspace")
+    return int(a.value)
+
+
+def pt_rms_norm(norm: pt_rms, stream=None):
+    rc = lib().pt_rms_norm(C.byref(norm), _stream(stream))
+    if rc:
+        _check(rc, "pt_rms_norm")
+
+
+def pt_rms_grads(norm: pt_rms, workspace=None, stream=None):
+    """workspace: a device tensor of pt_rms_workspace(norm) bytes, back to back."""
+    rc = lib().pt_rms_grads(C.byref(norm), *_work("pt_rms_grads", workspace), _stream(stream))
+    if rc:
+        _check(rc, "pt_rms_grads")
+
+
+def rows8(x, codes, scale) -> pt_rows:
+    """Describes rows to be laid out in 8 bits: x [rows, width] bfloat16, float16 or float32, codes [rows, width] in bytes, scale [rows] fp32."""
+    import torch
+    rows, width = x.shape
+    dtype = PT_FP32 if x.dtype == torch.float32 else _type_of("rows8", x)
+    st = _rows_of("rows8", [("x", x, (rows, width), x.dtype), ("codes", codes, (rows, width), _codes("rows8", "codes", codes))])
+    _rows_of("rows8", [("scale", scale, (rows,), torch.float32)])
+    return pt_rows(_addr(x), _addr(codes), _addr(scale), st["x"], st["codes"], rows, width, dtype, 0)
+
+
+def pt_rows8(rows: pt_rows, stream=None):
+    rc = lib().pt_rows8(C.byref(rows), _stream(stream))
+    if rc:
+        _check(rc, "pt_rows8")
+
+
+def dropout(x, out, p: float, seed: int, step=None, residual=None) -> pt_dropped:
+    """Describes out = residual + D(x) from torch tensors [rows, width] of one 16-bit type; step: one int64 on the device, or None."""
+    rows, width = x.shape
+    dtype = _type_of("dropout", x)
+    st = _rows_of("dropout", [(n, t, (rows, width), x.dtype) for n, t in (("x", x), ("residual", residual), ("out", out))])
+    return pt_dropped(_addr(x), _addr(residual), _addr(out), st["x"], st["residual"], st["out"], _drop("dropout", p, seed, step), rows, width, dtype, 0)
+
+
+def pt_dropout(dropped: pt_dropped, stream=None):
+    rc = lib().pt_dropout(C.byref(dropped), _stream(stream))
+    if rc:
+        _check(rc, "pt_dropout")

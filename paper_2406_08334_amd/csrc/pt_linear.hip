@@ -1,0 +1,586 @@
+// Matrix product with bias, activation, gate, dropout and residual in its epilogue, and its gradients.
+//
+//   out       z = x W^T + bias, out = residual + D(act(z) gate), z in 16 bits if it is to be kept: one product, the rest on its sums in registers
+//   slope     dz = D(d_out) gate act'(pre) in 16 bits, d_gate, and sums of dz's columns for the bias
+//   d_x       = dz W,  d_weight = dz^T x
+//
+#include "pt_random.h"
+#include "pt_rows.h"
+
+using namespace pt_rows_ops;
+
+namespace {
+
+// ---- activations ------------------------------------------------------------------------------------------
+
+constexpr float LOG2E = 1.44269504088896340736f, TANH_2A = 1.59576912160573071176f, TANH_B = 0.044715f;       // 2 sqrt(2 / pi)
+
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -LOG2E)); }
+
+// The normal distribution's function, and exp(-z^2 / 2).  Of |z| sqrt(1/2) = u, with t = 1 / (1 + 7/16 u): erfc(u) / 2 = t P(t) exp(-u^2), P of degree seven
+// fitted to erfcx over u up to 14 (relative error 1.7e-7); in fp32 2^-19 of the result up to |z| = 5, 2^-18 up to 9.
+__device__ __forceinline__ float normal(float z, float& e) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.30935921676911455f, 1.0f));
+  float p = 0.03591368817931173f;
+  for (float c : {-0.14291292135087455f, 0.15869404565010323f, -0.017569269200825362f, 0.11137608263966191f, 0.10724730147205802f, 0.12385262848412495f,
+                  0.1233984909969888f})
+    p = __builtin_fmaf(p, t, c);
+  e = __builtin_amdgcn_exp2f((z * z) * (-0.5f * LOG2E));
+  const float q = p * t * e;
+  return z < 0.0f ? q : 1.0f - q;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act(float z) {
+  if constexpr (ACT == PT_ACT_RELU) return z < 0.0f ? 0.0f : z;
+  else if constexpr (ACT == PT_ACT_SILU) return z * sigmoid(z);
+  else if constexpr (ACT == PT_ACT_GELU_TANH) return z * sigmoid(TANH_2A * __builtin_fmaf(TANH_B * z, z * z, z));     // (1 + tanh(u)) / 2 = sigmoid(2 u)
+  else if constexpr (ACT == PT_ACT_GELU) { float e; return z * normal(z, e); }
+  else return z;
+}
+// act(z) and its derivative, which beyond 32 is 0 or 1 (its terms there would be products of 0 and inf).
+template <int ACT>
+__device__ __forceinline__ float act(float z, float& slope) {
+  const float y = act<ACT>(z), c = z < -32.0f ? -32.0f : z > 32.0f ? 32.0f : z;
+  if constexpr (ACT == PT_ACT_RELU) slope = z > 0.0f ? 1.0f : 0.0f;
+  else if constexpr (ACT == PT_ACT_SILU) { const float f = sigmoid(c); slope = f * __builtin_fmaf(c, 1.0f - f, 1.0f); }
+  else if constexpr (ACT == PT_ACT_GELU_TANH) {
+    const float f = sigmoid(TANH_2A * __builtin_fmaf(TANH_B * c, c * c, c));
+    slope = __builtin_fmaf(c * f * (1.0f - f), TANH_2A * __builtin_fmaf(3.0f * TANH_B * c, c, 1.0f), f);
+  } else if constexpr (ACT == PT_ACT_GELU) {
+    float e;
+    const float f = normal(c, e);
+    slope = __builtin_fmaf(c * 0.39894228040143267794f, e, f);
+  } else slope = 1.0f;
+  return y;
+}
+
+// f: called with the activation as a constant.
+template <class F> __host__ __device__ __forceinline__ auto with_act(int a, F&& f) {
+  switch (a) {
+    case PT_ACT_RELU: return f(std::integral_constant<int, PT_ACT_RELU>{});
+    case PT_ACT_GELU: return f(std::integral_constant<int, PT_ACT_GELU>{});
+    case PT_ACT_GELU_TANH: return f(std::integral_constant<int, PT_ACT_GELU_TANH>{});
+    case PT_ACT_SILU: return f(std::integral_constant<int, PT_ACT_SILU>{});
+    default: return f(std::integral_constant<int, PT_ACT_NONE>{});
+  }
+}
+
+// ---- epilogues ---------------------------------------------------------------------------------------------
+
+// Results in 16 bits as they are.  m: of the row's elements, n: rows.
+struct Plain {
+  uint16_t* out;
+  uint64_t stride;
+  uint32_t extent_m, extent_n;
+
+  template <int DT, class T>
+  __device__ __forceinline__ void tile(const T& t, uint32_t m0, uint32_t n0, lds_char*, lds_char*) const {
+    const uint32_t lane = threadIdx.x & 63, mw = m0 + t.wave_m();
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      const uint32_t n = n0 + t.wave_n() + j * 16 + (lane & 15);
+      const bool live = n < extent_n;
+      PT_GLOBAL uint16_t* row = (PT_GLOBAL uint16_t*)out + (live ? n : 0) * stride;
+#pragma unroll
+      for (int i = 0; i < T::FM; i += 2) {
+        const u32x4 x = eight(encode16x4<DT>(t.acc[i][j]), encode16x4<DT>(t.acc[i + 1][j]));       // lanes without a row take part in the exchange
+        if (live) store8(row, mw + i * 16 + eight_at(), extent_m, x);
+      }
+    }
+  }
+  template <int DT>
+  __device__ __forceinline__ void four(uint32_t m, uint32_t n, f32x4 x) const {
+    if (n < extent_n && m < extent_m) store4((PT_GLOBAL uint16_t*)out + n * stride, m, extent_m, encode16x4<DT>(x));
+  }
+};
+
+// m: outs, n: rows.
+struct Layer {
+  const uint16_t *bias, *gate, *residual;
+  uint16_t *pre, *out;
+  const float *x_scale, *weight_scale;
+  uint64_t gate_stride, residual_stride, pre_stride, out_stride;
+  uint32_t extent_m, extent_n;
+  int act;
+  pt_random::Drop drop;
+  uint64_t words;            // of random numbers in a row
+
+  // z of outs m on of row n, from their sums.
+  template <int DT, int N>
+  __device__ __forceinline__ void z_of(float (&x)[N], uint32_t m, uint32_t n) const {
+    if (x_scale) {
+      const float s = ((const PT_GLOBAL float*)x_scale)[n];
+#pragma unroll
+      for (int q = 0; q < N; ++q) x[q] = x[q] * s * ((const PT_GLOBAL float*)weight_scale)[min(m + q, extent_m - 1)];
+    }
+    if (bias) {
+#pragma unroll
+      for (int q = 0; q < N; q += 4) {
+        const f32x4 b = decode4<DT>(load4((const PT_GLOBAL uint16_t*)bias, m + q, extent_m));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[q + i] += b[i];
+      }
+    }
+  }
+  // From there to the result; g, r: gate and residual.
+  template <int N>
+  __device__ __forceinline__ void result(float (&y)[N], uint64_t key, uint32_t m, uint32_t n, const float (&g)[N], const float (&r)[N]) const {
+    with_act(act, [&](auto a) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) y[q] = ::act<a()>(y[q]);
+    });
+    if (gate) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) y[q] *= g[q];
+    }
+    if (drop.off) {
+#pragma unroll
+      for (int q = 0; q < N; q += 4) {
+        const f32x4 k = drop.of(key, n * words + (m + q) / 4, f32x4{y[q], y[q + 1], y[q + 2], y[q + 3]});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[q + i] = k[i];
+      }
+    }
+    if (residual) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) y[q] += r[q];
+    }
+  }
+
+  // A wave's sums go through LDS, 16 rows at a time, so that a lane has eight outs of a row, the lanes of a row all that the wave has of it, and what is loaded
+  // and stored is whole lines; in a loop, as four times five activations of 128 sums a lane would not fit the instruction cache.  What is loaded for a
+  // turn is under way during the one before.  The wave's own part of the buffers: 16 bytes of piece c of row n at c ^ n.
+  template <int DT, class T>
+  __device__ __forceinline__ void tile(const T& t, uint32_t m0, uint32_t n0, lds_char* even, lds_char* odd) const {
+    constexpr uint32_t TM = T::TM, ROW = TM * 4, LANES = TM / 8, STEP = 64 / LANES, TURNS = 16 / STEP, WAVES = T::THREADS / 64;
+    static_assert(TM >= 32 && (WAVES + 1) / 2 * 16 * ROW <= T::BYTES, "the waves' parts fit the buffers");
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15;
+    lds_char* own = (wave & 1 ? odd : even) + (wave >> 1) * (16 * ROW);
+    const uint32_t r = lane / LANES, c = lane % LANES, m = m0 + t.wave_m() + c * 8, first = n0 + t.wave_n();
+    const uint64_t key = drop.key();
+    u32x4 qg = {0, 0, 0, 0}, qr = qg;
+    const auto fetch = [&](uint32_t turn) {                // turns of all fragments, one after the other
+      const uint32_t n = min(first + turn * STEP + r, extent_n - 1);
+      if (gate) qg = fetch8((const PT_GLOBAL uint16_t*)gate + n * gate_stride, m, extent_m);
+      if (residual) qr = fetch8((const PT_GLOBAL uint16_t*)residual + n * residual_stride, m, extent_m);
+    };
+    __syncthreads();                                       // every wave has read its last operands
+    fetch(0);
+#pragma unroll 1
+    for (uint32_t j = 0; j < uint32_t(T::FN); ++j) {
+#pragma unroll
+      for (int k = 0; k < T::FN; ++k)
+        if (j == uint32_t(k))
+#pragma unroll
+          for (int i = 0; i < T::FM; ++i) *(lds_f32x4*)(own + l * ROW + ((i * 4 + (lane >> 4)) ^ (l & (TM / 4 - 1))) * 16) = t.acc[i][k];
+#pragma unroll 1
+      for (uint32_t turn = 0; turn < TURNS; ++turn) {
+        const uint32_t row = turn * STEP + r, n = first + j * 16 + row;
+        const u32x4 now_g = qg, now_r = qr;
+        if (j * TURNS + turn + 1 < T::FN * TURNS) fetch(j * TURNS + turn + 1);
+        const f32x4 lo = *(lds_f32x4*)(own + row * ROW + ((c * 2) ^ (row & (TM / 4 - 1))) * 16);
+        const f32x4 hi = *(lds_f32x4*)(own + row * ROW + ((c * 2 + 1) ^ (row & (TM / 4 - 1))) * 16);
+        if (n >= extent_n || m >= extent_m) continue;
+        float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, g[8], b[8];
+        z_of<DT>(y, m, n);
+        if (pre) store8((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode8<DT>(y));
+        decode8<DT>(place8(now_g, m, extent_m), g);
+        decode8<DT>(place8(now_r, m, extent_m), b);
+        result(y, key, m, n, g, b);
+        store8((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode8<DT>(y));
+      }
+    }
+  }
+  template <int DT>
+  __device__ __forceinline__ void four(uint32_t m, uint32_t n, f32x4 x) const {
+    if (n >= extent_n || m >= extent_m) return;
+    float y[4] = {x[0], x[1], x[2], x[3]}, g[4] = {}, r[4] = {};
+    const auto get = [&](const uint16_t* from, uint64_t stride, float (&to)[4]) {
+      const f32x4 b = decode4<DT>(load4((const PT_GLOBAL uint16_t*)from + n * stride, m, extent_m));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] = b[i];
+    };
+    if (gate) get(gate, gate_stride, g);
+    if (residual) get(residual, residual_stride, r);
+    z_of<DT>(y, m, n);
+    if (pre) store4((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
+    result(y, drop.key(), m, n, g, r);
+    store4((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
+  }
+};
+
+// ---- products ------------------------------------------------------------------------------------------------
+
+struct ProductArgs {
+  Operand p, q;
+  uint32_t extent_m, extent_n, twos;
+  float* sums;
+  Split split;
+};
+
+// MUL: PT_BF16, PT_FP16 or PT_E4M3, what is multiplied; DT: what the epilogue reads and writes.
+template <int MUL, int DT, class C, bool PK, bool QK, class E>
+__global__ void __launch_bounds__(C::THREADS) k_linear_product(const ProductArgs a, const E e) {
+  constexpr int BYTES = C::template Of<MUL, PK, QK>::BYTES;
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+  uint32_t tm, tn, part;
+  PT_GLOBAL float* left;
+  if (!part_of<C>(a.split, blockIdx.x, (a.extent_m + C::BM - 1) / C::BM, (a.extent_n + C::BN - 1) / C::BN, a.sums, tm, tn, part, left)) return;
+  const uint32_t t0 = left ? uint32_t(uint64_t(a.twos) * part / a.split.n) : 0, t1 = left ? uint32_t(uint64_t(a.twos) * (part + 1) / a.split.n) : a.twos;
+  with_tile<MUL, C, PK, QK>(a.extent_m - tm * C::BM, [&](auto t) {
+    typedef decltype(t) T;
+    t.run((lds_char*)even, (lds_char*)odd, a.p, a.q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+    if (left) {
+#pragma unroll
+      for (int j = 0; j < T::FN; ++j) leave<C>(t, j, left);
+      return;
+    }
+    e.template tile<DT>(t, tm * C::BM, tn * C::BN, (lds_char*)even, (lds_char*)odd);
+  });
+}
+
+template <int DT, class C, class E>
+__global__ void __launch_bounds__(256) k_linear_join(const ProductArgs a, const E e) {
+  join_tiles<C>(a.sums, a.split, (a.extent_m + C::BM - 1) / C::BM, (a.extent_n + C::BN - 1) / C::BN,
+                [&](uint32_t m, uint32_t n, f32x4 x) { e.template four<DT>(m, n, x); });
+}
+
+// Rows of 16-bit words (or bytes) whose beginnings, distances or ends the products cannot take: they load 16 bytes a lane past registers.
+__global__ void __launch_bounds__(256) k_linear_copy(const uint16_t* __restrict__ from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch,
+                                                     uint16_t* __restrict__ to) {
+  const uint32_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  if (r >= rows) return;
+  const PT_GLOBAL uint16_t* row = (const PT_GLOBAL uint16_t*)from + r * stride;
+  PT_GLOBAL uint16_t* dst = (PT_GLOBAL uint16_t*)to + size_t(r) * pitch;
+#pragma unroll 4
+  for (uint32_t c = lane * 8; c < pitch; c += 512) *(PT_GLOBAL u32x4*)(dst + c) = load8(row, c, width);
+}
+__global__ void __launch_bounds__(256) k_linear_copy8(const uint8_t* __restrict__ from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch,
+                                                      uint8_t* __restrict__ to) {
+  const uint32_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  if (r >= rows) return;
+  const PT_GLOBAL uint8_t* row = (const PT_GLOBAL uint8_t*)from + r * stride;
+  PT_GLOBAL uint8_t* dst = (PT_GLOBAL uint8_t*)to + size_t(r) * pitch;
+#pragma unroll 4
+  for (uint32_t c = lane * 16; c < pitch; c += 1024) {
+    u32x4 q = {0, 0, 0, 0};
+    if (c + 16 <= width) q = *(const PT_GLOBAL u32x4_b*)(row + c);
+    else
+#pragma unroll
+      for (uint32_t j = 0; j < 16; ++j)
+        if (c + j < width) q[j / 4] |= uint32_t(row[c + j]) << (8 * (j & 3));
+    *(PT_GLOBAL u32x4*)(dst + c) = q;
+  }
+}
+
+// ---- slope ---------------------------------------------------------------------------------------------------
+
+struct SlopeArgs {
+  const uint16_t *d_out, *pre, *gate;
+  uint16_t *dz, *d_gate;     // dz: rows of `pitch`, zero behind outs; or NULL: it is d_out
+  float* part;               // [gridDim.y][pitch]: sums of the columns, or NULL
+  uint64_t d_out_stride, pre_stride, gate_stride, d_gate_stride;
+  pt_random::Drop drop;
+  uint64_t words;
+  uint32_t rows, outs, pitch, rows_each;
+  int act;
+};
+
+// 512 columns, eight a lane, of rows_each rows, a quarter of which is a wave's.  Bound by memory.
+template <int DT>
+__global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a) {
+  __shared__ float s_part[4][512];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = blockIdx.x * 512 + lane * 8;
+  const uint32_t first = blockIdx.y * a.rows_each, end = min(a.rows, first + a.rows_each);
+  const uint64_t key = a.drop.key();
+  float sum[8] = {};
+  if (c < a.pitch)
+    with_act(a.act, [&](auto act) {
+      for (uint32_t r = first + wave; r < end; r += 4) {
+        u32x4 qe = {0, 0, 0, 0}, qz = qe, qg = qe;
+        qe = fetch8((const PT_GLOBAL uint16_t*)a.d_out + r * a.d_out_stride, c, a.outs);
+        if (a.pre) qz = fetch8((const PT_GLOBAL uint16_t*)a.pre + r * a.pre_stride, c, a.outs);
+        if (a.gate) qg = fetch8((const PT_GLOBAL uint16_t*)a.gate + r * a.gate_stride, c, a.outs);
+        float e[8], z[8], g[8], slope[8];
+        decode8<DT>(place8(qe, c, a.outs), e);
+        if (a.drop.off) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const pt_random::f32x4 q = a.drop.of(key, r * a.words + c / 4 + h, pt_random::f32x4{e[4 * h], e[4 * h + 1], e[4 * h + 2], e[4 * h + 3]});
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[4 * h + j] = q[j];
+          }
+        }
+        if (a.pre) {
+          decode8<DT>(place8(qz, c, a.outs), z);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[j] = ::act<act()>(z[j], slope[j]);
+          if (a.d_gate) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] *= e[j];
+            store8((PT_GLOBAL uint16_t*)a.d_gate + r * a.d_gate_stride, c, a.outs, encode8<DT>(z));
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] *= slope[j];
+        }
+        if (a.gate) {
+          decode8<DT>(place8(qg, c, a.outs), g);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] *= g[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (c + j >= a.outs) e[j] = 0.0f;
+          sum[j] += e[j];
+        }
+        if (a.dz) *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.dz + size_t(r) * a.pitch + c) = encode8<DT>(e);
+      }
+    });
+  if (!a.part) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s_part[wave][lane * 8 + j] = sum[j];
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < 512; i += 256) {
+    const uint32_t col = blockIdx.x * 512 + i;
+    if (col < a.pitch) ((PT_GLOBAL float*)a.part)[size_t(blockIdx.y) * a.pitch + col] = ((s_part[0][i] + s_part[1][i]) + s_part[2][i]) + s_part[3][i];
+  }
+}
+
+__global__ void __launch_bounds__(256) k_linear_zero(uint16_t* __restrict__ out, uint64_t stride, uint32_t width) {
+  for (uint32_t c = threadIdx.x; c < width; c += 256) out[blockIdx.x * stride + c] = 0;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+enum Kind { BIG, MID, FEW };
+struct Choice { Kind kind; Split split; uint64_t bytes; };
+
+// Which tiles a product of m x n is soonest done in (of Big's the last of m may be a narrower one), and how they are split.
+Choice choose(uint32_t m, uint32_t n, uint32_t twos) {
+  const auto of = [&](auto c, Kind kind) {
+    typedef decltype(c) C;
+    const Split s = split<C>((m + C::BM - 1) / C::BM * ((n + C::BN - 1) / C::BN), twos);
+    return Choice{kind, s, 4ull * s.tail * s.n * C::BM * C::BN};
+  };
+  if (n <= uint32_t(Few::BN)) return of(Few{}, FEW);
+  const Choice big = of(Big{}, BIG), mid = of(Mid{}, MID);
+  const uint32_t left = m % 256, tenths = m / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
+  return mid.split.ns < big.split.ns * tenths / ((m + 255) / 256 * 10) ? mid : big;
+}
+
+bool direct(const void* at, uint64_t stride, uint32_t width, uint32_t bytes) {
+  return uint64_t(width) * bytes % 128 == 0 && stride * bytes % 16 == 0 && (uintptr_t)at % 16 == 0 && stride <= (1u << 21);
+}
+
+// Where everything lies in the workspace.
+struct Plan {
+  bool x_direct, w_direct, slope;          // slope: dz is not d_out
+  uint32_t Kd, Np;                         // width and outs rounded up to whole steps (Kd in 16-bit words)
+  Choice c, c_x, c_w;
+  uint32_t rows_each, row_blocks;
+  uint64_t x, w, dz, part, sums, total;
+};
+
+bool in8(const pt_linear& l) { return l.x_scale != nullptr; }
+
+struct Taker {
+  uint64_t at = 0;
+  uint64_t operator()(uint64_t bytes) { const uint64_t x = at; at += up(bytes, 256); return x; }
+};
+
+Plan plan_out(const pt_linear& l) {
+  Plan p{};
+  const uint32_t bytes = in8(l) ? 1 : 2;
+  Taker take;
+  p.Kd = uint32_t(up(uint64_t(l.width) * bytes, 2 * TWO) / 2);
+  p.x_direct = direct(l.x, l.x_stride, l.width, bytes);
+  p.w_direct = direct(l.weight, l.weight_stride, l.width, bytes);
+  p.c = choose(l.outs, l.rows, p.Kd / TWO);
+  p.x = take(p.x_direct ? 0 : 2ull * l.rows * p.Kd);
+  p.w = take(p.w_direct ? 0 : 2ull * l.outs * p.Kd);
+  p.sums = take(p.c.bytes);
+  p.total = take.at;
+  return p;
+}
+
+Plan plan_grads(const pt_linear& l) {
+  Plan p{};
+  Taker take;
+  p.Kd = uint32_t(up(l.width, TWO));
+  p.Np = uint32_t(up(l.outs, TWO));
+  p.x_direct = !l.d_weight || direct(l.x, l.x_stride, l.width, 2);
+  p.w_direct = !l.d_x || direct(l.weight, l.weight_stride, l.width, 2);
+  p.slope = l.act != PT_ACT_NONE || l.gate || l.drop.p > 0.0 || !direct(l.d_out, l.d_out_stride, l.outs, 2);
+  p.x = take(p.x_direct ? 0 : 2ull * l.rows * p.Kd);
+  p.w = take(p.w_direct ? 0 : 2ull * l.outs * p.Kd);
+  p.dz = take(p.slope ? 2ull * l.rows * p.Np : 0);
+  const uint32_t strips = (p.Np + 511) / 512;
+  p.rows_each = std::max(16u, std::min(256u, uint32_t(uint64_t(l.rows) * strips / 2048)));
+  p.rows_each = std::max(p.rows_each, (l.rows + 65534) / 65535);
+  p.row_blocks = (l.rows + p.rows_each - 1) / p.rows_each;
+  p.part = take(l.d_bias ? 4ull * p.row_blocks * p.Np : 0);
+  if (l.d_x) p.c_x = choose(l.width, l.rows, p.Np / TWO);
+  if (l.d_weight) p.c_w = choose(l.width, l.outs, (l.rows + TWO - 1) / TWO);
+  p.sums = take(std::max(p.c_x.bytes, p.c_w.bytes));
+  p.total = take.at;
+  return p;
+}
+
+int check(const pt_linear* l, const char* who) {
+  if (!l) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: layer is NULL", who);
+  if (l->dtype != PT_BF16 && l->dtype != PT_FP16) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: dtype %d is neither PT_BF16 nor PT_FP16", who, l->dtype);
+  if (l->act < PT_ACT_NONE || l->act > PT_ACT_SILU) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: act %d is none of pt_act", who, l->act);
+  if (!l->outs || !l->width) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: outs and width must be > 0", who);
+  if (!pt_random::valid(l->drop)) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: the dropout's p is not in [0, 1)", who);
+  if (!l->x_scale != !l->weight_scale) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: scales of one operand only", who);
+  const struct { const void* at; uint64_t stride; uint32_t width; } rows[] = {
+    {l->x, l->x_stride, l->width}, {l->weight, l->weight_stride, l->width}, {l->gate, l->gate_stride, l->outs}, {l->residual, l->residual_stride, l->outs},
+    {l->pre, l->pre_stride, l->outs}, {l->out, l->out_stride, l->outs}, {l->d_out, l->d_out_stride, l->outs}, {l->d_x, l->d_x_stride, l->width},
+    {l->d_weight, l->d_weight_stride, l->width}, {l->d_gate, l->d_gate_stride, l->outs}};
+  for (const auto& x : rows)
+    if (x.at && x.stride < x.width) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: rows of width %u at a smaller stride", who, x.width);
+  uintptr_t a = (uintptr_t)l->bias | (uintptr_t)l->gate | (uintptr_t)l->residual | (uintptr_t)l->pre | (uintptr_t)l->out | (uintptr_t)l->d_out |
+                (uintptr_t)l->d_x | (uintptr_t)l->d_weight | (uintptr_t)l->d_bias | (uintptr_t)l->d_gate;
+  if (!l->x_scale) a |= (uintptr_t)l->x | (uintptr_t)l->weight;
+  if (a % 2 != 0 || ((uintptr_t)l->x_scale | (uintptr_t)l->weight_scale) % 4 != 0 || (uintptr_t)l->drop.step % 8 != 0)
+    return pt_fail(nullptr, PT_ERR_ALIGNMENT, "%s: an array is not aligned to its elements", who);
+  const auto tiles = [](uint64_t m, uint64_t n) { return ((m + 127) / 128) * ((n + 63) / 64); };
+  if (l->rows > (1u << 25) || l->outs > (1u << 21) || l->width > (1u << 20) ||
+      std::max({tiles(l->outs, l->rows), tiles(l->width, l->rows), tiles(l->width, l->outs)}) > (1u << 30))
+    return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: more than 2^25 rows, 2^21 outs, a width over 2^20 or too many tiles", who);
+  return PT_OK;
+}
+int check_workspace(uint64_t need, const void* workspace, uint64_t bytes, const char* who) {
+  if (!need) return PT_OK;
+  if (!workspace) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: workspace is NULL", who);
+  if ((uintptr_t)workspace % 256 != 0) return pt_fail(nullptr, PT_ERR_ALIGNMENT, "%s: the workspace is not 256-byte aligned", who);
+  if (need > bytes)
+    return pt_fail(nullptr, PT_ERR_NOMEM, "%s: a workspace of %llu bytes is too small (pt_linear_workspace)", who, (unsigned long long)bytes);
+  return PT_OK;
+}
+
+// Launches.
+template <int MUL, int DT, class C, bool PK, bool QK, class E> int product_of(const ProductArgs& a, const E& e, hipStream_t st) {
+  hipLaunchKernelGGL((k_linear_product<MUL, DT, C, PK, QK, E>), dim3(split_grid(a.split)), dim3(C::THREADS), 0, st, a, e);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_product");
+  if (!a.split.tail) return PT_OK;
+  hipLaunchKernelGGL((k_linear_join<DT, C, E>), dim3(joiners<C>(a.split.tail)), dim3(256), 0, st, a, e);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_join");
+  return PT_OK;
+}
+template <int MUL, int DT, bool PK, bool QK, class E> int product(Kind k, const ProductArgs& a, const E& e, hipStream_t st) {
+  return k == FEW ? product_of<MUL, DT, Few, PK, QK>(a, e, st) : k == MID ? product_of<MUL, DT, Mid, PK, QK>(a, e, st) : product_of<MUL, DT, Big, PK, QK>(a, e, st);
+}
+
+// The operand of rows as they lie, or as they have been copied.
+Operand rows_of(bool as_is, const void* at, uint64_t stride, uint32_t width, const void* copy, uint32_t pitch, uint32_t rows) {
+  return as_is ? Operand{at, stride * 2, rows, width} : Operand{copy, 2ull * pitch, rows, pitch};
+}
+int copy(const void* from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch, void* to, hipStream_t st) {
+  hipLaunchKernelGGL(k_linear_copy, dim3((rows + 3) / 4), dim3(256), 0, st, (const uint16_t*)from, stride, rows, width, pitch, (uint16_t*)to);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_copy");
+  return PT_OK;
+}
+int copy8(const void* from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch, void* to, hipStream_t st) {
+  hipLaunchKernelGGL(k_linear_copy8, dim3((rows + 3) / 4), dim3(256), 0, st, (const uint8_t*)from, stride, rows, width, pitch * 2, (uint8_t*)to);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_copy8");
+  return PT_OK;
+}
+
+template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
+  const bool b8 = in8(l);
+  const auto place = b8 ? copy8 : copy;
+  if (!p.x_direct)
+    if (int rc = place(l.x, l.x_stride, l.rows, l.width, p.Kd, ws + p.x, st); rc != PT_OK) return rc;
+  if (!p.w_direct)
+    if (int rc = place(l.weight, l.weight_stride, l.outs, l.width, p.Kd, ws + p.w, st); rc != PT_OK) return rc;
+  const uint32_t per = b8 ? 2 : 1;         // elements in a 16-bit word
+  const ProductArgs a = {rows_of(p.w_direct, l.weight, l.weight_stride / per, l.width / per, ws + p.w, p.Kd, l.outs),
+                         rows_of(p.x_direct, l.x, l.x_stride / per, l.width / per, ws + p.x, p.Kd, l.rows), l.outs, l.rows, p.Kd / TWO, (float*)(ws + p.sums),
+                         p.c.split};
+  const Layer e = {(const uint16_t*)l.bias, (const uint16_t*)l.gate, (const uint16_t*)l.residual, (uint16_t*)l.pre, (uint16_t*)l.out, l.x_scale, l.weight_scale,
+                   l.gate_stride, l.residual_stride, l.pre_stride, l.out_stride, l.outs, l.rows, l.act, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4};
+  return b8 ? product<PT_E4M3, DT, true, true>(p.c.kind, a, e, st) : product<DT, DT, true, true>(p.c.kind, a, e, st);
+}
+
+template <int DT> int run_grads(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
+  if (!p.x_direct)
+    if (int rc = copy(l.x, l.x_stride, l.rows, l.width, p.Kd, ws + p.x, st); rc != PT_OK) return rc;
+  if (!p.w_direct)
+    if (int rc = copy(l.weight, l.weight_stride, l.outs, l.width, p.Kd, ws + p.w, st); rc != PT_OK) return rc;
+  if (p.slope || l.d_bias) {
+    const SlopeArgs a = {(const uint16_t*)l.d_out, l.act != PT_ACT_NONE || l.gate ? (const uint16_t*)l.pre : nullptr, (const uint16_t*)l.gate,
+                         p.slope && (l.d_x || l.d_weight) ? (uint16_t*)(ws + p.dz) : nullptr,
+                         l.gate ? (uint16_t*)l.d_gate : nullptr, l.d_bias ? (float*)(ws + p.part) : nullptr, l.d_out_stride, l.pre_stride, l.gate_stride,
+                         l.d_gate_stride, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4, l.rows, l.outs, p.Np, p.rows_each, l.act};
+    hipLaunchKernelGGL(k_linear_slope<DT>, dim3((p.Np + 511) / 512, p.row_blocks), dim3(256), 0, st, a);
+    PT_LAUNCH_CHECK(nullptr, "k_linear_slope");
+  }
+  if (l.d_bias) {
+    hipLaunchKernelGGL(k_columns<DT>, dim3((l.outs + 63) / 64), dim3(256), 0, st, (const float*)(ws + p.part), p.row_blocks, uint64_t(p.Np), l.outs,
+                       (uint16_t*)l.d_bias);
+    PT_LAUNCH_CHECK(nullptr, "k_columns");
+  }
+  const Operand dz = p.slope ? Operand{ws + p.dz, 2ull * p.Np, 0, 0} : Operand{l.d_out, 2 * l.d_out_stride, 0, 0};
+  const uint32_t dz_width = p.slope ? p.Np : l.outs;
+  if (l.d_x) {
+    Operand w = rows_of(p.w_direct, l.weight, l.weight_stride, l.width, ws + p.w, p.Kd, 0);
+    w.extent = w.k;
+    w.k = l.outs;
+    const ProductArgs a = {w, {dz.at, dz.pitch, l.rows, dz_width}, l.width, l.rows, p.Np / TWO, (float*)(ws + p.sums), p.c_x.split};
+    const Plain e = {(uint16_t*)l.d_x, l.d_x_stride, l.width, l.rows};
+    if (int rc = product<DT, DT, false, true>(p.c_x.kind, a, e, st); rc != PT_OK) return rc;
+  }
+  if (l.d_weight) {
+    Operand x = rows_of(p.x_direct, l.x, l.x_stride, l.width, ws + p.x, p.Kd, 0);
+    x.extent = x.k;
+    x.k = l.rows;
+    const ProductArgs a = {x, {dz.at, dz.pitch, dz_width, l.rows}, l.width, l.outs, (l.rows + TWO - 1) / TWO, (float*)(ws + p.sums), p.c_w.split};
+    const Plain e = {(uint16_t*)l.d_weight, l.d_weight_stride, l.width, l.outs};
+    if (int rc = product<DT, DT, false, false>(p.c_w.kind, a, e, st); rc != PT_OK) return rc;
+  }
+  return PT_OK;
+}
+
+}  // namespace
+
+extern "C" int pt_linear_workspace(const pt_linear* layer, uint64_t* out_bytes, uint64_t* grads_bytes) {
+  if (int rc = check(layer, "pt_linear_workspace"); rc != PT_OK) return rc;
+  if (out_bytes) *out_bytes = layer->rows ? plan_out(*layer).total : 0;
+  if (grads_bytes) *grads_bytes = layer->rows && !in8(*layer) ? plan_grads(*layer).total : 0;
+  return PT_OK;
+}
+
+extern "C" int pt_linear_out(const pt_linear* l, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (int rc = check(l, "pt_linear_out"); rc != PT_OK) return rc;
+  if (!l->rows) return PT_OK;
+  if (!l->x || !l->weight || !l->out) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_linear_out: NULL array");
+  const Plan p = plan_out(*l);
+  if (int rc = check_workspace(p.total, workspace, workspace_bytes, "pt_linear_out"); rc != PT_OK) return rc;
+  return l->dtype == PT_BF16 ? run_out<PT_BF16>(*l, p, (char*)workspace, (hipStream_t)stream) : run_out<PT_FP16>(*l, p, (char*)workspace, (hipStream_t)stream);
+}
+
+extern "C" int pt_linear_grads(const pt_linear* l, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (int rc = check(l, "pt_linear_grads"); rc != PT_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  if (in8(*l)) return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "pt_linear_grads: operands in 8 bits");
+  if (l->d_gate && !l->gate) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_linear_grads: d_gate without a gate");
+  if (!l->rows) {
+    if (l->d_weight) {
+      hipLaunchKernelGGL(k_linear_zero, dim3(l->outs), dim3(256), 0, st, (uint16_t*)l->d_weight, l->d_weight_stride, l->width);
+      PT_LAUNCH_CHECK(nullptr, "k_linear_zero");
+    }
+    if (l->d_bias) {
+      hipLaunchKernelGGL(k_linear_zero, dim3(1), dim3(256), 0, st, (uint16_t*)l->d_bias, 0, l->outs);
+      PT_LAUNCH_CHECK(nullptr, "k_linear_zero");
+    }
+    return PT_OK;
+  }
+  if (!l->d_out || (l->d_weight && !l->x) || (l->d_x && !l->weight) || ((l->act != PT_ACT_NONE || l->gate) && !l->pre))
+    return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_linear_grads: NULL array");
+  const Plan p = plan_grads(*l);
+  if (int rc = check_workspace(p.total, workspace, workspace_bytes, "pt_linear_grads"); rc != PT_OK) return rc;
+  return l->dtype == PT_BF16 ? run_grads<PT_BF16>(*l, p, (char*)workspace, st) : run_grads<PT_FP16>(*l, p, (char*)workspace, st);
+}

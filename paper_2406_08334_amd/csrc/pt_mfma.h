@@ -23,9 +23,16 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int BK = 64, TWO = 2 * BK;
+// Beside pt_dtype's: e4m3 codes, two of which are what is said here of a 16-bit element (k next to each other in both operands).
+constexpr int PT_E4M3 = 16;
 template <int DT>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
-  if constexpr (DT == PT_BF16)
+  if constexpr (DT == PT_E4M3) {
+    typedef long l64x2 __attribute__((ext_vector_type(2)));
+    const l64x2 x = __builtin_bit_cast(l64x2, a), y = __builtin_bit_cast(l64x2, b);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(x[0], y[0], c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(x[1], y[1], c, 0, 0, 0);
+  } else if constexpr (DT == PT_BF16)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
