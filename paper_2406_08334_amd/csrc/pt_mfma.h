@@ -37,6 +37,14 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+// 128 e4m3 codes a row, 32 a lane; which 32 is of no matter where both operands take the same.  Twice the rate of the above.
+__device__ __forceinline__ f32x4 mfma_128(s16x8 a0, s16x8 a1, s16x8 b0, s16x8 b1, f32x4 c) {
+  typedef int s32x8 __attribute__((ext_vector_type(8)));
+  typedef short s16x16 __attribute__((ext_vector_type(16)));
+  const s16x16 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
+  const s16x16 b = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(s32x8, a), __builtin_bit_cast(s32x8, b), c, 0, 0, 0, 0, 0, 0);
+}
 
 // One operand of a product.  What lies behind its m (or n) and behind its last k is loaded as zero, or, of m and n, as what lies between its rows: the
 // result is not used.  Where k lies next to each other it is a multiple of 64.
@@ -202,6 +210,103 @@ struct Tile {
     for (; twos; --twos) {
       step(f0, f1, even, odd);
       step(f0, f1, odd, even);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  }
+};
+
+// The same of e4m3 codes, a step of which is 128 of them: an instruction takes all of a step, so it is the fragments of m that are halved.  The first half is
+// multiplied while the second is read; after the workgroup has met, the second, while the first of the next step is read, and of the
+// other operand what has had its last product.  8192 x 4096 x 11008: see pt_linear.hip.
+template <int BM, int BN, int WM, int WN>
+struct Tile<PT_E4M3, true, true, BM, BN, WM, WN> {
+  static constexpr int THREADS = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16, H = FM / 2;
+  static_assert(FM % 2 == 0, "two halves");
+  typedef Stage<true, BM, THREADS> SP;
+  typedef Stage<true, BN, THREADS> SQ;
+  static constexpr int BYTES = SP::BYTES + SQ::BYTES;
+  f32x4 acc[FM][FN];
+  struct Pair { s16x8 lo, hi; };
+  Pair a0[H], a1[H], b[FN];
+  SP sp;
+  SQ sq;
+
+  __device__ __forceinline__ uint32_t wave_m() const { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WM) * TM; }
+  __device__ __forceinline__ uint32_t wave_n() const { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WM) * TN; }
+
+  // Read r of 2 H of a half (fragments of m from `first` on), or of 2 FN of the other operand.
+  __device__ __forceinline__ void read_a(Pair (&a)[H], const lds_char* from, int first, int r) const { (r & 1 ? a[r / 2].hi : a[r / 2].lo) = sp.read(from, first + r / 2, r & 1); }
+  __device__ __forceinline__ void read_b(const lds_char* from, int r) { (r & 1 ? b[r / 2].hi : b[r / 2].lo) = sq.read(from + SP::BYTES, r / 2, r & 1); }
+
+  template <bool LAST>
+  __device__ __forceinline__ void half(const Pair (&a)[H], Pair (&other)[H], const lds_char* from, lds_char* to) {
+    constexpr int PRODUCTS = H * FN, FETCHES = SP::N + SQ::N;
+    __builtin_amdgcn_sched_barrier(0);
+    int fetched = 0, reads = 0;
+#pragma unroll
+    for (int x = 0; x < PRODUCTS; ++x) {
+      const int j = x / H, i = x % H, m = (LAST ? H : 0) + i;
+      acc[m][j] = mfma_128(a[i].lo, a[i].hi, b[j].lo, b[j].hi, acc[m][j]);
+      __builtin_amdgcn_sched_barrier(0);
+      const bool end = x + 1 == PRODUCTS;
+      if (LAST)
+#pragma unroll
+        for (; fetched < FETCHES && (end || fetched * PRODUCTS < (x + 1) * FETCHES); ++fetched) {
+          if (fetched < SP::N) sp.fetch(to, fetched);
+          else sq.fetch(to + SP::BYTES, fetched - SP::N);
+        }
+      constexpr int READS = 2 * H + (LAST ? 2 * FN : 0);
+      // of b what has been multiplied with all of this half
+#pragma unroll
+      for (; reads < READS && (end || reads * PRODUCTS < (x + 1) * READS) && (end || reads < 2 * H || (reads - 2 * H) / 2 < (x + 1) / H); ++reads) {
+        if (reads < 2 * H) read_a(other, from, LAST ? 0 : H, reads);
+        else read_b(from, reads - 2 * H);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  static __device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  __device__ __forceinline__ void step(lds_char* now, lds_char* then) {
+    half<false>(a0, a1, now, nullptr);
+    meet();
+    half<true>(a1, a0, then, now);
+    sp.advance();
+    sq.advance();
+  }
+  __device__ __forceinline__ void fetch(lds_char* to) {
+#pragma unroll
+    for (int i = 0; i < SP::N; ++i) sp.fetch(to, i);
+#pragma unroll
+    for (int i = 0; i < SQ::N; ++i) sq.fetch(to + SP::BYTES, i);
+    sp.advance();
+    sq.advance();
+  }
+  __device__ __forceinline__ void run(lds_char* even, lds_char* odd, const Operand& p, const Operand& q, uint32_t m0, uint32_t n0, uint32_t k0,
+                                      uint32_t twos) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (!twos) return;
+    sp.init(p, m0, k0, wave_m());
+    sq.init(q, n0, k0, wave_n());
+    fetch(even);
+    fetch(odd);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SP::N + SQ::N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 2 * H; ++r) read_a(a0, even, 0, r);
+#pragma unroll
+    for (int r = 0; r < 2 * FN; ++r) read_b(even, r);
+#pragma unroll 1
+    for (; twos; --twos) {
+      step(even, odd);
+      step(odd, even);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   }
