@@ -247,6 +247,66 @@ __global__ void __launch_bounds__(256) k_linear_join(const ProductArgs a, const 
                 [&](uint32_t m, uint32_t n, f32x4 x) { e.template four<DT>(m, n, x); });
 }
 
+// Up to 16 rows: they take as long as the weight takes to read, which each wave has on its way straight into the registers that are multiplied: 16 outs a workgroup, of
+// which a wave takes 256 bytes of k in every WAVES times as many.  Any address, stride and width; no workspace.
+constexpr uint32_t THIN_ROWS = 16;
+
+struct ThinArgs {
+  const char *x, *weight;
+  uint64_t x_pitch, weight_pitch;          // bytes
+  uint32_t rows, outs, bytes;              // of a row
+};
+
+// 16 bytes of a row from `at` on, zero behind its end.
+template <int MUL>
+__device__ __forceinline__ u32x4 end16(const PT_GLOBAL char* row, uint32_t at, uint32_t bytes) {
+  if constexpr (MUL != PT_E4M3) return load8((const PT_GLOBAL uint16_t*)row, at / 2, bytes / 2);
+  u32x4 q = {0, 0, 0, 0};
+#pragma unroll
+  for (uint32_t j = 0; j < 16; ++j)
+    if (at + j < bytes) q[j / 4] |= uint32_t(uint8_t(row[at + j])) << (8 * (j & 3));
+  return q;
+}
+
+template <int MUL, int DT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_linear_thin(const ThinArgs a, const Layer e) {
+  constexpr uint32_t U = 4, CHUNK = U * 64;
+  __shared__ __attribute__((aligned(16))) f32x4 s_acc[WAVES][64];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, g = lane >> 4, m0 = blockIdx.x * 16;
+  const PT_GLOBAL char* w = (const PT_GLOBAL char*)a.weight + min(m0 + l, a.outs - 1) * a.weight_pitch;
+  const PT_GLOBAL char* x = (const PT_GLOBAL char*)a.x + min(l, a.rows - 1) * a.x_pitch;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  const uint32_t whole = a.bytes / CHUNK;
+  u32x4 qw[U], qx[U];
+  const auto load = [&](uint32_t c) {
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) qw[u] = *(const PT_GLOBAL u32x4_b*)(w + c * CHUNK + u * 64 + g * 16);
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) qx[u] = *(const PT_GLOBAL u32x4_b*)(x + c * CHUNK + u * 64 + g * 16);
+  };
+  if (wave < whole) load(wave);
+#pragma unroll 1
+  for (uint32_t c = wave; c < whole; c += WAVES) {
+    u32x4 nw[U], nx[U];
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) { nw[u] = qw[u]; nx[u] = qx[u]; }
+    if (c + WAVES < whole) load(c + WAVES);
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) acc = mfma<MUL>(__builtin_bit_cast(s16x8, nw[u]), __builtin_bit_cast(s16x8, nx[u]), acc);
+  }
+  if (wave == whole % WAVES)               // what is left
+#pragma unroll 1
+    for (uint32_t at = whole * CHUNK; at < a.bytes; at += 64)
+      acc = mfma<MUL>(__builtin_bit_cast(s16x8, end16<MUL>(w, at + g * 16, a.bytes)), __builtin_bit_cast(s16x8, end16<MUL>(x, at + g * 16, a.bytes)), acc);
+  s_acc[wave][lane] = acc;
+  __syncthreads();
+  if (wave) return;
+  acc = s_acc[0][lane];
+#pragma unroll
+  for (uint32_t k = 1; k < uint32_t(WAVES); ++k) acc += s_acc[k][lane];
+  e.template four<DT>(m0 + g * 4, l, acc);
+}
+
 // Rows of 16-bit words (or bytes) whose beginnings, distances or ends the products cannot take: they load 16 bytes a lane past registers.
 __global__ void __launch_bounds__(256) k_linear_copy(const uint16_t* __restrict__ from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch,
                                                      uint16_t* __restrict__ to) {
@@ -392,6 +452,7 @@ struct Taker {
 
 Plan plan_out(const pt_linear& l) {
   Plan p{};
+  if (l.rows <= THIN_ROWS) return p;
   const uint32_t bytes = in8(l) ? 1 : 2;
   Taker take;
   p.Kd = uint32_t(up(uint64_t(l.width) * bytes, 2 * TWO) / 2);
@@ -489,8 +550,24 @@ int copy8(const void* from, uint64_t stride, uint32_t rows, uint32_t width, uint
   return PT_OK;
 }
 
+template <int MUL, int DT> int thin(const ThinArgs& a, const Layer& e, hipStream_t st) {
+  const uint32_t grid = (a.outs + 15) / 16;
+  if (grid >= 1024) hipLaunchKernelGGL((k_linear_thin<MUL, DT, 4>), dim3(grid), dim3(256), 0, st, a, e);
+  else if (grid >= 256) hipLaunchKernelGGL((k_linear_thin<MUL, DT, 8>), dim3(grid), dim3(512), 0, st, a, e);
+  else hipLaunchKernelGGL((k_linear_thin<MUL, DT, 16>), dim3(grid), dim3(1024), 0, st, a, e);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_thin");
+  return PT_OK;
+}
+
 template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
   const bool b8 = in8(l);
+  const Layer e = {(const uint16_t*)l.bias, (const uint16_t*)l.gate, (const uint16_t*)l.residual, (uint16_t*)l.pre, (uint16_t*)l.out, l.x_scale, l.weight_scale,
+                   l.gate_stride, l.residual_stride, l.pre_stride, l.out_stride, l.outs, l.rows, l.act, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4};
+  if (l.rows <= THIN_ROWS) {
+    const uint32_t bytes = b8 ? 1 : 2;
+    const ThinArgs a = {(const char*)l.x, (const char*)l.weight, l.x_stride * bytes, l.weight_stride * bytes, l.rows, l.outs, l.width * bytes};
+    return b8 ? thin<PT_E4M3, DT>(a, e, st) : thin<DT, DT>(a, e, st);
+  }
   const auto place = b8 ? copy8 : copy;
   if (!p.x_direct)
     if (int rc = place(l.x, l.x_stride, l.rows, l.width, p.Kd, ws + p.x, st); rc != PT_OK) return rc;
@@ -500,8 +577,6 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
   const ProductArgs a = {rows_of(p.w_direct, l.weight, l.weight_stride / per, l.width / per, ws + p.w, p.Kd, l.outs),
                          rows_of(p.x_direct, l.x, l.x_stride / per, l.width / per, ws + p.x, p.Kd, l.rows), l.outs, l.rows, p.Kd / TWO, (float*)(ws + p.sums),
                          p.c.split};
-  const Layer e = {(const uint16_t*)l.bias, (const uint16_t*)l.gate, (const uint16_t*)l.residual, (uint16_t*)l.pre, (uint16_t*)l.out, l.x_scale, l.weight_scale,
-                   l.gate_stride, l.residual_stride, l.pre_stride, l.out_stride, l.outs, l.rows, l.act, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4};
   return b8 ? product<PT_E4M3, DT, true, true>(p.c.kind, a, e, st) : product<DT, DT, true, true>(p.c.kind, a, e, st);
 }
 
