@@ -106,23 +106,34 @@ struct Layer {
   pt_random::Drop drop;
   uint64_t words;            // of random numbers in a row
 
-  // z of outs m on of row n, from their sums.
-  template <int DT, int N>
-  __device__ __forceinline__ void z_of(float (&x)[N], uint32_t m, uint32_t n) const {
-    if (x_scale) {
-      const float s = ((const PT_GLOBAL float*)x_scale)[n];
+  // z of N outs of row n from their sums: scales in 8 bits and bias, of the outs m on.
+  template <int DT, int N> struct Columns {
+    float scale[N], bias[N];
+    __device__ __forceinline__ void load(const Layer& e, uint32_t m) {
 #pragma unroll
-      for (int q = 0; q < N; ++q) x[q] = x[q] * s * ((const PT_GLOBAL float*)weight_scale)[min(m + q, extent_m - 1)];
-    }
-    if (bias) {
+      for (int q = 0; q < N; ++q) {
+        scale[q] = e.weight_scale ? ((const PT_GLOBAL float*)e.weight_scale)[min(m + q, e.extent_m - 1)] : 1.0f;
+        bias[q] = 0.0f;
+      }
+      if (!e.bias || m >= e.extent_m) return;
 #pragma unroll
       for (int q = 0; q < N; q += 4) {
-        const f32x4 b = decode4<DT>(load4((const PT_GLOBAL uint16_t*)bias, m + q, extent_m));
+        const f32x4 b = decode4<DT>(load4((const PT_GLOBAL uint16_t*)e.bias, m + q, e.extent_m));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[q + i] += b[i];
+        for (int i = 0; i < 4; ++i) bias[q + i] = b[i];
       }
     }
-  }
+    __device__ __forceinline__ void z(const Layer& e, float x_scale, float (&x)[N]) const {
+      if (e.x_scale) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) x[q] = x[q] * x_scale * scale[q];
+      }
+      if (e.bias) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) x[q] += bias[q];
+      }
+    }
+  };
   // From there to the result; g, r: gate and residual.
   template <int N>
   __device__ __forceinline__ void result(float (&y)[N], uint64_t key, uint32_t m, uint32_t n, const float (&g)[N], const float (&r)[N]) const {
@@ -153,41 +164,57 @@ struct Layer {
   // turn is under way during the one before.  The wave's own part of the buffers: 16 bytes of piece c of row n at c ^ n.
   template <int DT, class T>
   __device__ __forceinline__ void tile(const T& t, uint32_t m0, uint32_t n0, lds_char* even, lds_char* odd) const {
-    constexpr uint32_t TM = T::TM, ROW = TM * 4, LANES = TM / 8, STEP = 64 / LANES, TURNS = 16 / STEP, WAVES = T::THREADS / 64;
+    constexpr uint32_t TM = T::TM, ROW = TM * 4, LANES = TM / 8, STEP = 64 / LANES, TURNS = 16 / STEP, G = TURNS < 2 ? 1 : 2, WAVES = T::THREADS / 64;
     static_assert(TM >= 32 && (WAVES + 1) / 2 * 16 * ROW <= T::BYTES, "the waves' parts fit the buffers");
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15;
     lds_char* own = (wave & 1 ? odd : even) + (wave >> 1) * (16 * ROW);
     const uint32_t r = lane / LANES, c = lane % LANES, m = m0 + t.wave_m() + c * 8, first = n0 + t.wave_n();
     const uint64_t key = drop.key();
-    u32x4 qg = {0, 0, 0, 0}, qr = qg;
-    const auto fetch = [&](uint32_t turn) {                // turns of all fragments, one after the other
-      const uint32_t n = min(first + turn * STEP + r, extent_n - 1);
-      if (gate) qg = fetch8((const PT_GLOBAL uint16_t*)gate + n * gate_stride, m, extent_m);
-      if (residual) qr = fetch8((const PT_GLOBAL uint16_t*)residual + n * residual_stride, m, extent_m);
+    u32x4 qg[G] = {}, qr[G] = {};
+    float qs[G] = {};
+    const auto fetch = [&](uint32_t it) {
+#pragma unroll
+      for (uint32_t turn = 0; turn < G; ++turn) {
+        const uint32_t n = min(first + (it * G + turn) * STEP + r, extent_n - 1);
+        if (x_scale) qs[turn] = ((const PT_GLOBAL float*)x_scale)[n];
+        if (gate) qg[turn] = fetch8((const PT_GLOBAL uint16_t*)gate + n * gate_stride, m, extent_m);
+        if (residual) qr[turn] = fetch8((const PT_GLOBAL uint16_t*)residual + n * residual_stride, m, extent_m);
+      }
     };
-    __syncthreads();                                       // every wave has read its last operands
+    Columns<DT, 8> columns;
     fetch(0);
+    columns.load(*this, m);
+    __syncthreads();                                       // every wave has read its last operands
 #pragma unroll 1
-    for (uint32_t j = 0; j < uint32_t(T::FN); ++j) {
+    for (uint32_t it = 0; it < T::FN * TURNS / G; ++it) {
 #pragma unroll
       for (int k = 0; k < T::FN; ++k)
-        if (j == uint32_t(k))
+        if (it == k * TURNS / G)
 #pragma unroll
           for (int i = 0; i < T::FM; ++i) *(lds_f32x4*)(own + l * ROW + ((i * 4 + (lane >> 4)) ^ (l & (TM / 4 - 1))) * 16) = t.acc[i][k];
-#pragma unroll 1
-      for (uint32_t turn = 0; turn < TURNS; ++turn) {
-        const uint32_t row = turn * STEP + r, n = first + j * 16 + row;
-        const u32x4 now_g = qg, now_r = qr;
-        if (j * TURNS + turn + 1 < T::FN * TURNS) fetch(j * TURNS + turn + 1);
-        const f32x4 lo = *(lds_f32x4*)(own + row * ROW + ((c * 2) ^ (row & (TM / 4 - 1))) * 16);
-        const f32x4 hi = *(lds_f32x4*)(own + row * ROW + ((c * 2 + 1) ^ (row & (TM / 4 - 1))) * 16);
+      u32x4 now_g[G], now_r[G];
+      float now_s[G];
+      f32x4 x[G][2];
+#pragma unroll
+      for (uint32_t turn = 0; turn < G; ++turn) {
+        const uint32_t row = (it * G + turn) % TURNS * STEP + r;
+        now_g[turn] = qg[turn]; now_r[turn] = qr[turn]; now_s[turn] = qs[turn];
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) x[turn][h] = *(lds_f32x4*)(own + row * ROW + ((c * 2 + h) ^ (row & (TM / 4 - 1))) * 16);
+      }
+      if ((it + 1) * G < T::FN * TURNS) fetch(it + 1);
+#pragma unroll
+      for (uint32_t turn = 0; turn < G; ++turn) {
+        const uint32_t n = first + (it * G + turn) * STEP + r;
         if (n >= extent_n || m >= extent_m) continue;
-        float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, g[8], b[8];
-        z_of<DT>(y, m, n);
+        float y[8], g[8], b[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) y[q] = x[turn][q / 4][q % 4];
+        columns.z(*this, now_s[turn], y);
         if (pre) store8((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode8<DT>(y));
-        decode8<DT>(place8(now_g, m, extent_m), g);
-        decode8<DT>(place8(now_r, m, extent_m), b);
+        if (gate) decode8<DT>(place8(now_g[turn], m, extent_m), g);
+        if (residual) decode8<DT>(place8(now_r[turn], m, extent_m), b);
         result(y, key, m, n, g, b);
         store8((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode8<DT>(y));
       }
@@ -204,7 +231,9 @@ struct Layer {
     };
     if (gate) get(gate, gate_stride, g);
     if (residual) get(residual, residual_stride, r);
-    z_of<DT>(y, m, n);
+    Columns<DT, 4> columns;
+    columns.load(*this, m);
+    columns.z(*this, x_scale ? ((const PT_GLOBAL float*)x_scale)[n] : 1.0f, y);
     if (pre) store4((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
     result(y, drop.key(), m, n, g, r);
     store4((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
