@@ -25,11 +25,7 @@ __device__ __forceinline__ void drop8(const DropArgs& a, uint64_t key, uint64_t 
   decode8<DT>(x, y);
   if (a.drop.off) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const pt_random::f32x4 q = a.drop.of(key, word + h, pt_random::f32x4{y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]});
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[4 * h + j] = q[j];
-    }
+    for (int h = 0; h < 2; ++h) a.drop.apply(key + (word + h + 1) * pt_random::PHI, y + 4 * h);
   }
   if (a.residual) {
     float b[8];

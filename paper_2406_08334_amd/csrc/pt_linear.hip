@@ -38,21 +38,29 @@ __device__ __forceinline__ float act(float z) {
   else if constexpr (ACT == PT_ACT_GELU) { float e; return z * normal(z, e); }
   else return z;
 }
-// act(z) and its derivative, which beyond 32 is 0 or 1 (its terms there would be products of 0 and inf).
+// act(z) and its derivative, which beyond 32 is 0 or 1 (its terms there would be products of 0 and inf), as are the factors of z.
 template <int ACT>
 __device__ __forceinline__ float act(float z, float& slope) {
-  const float y = act<ACT>(z), c = z < -32.0f ? -32.0f : z > 32.0f ? 32.0f : z;
-  if constexpr (ACT == PT_ACT_RELU) slope = z > 0.0f ? 1.0f : 0.0f;
-  else if constexpr (ACT == PT_ACT_SILU) { const float f = sigmoid(c); slope = f * __builtin_fmaf(c, 1.0f - f, 1.0f); }
-  else if constexpr (ACT == PT_ACT_GELU_TANH) {
+  const float c = z < -32.0f ? -32.0f : z > 32.0f ? 32.0f : z;
+  if constexpr (ACT == PT_ACT_RELU) {
+    slope = z > 0.0f ? 1.0f : 0.0f;
+    return act<ACT>(z);
+  } else if constexpr (ACT == PT_ACT_SILU) {
+    const float f = sigmoid(z);
+    slope = f * __builtin_fmaf(c, 1.0f - f, 1.0f);
+    return z * f;
+  } else if constexpr (ACT == PT_ACT_GELU_TANH) {
     const float f = sigmoid(TANH_2A * __builtin_fmaf(TANH_B * c, c * c, c));
     slope = __builtin_fmaf(c * f * (1.0f - f), TANH_2A * __builtin_fmaf(3.0f * TANH_B * c, c, 1.0f), f);
+    return z * f;
   } else if constexpr (ACT == PT_ACT_GELU) {
     float e;
     const float f = normal(c, e);
     slope = __builtin_fmaf(c * 0.39894228040143267794f, e, f);
-  } else slope = 1.0f;
-  return y;
+    return z * f;
+  }
+  slope = 1.0f;
+  return z;
 }
 
 // f: called with the activation as a constant.
@@ -134,9 +142,10 @@ struct Layer {
       }
     }
   };
-  // From there to the result; g, r: gate and residual.
+  __device__ __forceinline__ uint64_t counter(uint32_t m, uint32_t n) const { return drop.key() + (n * words + m / 4 + 1) * pt_random::PHI; }
+  // From there to the result; g, r: gate and residual; counter: of the first four's random numbers.
   template <int N>
-  __device__ __forceinline__ void result(float (&y)[N], uint64_t key, uint32_t m, uint32_t n, const float (&g)[N], const float (&r)[N]) const {
+  __device__ __forceinline__ void result(float (&y)[N], uint64_t counter, const float (&g)[N], const float (&r)[N]) const {
     with_act(act, [&](auto a) {
 #pragma unroll
       for (int q = 0; q < N; ++q) y[q] = ::act<a()>(y[q]);
@@ -147,11 +156,7 @@ struct Layer {
     }
     if (drop.off) {
 #pragma unroll
-      for (int q = 0; q < N; q += 4) {
-        const f32x4 k = drop.of(key, n * words + (m + q) / 4, f32x4{y[q], y[q + 1], y[q + 2], y[q + 3]});
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[q + i] = k[i];
-      }
+      for (int q = 0; q < N; q += 4) drop.apply(counter + q / 4 * pt_random::PHI, y + q);
     }
     if (residual) {
 #pragma unroll
@@ -170,7 +175,7 @@ struct Layer {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15;
     lds_char* own = (wave & 1 ? odd : even) + (wave >> 1) * (16 * ROW);
     const uint32_t r = lane / LANES, c = lane % LANES, m = m0 + t.wave_m() + c * 8, first = n0 + t.wave_n();
-    const uint64_t key = drop.key();
+    const uint64_t from = drop.off ? counter(m, first + r) : 0, row_step = words * pt_random::PHI;
     u32x4 qg[G] = {}, qr[G] = {};
     float qs[G] = {};
     const auto fetch = [&](uint32_t it) {
@@ -215,7 +220,7 @@ struct Layer {
         if (pre) store8((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode8<DT>(y));
         if (gate) decode8<DT>(place8(now_g[turn], m, extent_m), g);
         if (residual) decode8<DT>(place8(now_r[turn], m, extent_m), b);
-        result(y, key, m, n, g, b);
+        result(y, from + (it * G + turn) * STEP * row_step, g, b);
         store8((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode8<DT>(y));
       }
     }
@@ -235,7 +240,7 @@ struct Layer {
     columns.load(*this, m);
     columns.z(*this, x_scale ? ((const PT_GLOBAL float*)x_scale)[n] : 1.0f, y);
     if (pre) store4((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
-    result(y, drop.key(), m, n, g, r);
+    result(y, drop.off ? counter(m, n) : 0, g, r);
     store4((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
   }
 };
@@ -251,30 +256,65 @@ struct ProductArgs {
 
 // MUL: PT_BF16, PT_FP16 or PT_E4M3, what is multiplied; DT: what the epilogue reads and writes.
 template <int MUL, int DT, class C, bool PK, bool QK, class E>
-__global__ void __launch_bounds__(C::THREADS) k_linear_product(const ProductArgs a, const E e) {
-  constexpr int BYTES = C::template Of<MUL, PK, QK>::BYTES;
-  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+__device__ __forceinline__ void product_tile(const ProductArgs& a, const E& e, lds_char* even, lds_char* odd, uint32_t block) {
   uint32_t tm, tn, part;
   PT_GLOBAL float* left;
-  if (!part_of<C>(a.split, blockIdx.x, (a.extent_m + C::BM - 1) / C::BM, (a.extent_n + C::BN - 1) / C::BN, a.sums, tm, tn, part, left)) return;
+  if (!part_of<C>(a.split, block, (a.extent_m + C::BM - 1) / C::BM, (a.extent_n + C::BN - 1) / C::BN, a.sums, tm, tn, part, left)) return;
   const uint32_t t0 = left ? uint32_t(uint64_t(a.twos) * part / a.split.n) : 0, t1 = left ? uint32_t(uint64_t(a.twos) * (part + 1) / a.split.n) : a.twos;
   with_tile<MUL, C, PK, QK>(a.extent_m - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
-    t.run((lds_char*)even, (lds_char*)odd, a.p, a.q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+    t.run(even, odd, a.p, a.q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
     if (left) {
 #pragma unroll
       for (int j = 0; j < T::FN; ++j) leave<C>(t, j, left);
       return;
     }
-    e.template tile<DT>(t, tm * C::BM, tn * C::BN, (lds_char*)even, (lds_char*)odd);
+    e.template tile<DT>(t, tm * C::BM, tn * C::BN, even, odd);
   });
 }
 
+template <int MUL, int DT, class C, bool PK, bool QK, class E>
+__global__ void __launch_bounds__(C::THREADS) k_linear_product(const ProductArgs a, const E e) {
+  constexpr int BYTES = C::template Of<MUL, PK, QK>::BYTES;
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+  product_tile<MUL, DT, C, PK, QK>(a, e, (lds_char*)even, (lds_char*)odd, blockIdx.x);
+}
+
+template <int DT, class C, class E>
+__device__ __forceinline__ void join_product(const ProductArgs& a, const E& e, uint32_t block, uint32_t blocks) {
+  join_tiles<C>(a.sums, a.split, (a.extent_m + C::BM - 1) / C::BM, (a.extent_n + C::BN - 1) / C::BN,
+                [&](uint32_t m, uint32_t n, f32x4 x) { e.template four<DT>(m, n, x); }, block, blocks);
+}
 template <int DT, class C, class E>
 __global__ void __launch_bounds__(256) k_linear_join(const ProductArgs a, const E e) {
-  join_tiles<C>(a.sums, a.split, (a.extent_m + C::BM - 1) / C::BM, (a.extent_n + C::BN - 1) / C::BN,
-                [&](uint32_t m, uint32_t n, f32x4 x) { e.template four<DT>(m, n, x); });
+  join_product<DT, C>(a, e, blockIdx.x, gridDim.x);
 }
+
+// Both gradients in one launch, where neither fills the chip for long: 1531 x 771 x 3083 in 24 us, one after the other 20 + 21.  C: the tiles of d_x.
+template <int DT, class C>
+__global__ void __launch_bounds__(256) k_linear_both(const ProductArgs x, const Plain ex, const ProductArgs w, const Plain ew, uint32_t blocks_x) {
+  static_assert(C::THREADS == 256 && Mid::THREADS == 256, "one launch");
+  constexpr int BYTES = std::max(C::template Of<DT, false, true>::BYTES, Mid::Of<DT, false, false>::BYTES);
+  __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
+  if (blockIdx.x < blocks_x) product_tile<DT, DT, C, false, true>(x, ex, (lds_char*)even, (lds_char*)odd, blockIdx.x);
+  else product_tile<DT, DT, Mid, false, false>(w, ew, (lds_char*)even, (lds_char*)odd, blockIdx.x - blocks_x);
+}
+
+// What is left of the gradients: sums of several workgroups a tile, and of the bias's columns.
+struct BiasArgs {
+  const float* part;
+  uint32_t rows, pitch, outs;
+  uint16_t* d_bias;
+};
+template <int DT, class C>
+__global__ void __launch_bounds__(256) k_linear_ends(const ProductArgs x, const Plain ex, const ProductArgs w, const Plain ew, const BiasArgs b, uint32_t blocks_x,
+                                                     uint32_t blocks_w) {
+  if (blockIdx.x < blocks_x) join_product<DT, C>(x, ex, blockIdx.x, blocks_x);
+  else if (blockIdx.x < blocks_x + blocks_w) join_product<DT, Mid>(w, ew, blockIdx.x - blocks_x, blocks_w);
+  else add_columns<DT>(b.part, b.rows, b.pitch, b.outs, b.d_bias, blockIdx.x - blocks_x - blocks_w);
+}
+template <int DT>
+__global__ void __launch_bounds__(256) k_linear_bias(const BiasArgs b) { add_columns<DT>(b.part, b.rows, b.pitch, b.outs, b.d_bias, blockIdx.x); }
 
 // Up to 16 rows: they take as long as the weight takes to read, which each wave has on its way straight into the registers that are multiplied: 16 outs a workgroup, of
 // which a wave takes 256 bytes of k in every WAVES times as many.  Any address, stride and width; no workspace.
@@ -336,32 +376,35 @@ __global__ void __launch_bounds__(WAVES * 64) k_linear_thin(const ThinArgs a, co
   e.template four<DT>(m0 + g * 4, l, acc);
 }
 
-// Rows of 16-bit words (or bytes) whose beginnings, distances or ends the products cannot take: they load 16 bytes a lane past registers.
-__global__ void __launch_bounds__(256) k_linear_copy(const uint16_t* __restrict__ from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch,
-                                                     uint16_t* __restrict__ to) {
-  const uint32_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  if (r >= rows) return;
-  const PT_GLOBAL uint16_t* row = (const PT_GLOBAL uint16_t*)from + r * stride;
-  PT_GLOBAL uint16_t* dst = (PT_GLOBAL uint16_t*)to + size_t(r) * pitch;
+// Rows whose beginnings, distances or ends the products cannot take: they load 16 bytes a lane past registers.
+struct CopyArgs {
+  const void* from;
+  uint64_t stride;
+  uint32_t rows, width, pitch;             // elements; pitch: of a copied row, which is zero behind its end
+  void* to;
+};
+inline uint32_t copy_blocks(const CopyArgs& a) { return (a.rows + 3) / 4; }
+// Of one or two bytes an element, four rows by a workgroup of 256.
+template <int BYTES>
+__device__ __forceinline__ void copy_rows(const CopyArgs& a, uint32_t block) {
+  const uint32_t r = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  if (r >= a.rows) return;
+  if constexpr (BYTES == 2) {
+    copy_row((const PT_GLOBAL uint16_t*)a.from + r * a.stride, (PT_GLOBAL uint16_t*)a.to + size_t(r) * a.pitch, a.width, a.pitch, lane, 64);
+  } else {
+    const PT_GLOBAL char* row = (const PT_GLOBAL char*)a.from + r * a.stride;
+    PT_GLOBAL char* to = (PT_GLOBAL char*)a.to + size_t(r) * a.pitch;
 #pragma unroll 4
-  for (uint32_t c = lane * 8; c < pitch; c += 512) *(PT_GLOBAL u32x4*)(dst + c) = load8(row, c, width);
-}
-__global__ void __launch_bounds__(256) k_linear_copy8(const uint8_t* __restrict__ from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch,
-                                                      uint8_t* __restrict__ to) {
-  const uint32_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  if (r >= rows) return;
-  const PT_GLOBAL uint8_t* row = (const PT_GLOBAL uint8_t*)from + r * stride;
-  PT_GLOBAL uint8_t* dst = (PT_GLOBAL uint8_t*)to + size_t(r) * pitch;
-#pragma unroll 4
-  for (uint32_t c = lane * 16; c < pitch; c += 1024) {
-    u32x4 q = {0, 0, 0, 0};
-    if (c + 16 <= width) q = *(const PT_GLOBAL u32x4_b*)(row + c);
-    else
-#pragma unroll
-      for (uint32_t j = 0; j < 16; ++j)
-        if (c + j < width) q[j / 4] |= uint32_t(row[c + j]) << (8 * (j & 3));
-    *(PT_GLOBAL u32x4*)(dst + c) = q;
+    for (uint32_t c = lane * 16; c < a.pitch; c += 1024)
+      *(PT_GLOBAL u32x4*)(to + c) = c + 16 <= a.width ? u32x4(*(const PT_GLOBAL u32x4_b*)(row + c)) : end16<PT_E4M3>(row, c, a.width);
   }
+}
+// Both operands; either may have no rows.
+template <int BYTES>
+__global__ void __launch_bounds__(256) k_linear_copy(const CopyArgs x, const CopyArgs w) {
+  const uint32_t blocks = (x.rows + 3) / 4;
+  if (blockIdx.x < blocks) copy_rows<BYTES>(x, blockIdx.x);
+  else copy_rows<BYTES>(w, blockIdx.x - blocks);
 }
 
 // ---- slope ---------------------------------------------------------------------------------------------------
@@ -369,21 +412,29 @@ __global__ void __launch_bounds__(256) k_linear_copy8(const uint8_t* __restrict_
 struct SlopeArgs {
   const uint16_t *d_out, *pre, *gate;
   uint16_t *dz, *d_gate;     // dz: rows of `pitch`, zero behind outs; or NULL: it is d_out
-  float* part;               // [gridDim.y][pitch]: sums of the columns, or NULL
+  float* part;               // [rows / rows_each][pitch]: sums of the columns, or NULL
   uint64_t d_out_stride, pre_stride, gate_stride, d_gate_stride;
   pt_random::Drop drop;
   uint64_t words;
-  uint32_t rows, outs, pitch, rows_each;
+  uint32_t rows, outs, pitch, rows_each, strips;       // strips of 512 columns
   int act;
 };
 
-// 512 columns, eight a lane, of rows_each rows, a quarter of which is a wave's.  Bound by memory.
+// 512 columns, eight a lane, of rows_each rows, a quarter of which is a wave's.  Bound by memory.  The last workgroups copy what has to be copied of the
+// operands: two launches less.
 template <int DT>
-__global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a) {
+__global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a, const CopyArgs x, const CopyArgs w, uint32_t blocks) {
+  if (blockIdx.x >= blocks) {
+    const uint32_t i = blockIdx.x - blocks, blocks_x = (x.rows + 3) / 4;
+    if (i < blocks_x) copy_rows<2>(x, i);
+    else copy_rows<2>(w, i - blocks_x);
+    return;
+  }
   __shared__ float s_part[4][512];
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = blockIdx.x * 512 + lane * 8;
-  const uint32_t first = blockIdx.y * a.rows_each, end = min(a.rows, first + a.rows_each);
-  const uint64_t key = a.drop.key();
+  const uint32_t by = blockIdx.x / a.strips, bx = blockIdx.x - by * a.strips;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = bx * 512 + lane * 8;
+  const uint32_t first = by * a.rows_each, end = min(a.rows, first + a.rows_each);
+  const uint64_t from = a.drop.key() + (c / 4 + 1) * pt_random::PHI, row_step = a.words * pt_random::PHI;
   float sum[8] = {};
   if (c < a.pitch)
     with_act(a.act, [&](auto act) {
@@ -396,11 +447,7 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a) {
         decode8<DT>(place8(qe, c, a.outs), e);
         if (a.drop.off) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const pt_random::f32x4 q = a.drop.of(key, r * a.words + c / 4 + h, pt_random::f32x4{e[4 * h], e[4 * h + 1], e[4 * h + 2], e[4 * h + 3]});
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[4 * h + j] = q[j];
-          }
+          for (int h = 0; h < 2; ++h) a.drop.apply(from + r * row_step + h * pt_random::PHI, e + 4 * h);
         }
         if (a.pre) {
           decode8<DT>(place8(qz, c, a.outs), z);
@@ -432,8 +479,8 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a) {
   for (int j = 0; j < 8; ++j) s_part[wave][lane * 8 + j] = sum[j];
   __syncthreads();
   for (uint32_t i = threadIdx.x; i < 512; i += 256) {
-    const uint32_t col = blockIdx.x * 512 + i;
-    if (col < a.pitch) ((PT_GLOBAL float*)a.part)[size_t(blockIdx.y) * a.pitch + col] = ((s_part[0][i] + s_part[1][i]) + s_part[2][i]) + s_part[3][i];
+    const uint32_t col = bx * 512 + i;
+    if (col < a.pitch) ((PT_GLOBAL float*)a.part)[size_t(by) * a.pitch + col] = ((s_part[0][i] + s_part[1][i]) + s_part[2][i]) + s_part[3][i];
   }
 }
 
@@ -466,10 +513,11 @@ bool direct(const void* at, uint64_t stride, uint32_t width, uint32_t bytes) {
 // Where everything lies in the workspace.
 struct Plan {
   bool x_direct, w_direct, slope;          // slope: dz is not d_out
+  bool both;                               // gradients in one launch
   uint32_t Kd, Np;                         // width and outs rounded up to whole steps (Kd in 16-bit words)
   Choice c, c_x, c_w;
   uint32_t rows_each, row_blocks;
-  uint64_t x, w, dz, part, sums, total;
+  uint64_t x, w, dz, part, sums, sums_w, total;
 };
 
 bool in8(const pt_linear& l) { return l.x_scale != nullptr; }
@@ -513,7 +561,9 @@ Plan plan_grads(const pt_linear& l) {
   p.part = take(l.d_bias ? 4ull * p.row_blocks * p.Np : 0);
   if (l.d_x) p.c_x = choose(l.width, l.rows, p.Np / TWO);
   if (l.d_weight) p.c_w = choose(l.width, l.outs, (l.rows + TWO - 1) / TWO);
-  p.sums = take(std::max(p.c_x.bytes, p.c_w.bytes));
+  p.both = l.d_x && l.d_weight && p.c_x.kind != BIG && p.c_w.kind == MID;
+  p.sums = take(p.both ? p.c_x.bytes : std::max(p.c_x.bytes, p.c_w.bytes));
+  p.sums_w = p.both ? take(p.c_w.bytes) : p.sums;
   p.total = take.at;
   return p;
 }
@@ -564,18 +614,25 @@ template <int MUL, int DT, bool PK, bool QK, class E> int product(Kind k, const 
   return k == FEW ? product_of<MUL, DT, Few, PK, QK>(a, e, st) : k == MID ? product_of<MUL, DT, Mid, PK, QK>(a, e, st) : product_of<MUL, DT, Big, PK, QK>(a, e, st);
 }
 
+template <int DT, class C> int both(const ProductArgs& x, const Plain& ex, const ProductArgs& w, const Plain& ew, const BiasArgs& b, uint32_t bias_blocks, hipStream_t st) {
+  const uint32_t grid = split_grid(x.split);
+  hipLaunchKernelGGL((k_linear_both<DT, C>), dim3(grid + split_grid(w.split)), dim3(256), 0, st, x, ex, w, ew, grid);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_both");
+  const uint32_t jx = joiners<C>(x.split.tail), jw = joiners<Mid>(w.split.tail);
+  if (!(jx + jw + bias_blocks)) return PT_OK;
+  hipLaunchKernelGGL((k_linear_ends<DT, C>), dim3(jx + jw + bias_blocks), dim3(256), 0, st, x, ex, w, ew, b, jx, jw);
+  PT_LAUNCH_CHECK(nullptr, "k_linear_ends");
+  return PT_OK;
+}
+
 // The operand of rows as they lie, or as they have been copied.
 Operand rows_of(bool as_is, const void* at, uint64_t stride, uint32_t width, const void* copy, uint32_t pitch, uint32_t rows) {
   return as_is ? Operand{at, stride * 2, rows, width} : Operand{copy, 2ull * pitch, rows, pitch};
 }
-int copy(const void* from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch, void* to, hipStream_t st) {
-  hipLaunchKernelGGL(k_linear_copy, dim3((rows + 3) / 4), dim3(256), 0, st, (const uint16_t*)from, stride, rows, width, pitch, (uint16_t*)to);
+template <int BYTES> int copy(const CopyArgs& x, const CopyArgs& w, hipStream_t st) {
+  if (!x.rows && !w.rows) return PT_OK;
+  hipLaunchKernelGGL(k_linear_copy<BYTES>, dim3(copy_blocks(x) + copy_blocks(w)), dim3(256), 0, st, x, w);
   PT_LAUNCH_CHECK(nullptr, "k_linear_copy");
-  return PT_OK;
-}
-int copy8(const void* from, uint64_t stride, uint32_t rows, uint32_t width, uint32_t pitch, void* to, hipStream_t st) {
-  hipLaunchKernelGGL(k_linear_copy8, dim3((rows + 3) / 4), dim3(256), 0, st, (const uint8_t*)from, stride, rows, width, pitch * 2, (uint8_t*)to);
-  PT_LAUNCH_CHECK(nullptr, "k_linear_copy8");
   return PT_OK;
 }
 
@@ -597,11 +654,9 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
     const ThinArgs a = {(const char*)l.x, (const char*)l.weight, l.x_stride * bytes, l.weight_stride * bytes, l.rows, l.outs, l.width * bytes};
     return b8 ? thin<PT_E4M3, DT>(a, e, st) : thin<DT, DT>(a, e, st);
   }
-  const auto place = b8 ? copy8 : copy;
-  if (!p.x_direct)
-    if (int rc = place(l.x, l.x_stride, l.rows, l.width, p.Kd, ws + p.x, st); rc != PT_OK) return rc;
-  if (!p.w_direct)
-    if (int rc = place(l.weight, l.weight_stride, l.outs, l.width, p.Kd, ws + p.w, st); rc != PT_OK) return rc;
+  const uint32_t pitch = b8 ? 2 * p.Kd : p.Kd;
+  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, pitch, ws + p.x}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, pitch, ws + p.w};
+  if (int rc = b8 ? copy<1>(cx, cw, st) : copy<2>(cx, cw, st); rc != PT_OK) return rc;
   const uint32_t per = b8 ? 2 : 1;         // elements in a 16-bit word
   const ProductArgs a = {rows_of(p.w_direct, l.weight, l.weight_stride / per, l.width / per, ws + p.w, p.Kd, l.outs),
                          rows_of(p.x_direct, l.x, l.x_stride / per, l.width / per, ws + p.x, p.Kd, l.rows), l.outs, l.rows, p.Kd / TWO, (float*)(ws + p.sums),
@@ -610,42 +665,38 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
 }
 
 template <int DT> int run_grads(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
-  if (!p.x_direct)
-    if (int rc = copy(l.x, l.x_stride, l.rows, l.width, p.Kd, ws + p.x, st); rc != PT_OK) return rc;
-  if (!p.w_direct)
-    if (int rc = copy(l.weight, l.weight_stride, l.outs, l.width, p.Kd, ws + p.w, st); rc != PT_OK) return rc;
-  if (p.slope || l.d_bias) {
+  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, p.Kd, ws + p.x}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, p.Kd, ws + p.w};
+  const bool dz_wanted = p.slope && (l.d_x || l.d_weight);
+  if (dz_wanted || l.d_bias || l.d_gate) {
     const SlopeArgs a = {(const uint16_t*)l.d_out, l.act != PT_ACT_NONE || l.gate ? (const uint16_t*)l.pre : nullptr, (const uint16_t*)l.gate,
-                         p.slope && (l.d_x || l.d_weight) ? (uint16_t*)(ws + p.dz) : nullptr,
-                         l.gate ? (uint16_t*)l.d_gate : nullptr, l.d_bias ? (float*)(ws + p.part) : nullptr, l.d_out_stride, l.pre_stride, l.gate_stride,
-                         l.d_gate_stride, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4, l.rows, l.outs, p.Np, p.rows_each, l.act};
-    hipLaunchKernelGGL(k_linear_slope<DT>, dim3((p.Np + 511) / 512, p.row_blocks), dim3(256), 0, st, a);
+                         dz_wanted ? (uint16_t*)(ws + p.dz) : nullptr, (uint16_t*)l.d_gate, l.d_bias ? (float*)(ws + p.part) : nullptr, l.d_out_stride,
+                         l.pre_stride, l.gate_stride, l.d_gate_stride, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4, l.rows, l.outs, p.Np, p.rows_each,
+                         (p.Np + 511) / 512, l.act};
+    const uint32_t blocks = a.strips * p.row_blocks;
+    hipLaunchKernelGGL(k_linear_slope<DT>, dim3(blocks + copy_blocks(cx) + copy_blocks(cw)), dim3(256), 0, st, a, cx, cw, blocks);
     PT_LAUNCH_CHECK(nullptr, "k_linear_slope");
+  } else if (int rc = copy<2>(cx, cw, st); rc != PT_OK) {
+    return rc;
   }
-  if (l.d_bias) {
-    hipLaunchKernelGGL(k_columns<DT>, dim3((l.outs + 63) / 64), dim3(256), 0, st, (const float*)(ws + p.part), p.row_blocks, uint64_t(p.Np), l.outs,
-                       (uint16_t*)l.d_bias);
-    PT_LAUNCH_CHECK(nullptr, "k_columns");
+  const BiasArgs bias = {(const float*)(ws + p.part), p.row_blocks, p.Np, l.outs, (uint16_t*)l.d_bias};
+  const uint32_t bias_blocks = l.d_bias ? column_blocks(l.outs) : 0;
+  if (l.d_bias && !p.both) {
+    hipLaunchKernelGGL(k_linear_bias<DT>, dim3(bias_blocks), dim3(256), 0, st, bias);
+    PT_LAUNCH_CHECK(nullptr, "k_linear_bias");
   }
   const Operand dz = p.slope ? Operand{ws + p.dz, 2ull * p.Np, 0, 0} : Operand{l.d_out, 2 * l.d_out_stride, 0, 0};
   const uint32_t dz_width = p.slope ? p.Np : l.outs;
-  if (l.d_x) {
-    Operand w = rows_of(p.w_direct, l.weight, l.weight_stride, l.width, ws + p.w, p.Kd, 0);
-    w.extent = w.k;
-    w.k = l.outs;
-    const ProductArgs a = {w, {dz.at, dz.pitch, l.rows, dz_width}, l.width, l.rows, p.Np / TWO, (float*)(ws + p.sums), p.c_x.split};
-    const Plain e = {(uint16_t*)l.d_x, l.d_x_stride, l.width, l.rows};
-    if (int rc = product<DT, DT, false, true>(p.c_x.kind, a, e, st); rc != PT_OK) return rc;
-  }
-  if (l.d_weight) {
-    Operand x = rows_of(p.x_direct, l.x, l.x_stride, l.width, ws + p.x, p.Kd, 0);
-    x.extent = x.k;
-    x.k = l.rows;
-    const ProductArgs a = {x, {dz.at, dz.pitch, dz_width, l.rows}, l.width, l.outs, (l.rows + TWO - 1) / TWO, (float*)(ws + p.sums), p.c_w.split};
-    const Plain e = {(uint16_t*)l.d_weight, l.d_weight_stride, l.width, l.outs};
-    if (int rc = product<DT, DT, false, false>(p.c_w.kind, a, e, st); rc != PT_OK) return rc;
-  }
-  return PT_OK;
+  // of weight and x, k are their rows
+  const auto across = [](Operand o, uint32_t rows) { return Operand{o.at, o.pitch, o.k, rows}; };
+  const ProductArgs ax = {across(rows_of(p.w_direct, l.weight, l.weight_stride, l.width, ws + p.w, p.Kd, 0), l.outs), {dz.at, dz.pitch, l.rows, dz_width}, l.width, l.rows,
+                          p.Np / TWO, (float*)(ws + p.sums), p.c_x.split};
+  const ProductArgs aw = {across(rows_of(p.x_direct, l.x, l.x_stride, l.width, ws + p.x, p.Kd, 0), l.rows), {dz.at, dz.pitch, dz_width, l.rows}, l.width, l.outs,
+                          (l.rows + TWO - 1) / TWO, (float*)(ws + p.sums_w), p.c_w.split};
+  const Plain ex = {(uint16_t*)l.d_x, l.d_x_stride, l.width, l.rows}, ew = {(uint16_t*)l.d_weight, l.d_weight_stride, l.width, l.outs};
+  if (p.both) return p.c_x.kind == FEW ? both<DT, Few>(ax, ex, aw, ew, bias, bias_blocks, st) : both<DT, Mid>(ax, ex, aw, ew, bias, bias_blocks, st);
+  if (l.d_x)
+    if (int rc = product<DT, DT, false, true>(p.c_x.kind, ax, ex, st); rc != PT_OK) return rc;
+  return l.d_weight ? product<DT, DT, false, false>(p.c_w.kind, aw, ew, st) : int(PT_OK);
 }
 
 }  // namespace

@@ -7,7 +7,6 @@
 
 namespace pt_random {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr uint64_t PHI = 0x9E3779B97F4A7C15ull;
 
 __device__ __forceinline__ uint64_t mix64(uint64_t x) {
@@ -25,9 +24,11 @@ struct Drop {
   __device__ __forceinline__ uint64_t key() const { return off ? mix64(seed + (step ? *(const PT_GLOBAL uint64_t*)step : 0) * PHI) : 0; }
   // Element c (0 to 3) of the four that share word z: x scaled, or 0.
   __device__ __forceinline__ float of(uint64_t z, int c, float x) const { return (uint32_t(z >> (16 * c)) & 0xffffu) < off ? 0.0f : x * scale; }
-  __device__ __forceinline__ f32x4 of(uint64_t key, uint64_t word, f32x4 x) const {
-    const uint64_t z = mix64(key + (word + 1) * PHI);
-    return f32x4{of(z, 0, x[0]), of(z, 1, x[1]), of(z, 2, x[2]), of(z, 3, x[3])};
+  // Four elements whose word has the counter key + (word + 1) PHI.
+  __device__ __forceinline__ void apply(uint64_t counter, float* x) const {
+    const uint64_t z = mix64(counter);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) x[c] = of(z, c, x[c]);
   }
 };
 

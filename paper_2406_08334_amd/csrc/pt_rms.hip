@@ -221,6 +221,11 @@ __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rms_grads(const GradAr
   }
 }
 
+template <int DT>
+__global__ void __launch_bounds__(256) k_rms_gain(const float* part, uint32_t rows, uint64_t pitch, uint32_t width, uint16_t* out) {
+  add_columns<DT>(part, rows, pitch, width, out, blockIdx.x);
+}
+
 struct Rows8Args {
   const void* x;
   uint8_t* codes;
@@ -358,10 +363,10 @@ extern "C" int pt_rms_grads(const pt_rms* n, void* workspace, uint64_t workspace
       PT_LAUNCH_CHECK(nullptr, "k_rms_grads");
     }
     if (!n->d_gain) return int(PT_OK);
-    const dim3 columns((n->width + 63) / 64);
-    if (n->dtype == PT_BF16) hipLaunchKernelGGL(k_columns<PT_BF16>, columns, dim3(256), 0, st, a.part, part_rows, pitch, n->width, (uint16_t*)n->d_gain);
-    else hipLaunchKernelGGL(k_columns<PT_FP16>, columns, dim3(256), 0, st, a.part, part_rows, pitch, n->width, (uint16_t*)n->d_gain);
-    PT_LAUNCH_CHECK(nullptr, "k_columns");
+    const dim3 columns(column_blocks(n->width));
+    if (n->dtype == PT_BF16) hipLaunchKernelGGL(k_rms_gain<PT_BF16>, columns, dim3(256), 0, st, a.part, part_rows, pitch, n->width, (uint16_t*)n->d_gain);
+    else hipLaunchKernelGGL(k_rms_gain<PT_FP16>, columns, dim3(256), 0, st, a.part, part_rows, pitch, n->width, (uint16_t*)n->d_gain);
+    PT_LAUNCH_CHECK(nullptr, "k_rms_gain");
     return int(PT_OK);
   });
 }

@@ -93,20 +93,27 @@ __device__ __forceinline__ void store8b(PT_GLOBAL uint8_t* row, uint32_t m, uint
       if (m + q < d) row[m + q] = uint8_t(w[q / 4] >> (8 * (q & 3)));
 }
 
-// Sums of the columns of `rows` rows of partial sums, in a fixed order, to 16 bits: 64 columns a workgroup, a quarter of the rows a wave.
+// Sums of the columns of `rows` rows of partial sums, in a fixed order, to 16 bits, by a workgroup of 256: 16 columns, and of the rows a sixteenth a lane.
+// (64 columns a workgroup are few workgroups: 512 rows of 4096 in 6.2 us.)
+constexpr uint32_t COLUMNS = 16;
 template <int DT>
-__global__ void __launch_bounds__(256) k_columns(const float* __restrict__ part, uint32_t rows, uint64_t pitch, uint32_t width, uint16_t* __restrict__ out) {
-  __shared__ float s_x[4][64];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+__device__ __forceinline__ void add_columns(const float* part, uint32_t rows, uint64_t pitch, uint32_t width, uint16_t* out, uint32_t block) {
+  __shared__ float s_x[16][COLUMNS + 1];
+  const uint32_t c = block * COLUMNS + threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
   float x = 0.0f;
   if (c < width) {
     const PT_GLOBAL float* p = (const PT_GLOBAL float*)part + c;
 #pragma unroll 16
-    for (uint32_t r = wave; r < rows; r += 4) x += p[r * pitch];
+    for (uint32_t r = group; r < rows; r += 16) x += p[r * pitch];
   }
-  s_x[wave][lane] = x;
+  s_x[group][threadIdx.x % COLUMNS] = x;
   __syncthreads();
-  if (wave == 0 && c < width) ((PT_GLOBAL uint16_t*)out)[c] = uint16_t(encode16<DT>(((s_x[0][lane] + s_x[1][lane]) + s_x[2][lane]) + s_x[3][lane]));
+  if (threadIdx.x >= COLUMNS || c >= width) return;
+  x = s_x[0][threadIdx.x];
+#pragma unroll
+  for (int g = 1; g < 16; ++g) x += s_x[g][threadIdx.x];
+  ((PT_GLOBAL uint16_t*)out)[c] = uint16_t(encode16<DT>(x));
 }
+inline uint32_t column_blocks(uint32_t width) { return (width + COLUMNS - 1) / COLUMNS; }
 
 }  // namespace pt_rows_ops

@@ -126,10 +126,11 @@ __device__ __forceinline__ void leave(const T& t, int j, PT_GLOBAL float* sums) 
 constexpr uint32_t JOINERS = 2048;
 template <class C> inline uint32_t joiners(uint32_t tail) { return std::min<uint32_t>(JOINERS, tail * (C::BM * C::BN / 1024)); }
 template <class C, class F>
-__device__ __forceinline__ void join_tiles(const float* room, const Split& s, uint32_t tm, uint32_t tn, F&& f) {
+__device__ __forceinline__ void join_tiles(const float* room, const Split& s, uint32_t tm, uint32_t tn, F&& f, uint32_t block = blockIdx.x,
+                                           uint32_t blocks = gridDim.x) {
   constexpr uint32_t TILE = C::BM * C::BN;
   const size_t next = size_t(s.tail) * TILE;
-  for (uint32_t i = blockIdx.x; i < s.tail * (TILE / 1024); i += gridDim.x) {
+  for (uint32_t i = block; i < s.tail * (TILE / 1024); i += blocks) {
     const uint32_t j = i / (TILE / 1024), e = i % (TILE / 1024) * 1024 + threadIdx.x * 4;
     uint32_t m, n;
     tile_at(s.whole + j, tm, tn, m, n);
