@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(256) k_dropout(const DropArgs a) {
   if (a.residual) r = load8((const PT_GLOBAL uint16_t*)a.residual + row * a.residual_stride + at, 0, left);
   float y[8];
   drop8<DT>(a, key, word, q, r, y);
-  store8((PT_GLOBAL uint16_t*)a.out + row * a.out_stride + at, 0, left, encode8<DT>(y));
+  pass8((PT_GLOBAL uint16_t*)a.out + row * a.out_stride + at, 0, left, encode8<DT>(y));
 }
 
 }  // namespace

@@ -316,9 +316,11 @@ __global__ void __launch_bounds__(256) k_linear_ends(const ProductArgs x, const 
 template <int DT>
 __global__ void __launch_bounds__(256) k_linear_bias(const BiasArgs b) { add_columns<DT>(b.part, b.rows, b.pitch, b.outs, b.d_bias, blockIdx.x); }
 
-// Up to 16 rows: they take as long as the weight takes to read, which each wave has on its way straight into the registers that are multiplied: 16 outs a workgroup, of
-// which a wave takes 256 bytes of k in every WAVES times as many.  Any address, stride and width; no workspace.
-constexpr uint32_t THIN_ROWS = 16;
+// Up to 32 rows: they take as long as the weight takes to read, which each wave has on its way straight into the registers that are multiplied: 16 MT outs a workgroup, of
+// which a wave takes 64 U bytes of k in every WAVES times as many.  Any address, stride and width; no workspace.
+// (Before, tiles of Few: 1 x 4096 x 11008 34.7 -> 17.4 us, 5.2 TB/s; 17 rows 33.5 -> 22.4; 32 x 1600 x 6400 13.8 -> 8.4; but 32 x 11008 x 4096 28.0 -> 31.3: few outs and
+// many rows of long k are read as often as the weight.)
+inline bool thin(uint64_t rows, uint64_t outs, uint64_t bytes) { return rows <= 16 || (rows <= 32 && (outs > 6128 || bytes <= 16384)); }
 
 struct ThinArgs {
   const char *x, *weight;
@@ -337,43 +339,65 @@ __device__ __forceinline__ u32x4 end16(const PT_GLOBAL char* row, uint32_t at, u
   return q;
 }
 
-template <int MUL, int DT, int WAVES>
+template <int MUL, int DT, int MT, int RT, int U, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64) k_linear_thin(const ThinArgs a, const Layer e) {
-  constexpr uint32_t U = 4, CHUNK = U * 64;
-  __shared__ __attribute__((aligned(16))) f32x4 s_acc[WAVES][64];
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, g = lane >> 4, m0 = blockIdx.x * 16;
-  const PT_GLOBAL char* w = (const PT_GLOBAL char*)a.weight + min(m0 + l, a.outs - 1) * a.weight_pitch;
-  const PT_GLOBAL char* x = (const PT_GLOBAL char*)a.x + min(l, a.rows - 1) * a.x_pitch;
-  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr uint32_t CHUNK = U * 64;
+  constexpr int N = MT * RT;
+  __shared__ __attribute__((aligned(16))) f32x4 s_acc[WAVES][N][64];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, g = lane >> 4, m0 = blockIdx.x * (16 * MT);
+  const PT_GLOBAL char *w[MT], *x[RT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) w[i] = (const PT_GLOBAL char*)a.weight + min(m0 + i * 16 + l, a.outs - 1) * a.weight_pitch;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) x[i] = (const PT_GLOBAL char*)a.x + min(i * 16 + l, a.rows - 1) * a.x_pitch;
+  f32x4 acc[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const uint32_t whole = a.bytes / CHUNK;
-  u32x4 qw[U], qx[U];
-  const auto load = [&](uint32_t c) {
+  struct Step { u32x4 w[U][MT], x[U][RT]; } now, next;
+  const auto load = [&](Step& to, uint32_t c) {
+    const uint32_t at = c * CHUNK + g * 16;
 #pragma unroll
-    for (uint32_t u = 0; u < U; ++u) qw[u] = *(const PT_GLOBAL u32x4_b*)(w + c * CHUNK + u * 64 + g * 16);
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-    for (uint32_t u = 0; u < U; ++u) qx[u] = *(const PT_GLOBAL u32x4_b*)(x + c * CHUNK + u * 64 + g * 16);
+      for (int i = 0; i < MT; ++i) to.w[u][i] = *(const PT_GLOBAL u32x4_b*)(w[i] + at + u * 64);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) to.x[u][i] = *(const PT_GLOBAL u32x4_b*)(x[i] + at + u * 64);
+    }
   };
-  if (wave < whole) load(wave);
+  const auto multiply = [&](const Step& s, int u) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) acc[i * RT + j] = mfma<MUL>(__builtin_bit_cast(s16x8, s.w[u][i]), __builtin_bit_cast(s16x8, s.x[u][j]), acc[i * RT + j]);
+  };
+  if (wave < whole) load(next, wave);
 #pragma unroll 1
   for (uint32_t c = wave; c < whole; c += WAVES) {
-    u32x4 nw[U], nx[U];
+    now = next;
+    if (c + WAVES < whole) load(next, c + WAVES);
 #pragma unroll
-    for (uint32_t u = 0; u < U; ++u) { nw[u] = qw[u]; nx[u] = qx[u]; }
-    if (c + WAVES < whole) load(c + WAVES);
-#pragma unroll
-    for (uint32_t u = 0; u < U; ++u) acc = mfma<MUL>(__builtin_bit_cast(s16x8, nw[u]), __builtin_bit_cast(s16x8, nx[u]), acc);
+    for (int u = 0; u < U; ++u) multiply(now, u);
   }
   if (wave == whole % WAVES)               // what is left
 #pragma unroll 1
-    for (uint32_t at = whole * CHUNK; at < a.bytes; at += 64)
-      acc = mfma<MUL>(__builtin_bit_cast(s16x8, end16<MUL>(w, at + g * 16, a.bytes)), __builtin_bit_cast(s16x8, end16<MUL>(x, at + g * 16, a.bytes)), acc);
-  s_acc[wave][lane] = acc;
-  __syncthreads();
-  if (wave) return;
-  acc = s_acc[0][lane];
+    for (uint32_t at = whole * CHUNK; at < a.bytes; at += 64) {
 #pragma unroll
-  for (uint32_t k = 1; k < uint32_t(WAVES); ++k) acc += s_acc[k][lane];
-  e.template four<DT>(m0 + g * 4, l, acc);
+      for (int i = 0; i < MT; ++i) now.w[0][i] = end16<MUL>(w[i], at + g * 16, a.bytes);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) now.x[0][i] = end16<MUL>(x[i], at + g * 16, a.bytes);
+      multiply(now, 0);
+    }
+#pragma unroll
+  for (int i = 0; i < N; ++i) s_acc[wave][i][lane] = acc[i];
+  __syncthreads();
+#pragma unroll 1
+  for (uint32_t i = wave; i < uint32_t(N); i += WAVES) {
+    f32x4 sum = s_acc[0][i][lane];
+#pragma unroll
+    for (uint32_t k = 1; k < uint32_t(WAVES); ++k) sum += s_acc[k][i][lane];
+    e.template four<DT>(m0 + i / RT * 16 + g * 4, i % RT * 16 + l, sum);
+  }
 }
 
 // Rows whose beginnings, distances or ends the products cannot take: they load 16 bytes a lane past registers.
@@ -493,11 +517,12 @@ __global__ void __launch_bounds__(256) k_linear_zero(uint16_t* __restrict__ out,
 enum Kind { BIG, MID, FEW };
 struct Choice { Kind kind; Split split; uint64_t bytes; };
 
-// Which tiles a product of m x n is soonest done in (of Big's the last of m may be a narrower one), and how they are split.
-Choice choose(uint32_t m, uint32_t n, uint32_t twos) {
+// Which tiles a product of m x n is soonest done in (of Big's the last of m may be a narrower one), and how they are split.  layer: with an epilogue, which in Big nothing
+// else of its compute unit hides (8192 x 768 x 2304 57.7 us in Big, 50.1 in Mid; 4096 x 512 x 4096 28.1, 33.3).
+Choice choose(uint32_t m, uint32_t n, uint32_t twos, bool layer) {
   const auto of = [&](auto c, Kind kind) {
     typedef decltype(c) C;
-    const Split s = split<C>((m + C::BM - 1) / C::BM * ((n + C::BN - 1) / C::BN), twos);
+    const Split s = split<C>((m + C::BM - 1) / C::BM * ((n + C::BN - 1) / C::BN), twos, !layer ? 3000 : C::BM == 256 ? 12000 : 5000);
     return Choice{kind, s, 4ull * s.tail * s.n * C::BM * C::BN};
   };
   if (n <= uint32_t(Few::BN)) return of(Few{}, FEW);
@@ -529,13 +554,13 @@ struct Taker {
 
 Plan plan_out(const pt_linear& l) {
   Plan p{};
-  if (l.rows <= THIN_ROWS) return p;
   const uint32_t bytes = in8(l) ? 1 : 2;
+  if (thin(l.rows, l.outs, uint64_t(l.width) * bytes)) return p;
   Taker take;
   p.Kd = uint32_t(up(uint64_t(l.width) * bytes, 2 * TWO) / 2);
   p.x_direct = direct(l.x, l.x_stride, l.width, bytes);
   p.w_direct = direct(l.weight, l.weight_stride, l.width, bytes);
-  p.c = choose(l.outs, l.rows, p.Kd / TWO);
+  p.c = choose(l.outs, l.rows, p.Kd / TWO, true);
   p.x = take(p.x_direct ? 0 : 2ull * l.rows * p.Kd);
   p.w = take(p.w_direct ? 0 : 2ull * l.outs * p.Kd);
   p.sums = take(p.c.bytes);
@@ -559,8 +584,8 @@ Plan plan_grads(const pt_linear& l) {
   p.rows_each = std::max(p.rows_each, (l.rows + 65534) / 65535);
   p.row_blocks = (l.rows + p.rows_each - 1) / p.rows_each;
   p.part = take(l.d_bias ? 4ull * p.row_blocks * p.Np : 0);
-  if (l.d_x) p.c_x = choose(l.width, l.rows, p.Np / TWO);
-  if (l.d_weight) p.c_w = choose(l.width, l.outs, (l.rows + TWO - 1) / TWO);
+  if (l.d_x) p.c_x = choose(l.width, l.rows, p.Np / TWO, false);
+  if (l.d_weight) p.c_w = choose(l.width, l.outs, (l.rows + TWO - 1) / TWO, false);
   p.both = l.d_x && l.d_weight && p.c_x.kind != BIG && p.c_w.kind == MID;
   p.sums = take(p.both ? p.c_x.bytes : std::max(p.c_x.bytes, p.c_w.bytes));
   p.sums_w = p.both ? take(p.c_w.bytes) : p.sums;
@@ -636,25 +661,29 @@ template <int BYTES> int copy(const CopyArgs& x, const CopyArgs& w, hipStream_t 
   return PT_OK;
 }
 
-template <int MUL, int DT> int thin(const ThinArgs& a, const Layer& e, hipStream_t st) {
-  const uint32_t grid = (a.outs + 15) / 16;
-  if (grid >= 1024) hipLaunchKernelGGL((k_linear_thin<MUL, DT, 4>), dim3(grid), dim3(256), 0, st, a, e);
-  else if (grid >= 256) hipLaunchKernelGGL((k_linear_thin<MUL, DT, 8>), dim3(grid), dim3(512), 0, st, a, e);
-  else hipLaunchKernelGGL((k_linear_thin<MUL, DT, 16>), dim3(grid), dim3(1024), 0, st, a, e);
+template <int MUL, int DT, int MT, int RT, int U, int WAVES> int thin_of(const ThinArgs& a, const Layer& e, hipStream_t st) {
+  hipLaunchKernelGGL((k_linear_thin<MUL, DT, MT, RT, U, WAVES>), dim3((a.outs + 16 * MT - 1) / (16 * MT)), dim3(WAVES * 64), 0, st, a, e);
   PT_LAUNCH_CHECK(nullptr, "k_linear_thin");
   return PT_OK;
+}
+template <int MUL, int DT> int run_thin(const ThinArgs& a, const Layer& e, hipStream_t st) {
+  const uint32_t groups = (a.outs + 15) / 16;
+  if (a.rows <= 16) {
+    return groups >= 512 ? thin_of<MUL, DT, 1, 1, 2, 4>(a, e, st) : groups >= 256 ? thin_of<MUL, DT, 1, 1, 2, 8>(a, e, st) : thin_of<MUL, DT, 1, 1, 2, 16>(a, e, st);
+  }
+  return groups >= 640 ? thin_of<MUL, DT, 4, 2, 2, 8>(a, e, st) : groups >= 384 ? thin_of<MUL, DT, 2, 2, 2, 8>(a, e, st) : thin_of<MUL, DT, 1, 2, 2, 8>(a, e, st);
 }
 
 template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
   const bool b8 = in8(l);
   const Layer e = {(const uint16_t*)l.bias, (const uint16_t*)l.gate, (const uint16_t*)l.residual, (uint16_t*)l.pre, (uint16_t*)l.out, l.x_scale, l.weight_scale,
                    l.gate_stride, l.residual_stride, l.pre_stride, l.out_stride, l.outs, l.rows, l.act, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4};
-  if (l.rows <= THIN_ROWS) {
-    const uint32_t bytes = b8 ? 1 : 2;
+  const uint32_t bytes = b8 ? 1 : 2;
+  if (thin(l.rows, l.outs, uint64_t(l.width) * bytes)) {
     const ThinArgs a = {(const char*)l.x, (const char*)l.weight, l.x_stride * bytes, l.weight_stride * bytes, l.rows, l.outs, l.width * bytes};
-    return b8 ? thin<PT_E4M3, DT>(a, e, st) : thin<DT, DT>(a, e, st);
+    return b8 ? run_thin<PT_E4M3, DT>(a, e, st) : run_thin<DT, DT>(a, e, st);
   }
-  const uint32_t pitch = b8 ? 2 * p.Kd : p.Kd;
+  const uint32_t pitch = 2 * p.Kd / bytes;
   const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, pitch, ws + p.x}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, pitch, ws + p.w};
   if (int rc = b8 ? copy<1>(cx, cw, st) : copy<2>(cx, cw, st); rc != PT_OK) return rc;
   const uint32_t per = b8 ? 2 : 1;         // elements in a 16-bit word

@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rms(const NormArgs a) 
   uint32_t big = 0;
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    if (a.sum) store8((PT_GLOBAL uint16_t*)a.sum + r * a.sum_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
+    if (a.sum) pass8((PT_GLOBAL uint16_t*)a.sum + r * a.sum_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
     float g[8];
     if (a.gain) decode8<DT>(place8(qg[p], at + p * R::STEP, a.width), g);
 #pragma unroll
@@ -111,12 +111,12 @@ __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rms(const NormArgs a) 
   }
   if (!a.y_scale) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) store8((PT_GLOBAL uint16_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
+    for (int p = 0; p < PIECES; ++p) pass8((PT_GLOBAL uint16_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
     return;
   }
   const Scale8 s = scale8(row_max<WAVES>(big, s_big));
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) store8b((PT_GLOBAL uint8_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, codes8(v[p], s.inv));
+  for (int p = 0; p < PIECES; ++p) pass8b((PT_GLOBAL uint8_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, codes8(v[p], s.inv));
   if (at == 0) ((PT_GLOBAL float*)a.y_scale)[r] = s.scale;
 }
 
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rms_grads(const GradAr
         const float x = now.rstd * __builtin_fmaf(-c, s[j], t[j]);
         d[j] = a.d_sum ? d[j] + x : x;
       }
-      store8((PT_GLOBAL uint16_t*)a.d_x + r * a.d_x_stride, at + p * R::STEP, a.width, encode8<DT>(d));
+      pass8((PT_GLOBAL uint16_t*)a.d_x + r * a.d_x_stride, at + p * R::STEP, a.width, encode8<DT>(d));
     }
   }
   if (!a.part) return;
@@ -272,21 +272,35 @@ __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rows8(const Rows8Args 
     for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(v[p][j]) & 0x7fffffffu);
   const Scale8 s = scale8(row_max<WAVES>(big, s_big));
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) store8b((PT_GLOBAL uint8_t*)a.codes + r * a.codes_stride, at + p * R::STEP, a.width, codes8(v[p], s.inv));
+  for (int p = 0; p < PIECES; ++p) pass8b((PT_GLOBAL uint8_t*)a.codes + r * a.codes_stride, at + p * R::STEP, a.width, codes8(v[p], s.inv));
   if (at == 0) ((PT_GLOBAL float*)a.scale)[r] = s.scale;
 }
 
 // ---- host -----------------------------------------------------------------------------------------------
 
-// f: called with the waves that share a row of `width` and a lane's pieces of it, as constants.
+// f: called with the waves that share a row of `width` and a lane's pieces of it, as constants: as few waves as 32 elements a lane allow (no more than 16 where
+// sums over the rows are kept too), and no more idle lanes than that makes.
+template <int W, int P, class F> int with(F&& f) { return f(std::integral_constant<int, W>{}, std::integral_constant<int, P>{}); }
 template <class F> int by_width(uint32_t width, F&& f) {
-  if (width <= 512) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
-  if (width <= 1024) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
-  if (width <= 2048) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
-  if (width <= 4096) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-  if (width <= 8192) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
-  if (width <= 16384) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
-  return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+  if (width <= 512) return with<1, 1>(f);
+  if (width <= 1024) return with<1, 2>(f);
+  if (width <= 1536) return with<1, 3>(f);
+  if (width <= 2048) return with<1, 4>(f);
+  if (width <= 4096) return with<4, 2>(f);
+  if (width <= 6144) return with<4, 3>(f);
+  if (width <= 8192) return with<4, 4>(f);
+  if (width <= 16384) return with<16, 2>(f);
+  return with<16, 4>(f);
+}
+template <class F> int by_width_grads(uint32_t width, F&& f) {
+  if (width <= 512) return with<1, 1>(f);
+  if (width <= 1024) return with<1, 2>(f);
+  if (width <= 2048) return with<4, 1>(f);
+  if (width <= 4096) return with<4, 2>(f);
+  if (width <= 6144) return with<4, 3>(f);
+  if (width <= 8192) return with<8, 2>(f);
+  if (width <= 16384) return with<16, 2>(f);
+  return with<16, 4>(f);
 }
 template <int WAVES> uint32_t grid_of(uint32_t rows) { return (rows + Rows<WAVES>::PER - 1) / Rows<WAVES>::PER; }
 
@@ -295,7 +309,7 @@ template <int WAVES> uint32_t grads_grid(uint32_t rows) { return std::min(grid_o
 uint64_t grads_bytes(const pt_rms& n) {
   uint64_t bytes = 0;
   if (n.d_gain && n.rows)
-    by_width(n.width, [&](auto w, auto) { bytes = 4ull * grads_grid<w()>(n.rows) * Rows<w()>::PER * up(n.width, 8); return PT_OK; });
+    by_width_grads(n.width, [&](auto w, auto) { bytes = 4ull * grads_grid<w()>(n.rows) * Rows<w()>::PER * up(n.width, 8); return PT_OK; });
   return bytes;
 }
 
@@ -350,7 +364,7 @@ extern "C" int pt_rms_grads(const pt_rms* n, void* workspace, uint64_t workspace
   if (bytes > workspace_bytes)
     return pt_fail(nullptr, PT_ERR_NOMEM, "pt_rms_grads: a workspace of %llu bytes is too small (pt_rms_workspace)", (unsigned long long)workspace_bytes);
   hipStream_t st = (hipStream_t)stream;
-  return by_width(n->width, [&](auto w, auto p) {
+  return by_width_grads(n->width, [&](auto w, auto p) {
     typedef Rows<w()> R;
     const uint32_t grid = grads_grid<w()>(n->rows), part_rows = grid * R::PER;
     const uint64_t pitch = up(n->width, 8);

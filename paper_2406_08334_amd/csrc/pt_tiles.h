@@ -44,14 +44,15 @@ typedef Cfg<128, 64, 4, 1, 256, 1700> Few;
 // How the tiles of a gradient are done: `whole` by one workgroup each, and `tail`, those of the last round, by `n` each, which share its k and leave sums to
 // be added; and when they are done, in ns.  (512 x 4096 x 32000: 690 us without, 450 with; 1000 x 768 x 5000: 112, 76.)
 struct Split { uint32_t whole, tail, n; uint64_t ns; };
-template <class C> __host__ __device__ inline Split split(uint32_t tiles, uint32_t twos) {
-  const uint64_t round = uint64_t(twos) * C::TWO_NS + 3000;
+// over: ns of a tile beside its products.
+template <class C> __host__ __device__ inline Split split(uint32_t tiles, uint32_t twos, uint32_t over = 3000) {
+  const uint64_t round = uint64_t(twos) * C::TWO_NS + over;
   Split best = {tiles, 0, 1, (tiles + C::SLOTS - 1) / C::SLOTS * round};
   const uint32_t tail = tiles % C::SLOTS, whole = tiles - tail;
   if (!tail) return best;
   for (uint32_t n : {2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u, std::min(32u, uint32_t(C::SLOTS) / tail)}) {
     if (n < 2 || n * 2 > twos) continue;
-    const uint64_t ns = whole / C::SLOTS * round + (tail * n + C::SLOTS - 1) / C::SLOTS * (uint64_t((twos + n - 1) / n) * C::TWO_NS + 3000) +
+    const uint64_t ns = whole / C::SLOTS * round + (tail * n + C::SLOTS - 1) / C::SLOTS * (uint64_t((twos + n - 1) / n) * C::TWO_NS + over) +
                         uint64_t(tail) * n * C::PART_NS + 4000;
     if (ns < best.ns) best = {whole, tail, n, ns};
   }
