@@ -63,61 +63,75 @@ struct NormArgs {
   uint32_t rows, width;
 };
 
-template <int DT, int WAVES, int PIECES>
+// AHEAD: workgroups take rows one after the other, the next one's loads under way while one is worked on.  That is for 8 bits, whose second sum over the row
+// leaves the memory idle otherwise (16384 x 5120 fp16 117 -> 106 us with two workgroups a compute unit, 111 with four; 16 bits 124 -> 127).
+template <int DT, int WAVES, int PIECES, bool AHEAD>
 __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rms(const NormArgs a) {
   typedef Rows<WAVES> R;
-  __shared__ float s_sum[WAVES];
-  __shared__ uint32_t s_big[WAVES];
-  const uint32_t r = R::first(), at = R::lane_at();
-  if (r >= a.rows) return;
-  u32x4 qx[PIECES], qr[PIECES], qg[PIECES];
-  const PT_GLOBAL uint16_t* x = (const PT_GLOBAL uint16_t*)a.x + r * a.x_stride;
-#pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
-    qx[p] = fetch8(x, at + p * R::STEP, a.width);
-    if (a.residual) qr[p] = fetch8((const PT_GLOBAL uint16_t*)a.residual + r * a.residual_stride, at + p * R::STEP, a.width);
-  }
+  __shared__ float s_sum[2][WAVES];
+  __shared__ uint32_t s_big[2][WAVES];
+  const uint32_t first = R::first(), at = R::lane_at();
+  u32x4 qg[PIECES];
+  struct Row { u32x4 x[PIECES], r[PIECES]; } now, next;
 #pragma unroll
   for (int p = 0; p < PIECES; ++p)
     if (a.gain) qg[p] = fetch8((const PT_GLOBAL uint16_t*)a.gain, at + p * R::STEP, a.width);
-  float v[PIECES][8], sq = 0.0f;
+  const auto load = [&](Row& to, uint32_t r) {
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
-    decode8<DT>(place8(qx[p], at + p * R::STEP, a.width), v[p]);
-    if (a.residual) {
-      float b[8];
-      decode8<DT>(place8(qr[p], at + p * R::STEP, a.width), b);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[p][j] += b[j];
+    for (int p = 0; p < PIECES; ++p) {
+      to.x[p] = fetch8((const PT_GLOBAL uint16_t*)a.x + r * a.x_stride, at + p * R::STEP, a.width);
+      if (a.residual) to.r[p] = fetch8((const PT_GLOBAL uint16_t*)a.residual + r * a.residual_stride, at + p * R::STEP, a.width);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sq = __builtin_fmaf(v[p][j], v[p][j], sq);
-  }
-  sq = row_sum<WAVES>(sq, s_sum);
-  const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(sq, a.inv_width, a.eps));
-  if (a.rstd && at == 0) ((PT_GLOBAL float*)a.rstd)[r] = rstd;
-  uint32_t big = 0;
-#pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
-    if (a.sum) pass8((PT_GLOBAL uint16_t*)a.sum + r * a.sum_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
-    float g[8];
-    if (a.gain) decode8<DT>(place8(qg[p], at + p * R::STEP, a.width), g);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[p][j] *= rstd;
-      if (a.gain) v[p][j] *= g[j];
-      big = max(big, __float_as_uint(v[p][j]) & 0x7fffffffu);
+  };
+  if (first < a.rows) load(AHEAD ? next : now, first);
+  uint32_t odd = 0;
+  const uint32_t turn = gridDim.x * R::PER;
+  for (uint32_t r = first; r < a.rows; r += turn, odd ^= 1) {
+    if constexpr (AHEAD) {
+      now = next;
+      if (r + turn < a.rows) load(next, r + turn);
     }
-  }
-  if (!a.y_scale) {
+    float v[PIECES][8], sq = 0.0f;
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) pass8((PT_GLOBAL uint16_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
-    return;
-  }
-  const Scale8 s = scale8(row_max<WAVES>(big, s_big));
+    for (int p = 0; p < PIECES; ++p) {
+      decode8<DT>(place8(now.x[p], at + p * R::STEP, a.width), v[p]);
+      if (a.residual) {
+        float b[8];
+        decode8<DT>(place8(now.r[p], at + p * R::STEP, a.width), b);
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) pass8b((PT_GLOBAL uint8_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, codes8(v[p], s.inv));
-  if (at == 0) ((PT_GLOBAL float*)a.y_scale)[r] = s.scale;
+        for (int j = 0; j < 8; ++j) v[p][j] += b[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sq = __builtin_fmaf(v[p][j], v[p][j], sq);
+    }
+    sq = row_sum<WAVES>(sq, s_sum[odd]);
+    const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(sq, a.inv_width, a.eps));
+    if (a.rstd && at == 0) ((PT_GLOBAL float*)a.rstd)[r] = rstd;
+    uint32_t big = 0;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      if (a.sum) pass8((PT_GLOBAL uint16_t*)a.sum + r * a.sum_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
+      float g[8];
+      if (a.gain) decode8<DT>(place8(qg[p], at + p * R::STEP, a.width), g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[p][j] *= rstd;
+        if (a.gain) v[p][j] *= g[j];
+        big = max(big, __float_as_uint(v[p][j]) & 0x7fffffffu);
+      }
+    }
+    if (!a.y_scale) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) pass8((PT_GLOBAL uint16_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, encode8<DT>(v[p]));
+      if constexpr (AHEAD) continue;
+      else return;
+    }
+    const Scale8 s = scale8(row_max<WAVES>(big, s_big[odd]));
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) pass8b((PT_GLOBAL uint8_t*)a.y + r * a.y_stride, at + p * R::STEP, a.width, codes8(v[p], s.inv));
+    if (at == 0) ((PT_GLOBAL float*)a.y_scale)[r] = s.scale;
+    if constexpr (!AHEAD) return;
+  }
 }
 
 struct GradArgs {
@@ -135,7 +149,7 @@ struct GradArgs {
 template <int DT, int WAVES, int PIECES>
 __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rms_grads(const GradArgs a) {
   typedef Rows<WAVES> R;
-  constexpr bool AHEAD = WAVES < 16;
+  constexpr bool AHEAD = WAVES * PIECES <= 16;
   __shared__ float s_sum[2][WAVES];
   const uint32_t first = R::first(), at = R::lane_at();
   struct Row {
@@ -299,17 +313,18 @@ template <class F> int by_width_grads(uint32_t width, F&& f) {
   if (width <= 4096) return with<4, 2>(f);
   if (width <= 6144) return with<4, 3>(f);
   if (width <= 8192) return with<8, 2>(f);
-  if (width <= 16384) return with<16, 2>(f);
+  if (width <= 16384) return with<8, 4>(f);
   return with<16, 4>(f);
 }
 template <int WAVES> uint32_t grid_of(uint32_t rows) { return (rows + Rows<WAVES>::PER - 1) / Rows<WAVES>::PER; }
 
-// Workgroups of the gradients: two to a compute unit, each with a row of partial sums of the gain's gradient for every row it works on at a time.
-template <int WAVES> uint32_t grads_grid(uint32_t rows) { return std::min(grid_of<WAVES>(rows), 512u); }
+// Workgroups of the gradients: as many as run at a time, each with a row of partial sums of the gain's gradient for every row it works on at a time.  (8192 x 4096 by 512
+// 53.2 us, 256 63.1, 768 61.8; 8192 x 1600 by 512 26.9, 256 40.3; 2048 x 16384 by 256 72.3, 512 82.9, 1024 104.5.)
+template <int WAVES> uint32_t grads_grid(uint32_t rows, uint32_t width) { return std::min(grid_of<WAVES>(rows), width > 8192 ? 256u : 512u); }
 uint64_t grads_bytes(const pt_rms& n) {
   uint64_t bytes = 0;
   if (n.d_gain && n.rows)
-    by_width_grads(n.width, [&](auto w, auto) { bytes = 4ull * grads_grid<w()>(n.rows) * Rows<w()>::PER * up(n.width, 8); return PT_OK; });
+    by_width_grads(n.width, [&](auto w, auto) { bytes = 4ull * grads_grid<w()>(n.rows, n.width) * Rows<w()>::PER * up(n.width, 8); return PT_OK; });
   return bytes;
 }
 
@@ -344,9 +359,21 @@ extern "C" int pt_rms_norm(const pt_rms* n, void* stream) {
   const NormArgs a = {(const uint16_t*)n->x, (const uint16_t*)n->residual, (const uint16_t*)n->gain, (uint16_t*)n->sum, n->rstd, n->y, n->y_scale,
                       n->x_stride, n->residual_stride, n->sum_stride, n->y_stride, float(n->eps), 1.0f / float(n->width), n->rows, n->width};
   return by_width(n->width, [&](auto w, auto p) {
-    const dim3 grid(grid_of<w()>(n->rows)), block(Rows<w()>::THREADS);
-    if (n->dtype == PT_BF16) hipLaunchKernelGGL((k_rms<PT_BF16, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((k_rms<PT_FP16, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
+    constexpr uint32_t TWO_A_UNIT = 512;
+    const uint32_t grid = grid_of<w()>(n->rows);
+    const bool ahead = w() == 4 && n->y_scale && grid >= 8 * TWO_A_UNIT;
+    const dim3 block(Rows<w()>::THREADS);
+    const auto launch = [&](auto dt) {
+      if constexpr (w() == 4) {
+        if (ahead) {
+          hipLaunchKernelGGL((k_rms<dt(), w(), p(), true>), dim3(TWO_A_UNIT), block, 0, (hipStream_t)stream, a);
+          return;
+        }
+      }
+      hipLaunchKernelGGL((k_rms<dt(), w(), p(), false>), dim3(grid), block, 0, (hipStream_t)stream, a);
+    };
+    if (n->dtype == PT_BF16) launch(std::integral_constant<int, PT_BF16>{});
+    else launch(std::integral_constant<int, PT_FP16>{});
     PT_LAUNCH_CHECK(nullptr, "k_rms");
     return int(PT_OK);
   });
@@ -366,7 +393,7 @@ extern "C" int pt_rms_grads(const pt_rms* n, void* workspace, uint64_t workspace
   hipStream_t st = (hipStream_t)stream;
   return by_width_grads(n->width, [&](auto w, auto p) {
     typedef Rows<w()> R;
-    const uint32_t grid = grads_grid<w()>(n->rows), part_rows = grid * R::PER;
+    const uint32_t grid = grads_grid<w()>(n->rows, n->width), part_rows = grid * R::PER;
     const uint64_t pitch = up(n->width, 8);
     const GradArgs a = {(const uint16_t*)sum, (const uint16_t*)n->gain, (const uint16_t*)n->d_y, (const uint16_t*)n->d_sum, n->rstd, (uint16_t*)n->d_x,
                         n->d_gain ? (float*)workspace : nullptr, n->sum ? n->sum_stride : n->x_stride, n->d_y_stride, n->d_sum_stride, n->d_x_stride, pitch,
