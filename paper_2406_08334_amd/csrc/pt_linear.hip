@@ -13,6 +13,7 @@ namespace {
 
 // ---- activations ------------------------------------------------------------------------------------------
 
+constexpr int ANY = -1;      // of activations: whichever the call says
 constexpr float LOG2E = 1.44269504088896340736f, TANH_2A = 1.59576912160573071176f, TANH_B = 0.044715f;       // 2 sqrt(2 / pi)
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -LOG2E)); }
@@ -82,7 +83,7 @@ struct Plain {
   uint64_t stride;
   uint32_t extent_m, extent_n;
 
-  template <int DT, class T>
+  template <int DT, int ACT, class C, class T>
   __device__ __forceinline__ void tile(const T& t, uint32_t m0, uint32_t n0, lds_char*, lds_char*) const {
     const uint32_t lane = threadIdx.x & 63, mw = m0 + t.wave_m();
 #pragma unroll
@@ -144,12 +145,14 @@ struct Layer {
   };
   __device__ __forceinline__ uint64_t counter(uint32_t m, uint32_t n) const { return drop.key() + (n * words + m / 4 + 1) * pt_random::PHI; }
   // From there to the result; g, r: gate and residual; counter: of the first four's random numbers.
-  template <int N>
+  template <int ACT, int N>
   __device__ __forceinline__ void result(float (&y)[N], uint64_t counter, const float (&g)[N], const float (&r)[N]) const {
-    with_act(act, [&](auto a) {
+    const auto each = [&](auto a) {
 #pragma unroll
       for (int q = 0; q < N; ++q) y[q] = ::act<a()>(y[q]);
-    });
+    };
+    if constexpr (ACT == ANY) with_act(act, each);
+    else each(std::integral_constant<int, ACT>{});
     if (gate) {
 #pragma unroll
       for (int q = 0; q < N; ++q) y[q] *= g[q];
@@ -164,11 +167,67 @@ struct Layer {
     }
   }
 
+  // A tile all of which there is, on its sums where they are: four of consecutive outs of a row and of the 16 outs behind, exchanged for eight as arrays are read and
+  // written.  For one activation: five of 64 sums each do not fit the instruction cache.  (Through LDS, as at the edges: 8192 x 1600 x 6144 167.7 us instead of
+  // 149.4, of which the products 127; 8192 x 4096 x 8192 434, 410; but with a gate, which is read in pieces of lines then, 8192 x 4096 x 11008 671, 690.)
+  template <int DT, int ACT, class T>
+  __device__ __forceinline__ void whole(const T& t, uint32_t m0, uint32_t n0) const {
+    constexpr int PAIRS = T::FM / 2, PARTS = PAIRS * T::FN;
+    typedef f32x4 f32x4_a __attribute__((aligned(4)));
+    const uint32_t lane = threadIdx.x & 63, mw = m0 + t.wave_m(), mb = mw + (lane >> 4) * 4, n = n0 + t.wave_n() + (lane & 15), m8 = mw + eight_at();
+    const uint64_t from = drop.off ? counter(mb, n) : 0, row_step = words * pt_random::PHI;
+    u32x4 qr = {0, 0, 0, 0};
+    const auto at = [&](const uint16_t* x, uint64_t stride, int part) { return (PT_GLOBAL u32x4_a*)((PT_GLOBAL uint16_t*)x + (n + part / PAIRS * 16) * stride + m8 + part % PAIRS * 32); };
+    const auto fetch = [&](int part) {
+      if (residual) qr = *at(residual, residual_stride, part);
+    };
+    fetch(0);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+      const int i = part % PAIRS * 2, j = part / PAIRS;
+      const u32x4 now_r = qr;
+      if (part + 1 < PARTS) fetch(part + 1);
+      f32x4 x[2] = {t.acc[i][j], t.acc[i + 1][j]};
+      if (x_scale) {
+        const float s = ((const PT_GLOBAL float*)x_scale)[n + j * 16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[h] = x[h] * s * *(const PT_GLOBAL f32x4_a*)((const PT_GLOBAL float*)weight_scale + mb + (i + h) * 16);
+      }
+      if (bias) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[h] += decode4<DT>(*(const PT_GLOBAL u32x2_a*)((const PT_GLOBAL uint16_t*)bias + mb + (i + h) * 16));
+      }
+      if (pre) *at(pre, pre_stride, part) = eight(encode16x4<DT>(x[0]), encode16x4<DT>(x[1]));
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[h][q] = ::act<ACT>(x[h][q]);
+      if (drop.off) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint64_t z = pt_random::mix64(from + j * 16 * row_step + (i + h) * 4 * pt_random::PHI);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[h][q] = drop.of(z, q, x[h][q]);
+        }
+      }
+      if (residual) {                                      // the exchange is its own inverse
+        const u32x4 y = eight(u32x2{now_r.x, now_r.y}, u32x2{now_r.z, now_r.w});
+        x[0] += decode4<DT>(u32x2{y.x, y.y});
+        x[1] += decode4<DT>(u32x2{y.z, y.w});
+      }
+      *at(out, out_stride, part) = eight(encode16x4<DT>(x[0]), encode16x4<DT>(x[1]));
+      __builtin_amdgcn_sched_barrier(0);                   // there are no registers for more than that at a time
+    }
+  }
+
   // A wave's sums go through LDS, 16 rows at a time, so that a lane has eight outs of a row, the lanes of a row all that the wave has of it, and what is loaded
   // and stored is whole lines; in a loop, as four times five activations of 128 sums a lane would not fit the instruction cache.  What is loaded for a
   // turn is under way during the one before.  The wave's own part of the buffers: 16 bytes of piece c of row n at c ^ n.
-  template <int DT, class T>
-  __device__ __forceinline__ void tile(const T& t, uint32_t m0, uint32_t n0, lds_char* even, lds_char* odd) const {
+  template <int DT, int ACT, class C, class T>
+  __device__ __forceinline__ void tile(T& t, uint32_t m0, uint32_t n0, lds_char* even, lds_char* odd) const {
+    if constexpr (ACT != ANY && T::TM * C::WM == C::BM) {  // not a narrower one
+      if (!gate && m0 + C::BM <= extent_m && n0 + C::BN <= extent_n) return whole<DT, ACT>(t, m0, n0);
+    }
     constexpr uint32_t TM = T::TM, ROW = TM * 4, LANES = TM / 8, STEP = 64 / LANES, TURNS = 16 / STEP, G = TURNS < 2 ? 1 : 2, WAVES = T::THREADS / 64;
     static_assert(TM >= 32 && (WAVES + 1) / 2 * 16 * ROW <= T::BYTES, "the waves' parts fit the buffers");
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
@@ -220,7 +279,7 @@ struct Layer {
         if (pre) store8((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode8<DT>(y));
         if (gate) decode8<DT>(place8(now_g[turn], m, extent_m), g);
         if (residual) decode8<DT>(place8(now_r[turn], m, extent_m), b);
-        result(y, from + (it * G + turn) * STEP * row_step, g, b);
+        result<ACT>(y, from + (it * G + turn) * STEP * row_step, g, b);
         store8((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode8<DT>(y));
       }
     }
@@ -240,7 +299,7 @@ struct Layer {
     columns.load(*this, m);
     columns.z(*this, x_scale ? ((const PT_GLOBAL float*)x_scale)[n] : 1.0f, y);
     if (pre) store4((PT_GLOBAL uint16_t*)pre + n * pre_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
-    result(y, drop.off ? counter(m, n) : 0, g, r);
+    result<ANY>(y, drop.off ? counter(m, n) : 0, g, r);
     store4((PT_GLOBAL uint16_t*)out + n * out_stride, m, extent_m, encode16x4<DT>(f32x4{y[0], y[1], y[2], y[3]}));
   }
 };
@@ -255,7 +314,7 @@ struct ProductArgs {
 };
 
 // MUL: PT_BF16, PT_FP16 or PT_E4M3, what is multiplied; DT: what the epilogue reads and writes.
-template <int MUL, int DT, class C, bool PK, bool QK, class E>
+template <int MUL, int DT, int ACT, class C, bool PK, bool QK, class E>
 __device__ __forceinline__ void product_tile(const ProductArgs& a, const E& e, lds_char* even, lds_char* odd, uint32_t block) {
   uint32_t tm, tn, part;
   PT_GLOBAL float* left;
@@ -269,15 +328,15 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, const E& e, l
       for (int j = 0; j < T::FN; ++j) leave<C>(t, j, left);
       return;
     }
-    e.template tile<DT>(t, tm * C::BM, tn * C::BN, even, odd);
+    e.template tile<DT, ACT, C>(t, tm * C::BM, tn * C::BN, even, odd);
   });
 }
 
-template <int MUL, int DT, class C, bool PK, bool QK, class E>
+template <int MUL, int DT, int ACT, class C, bool PK, bool QK, class E>
 __global__ void __launch_bounds__(C::THREADS) k_linear_product(const ProductArgs a, const E e) {
   constexpr int BYTES = C::template Of<MUL, PK, QK>::BYTES;
   __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
-  product_tile<MUL, DT, C, PK, QK>(a, e, (lds_char*)even, (lds_char*)odd, blockIdx.x);
+  product_tile<MUL, DT, ACT, C, PK, QK>(a, e, (lds_char*)even, (lds_char*)odd, blockIdx.x);
 }
 
 template <int DT, class C, class E>
@@ -296,8 +355,8 @@ __global__ void __launch_bounds__(256) k_linear_both(const ProductArgs x, const 
   static_assert(C::THREADS == 256 && Mid::THREADS == 256, "one launch");
   constexpr int BYTES = std::max(C::template Of<DT, false, true>::BYTES, Mid::Of<DT, false, false>::BYTES);
   __shared__ __attribute__((aligned(16))) char even[BYTES], odd[BYTES];
-  if (blockIdx.x < blocks_x) product_tile<DT, DT, C, false, true>(x, ex, (lds_char*)even, (lds_char*)odd, blockIdx.x);
-  else product_tile<DT, DT, Mid, false, false>(w, ew, (lds_char*)even, (lds_char*)odd, blockIdx.x - blocks_x);
+  if (blockIdx.x < blocks_x) product_tile<DT, DT, ANY, C, false, true>(x, ex, (lds_char*)even, (lds_char*)odd, blockIdx.x);
+  else product_tile<DT, DT, ANY, Mid, false, false>(w, ew, (lds_char*)even, (lds_char*)odd, blockIdx.x - blocks_x);
 }
 
 // What is left of the gradients: sums of several workgroups a tile, and of the bias's columns.
@@ -628,7 +687,11 @@ int check_workspace(uint64_t need, const void* workspace, uint64_t bytes, const 
 
 // Launches.
 template <int MUL, int DT, class C, bool PK, bool QK, class E> int product_of(const ProductArgs& a, const E& e, hipStream_t st) {
-  hipLaunchKernelGGL((k_linear_product<MUL, DT, C, PK, QK, E>), dim3(split_grid(a.split)), dim3(C::THREADS), 0, st, a, e);
+  const auto launch = [&](auto act) {
+    hipLaunchKernelGGL((k_linear_product<MUL, DT, act(), C, PK, QK, E>), dim3(split_grid(a.split)), dim3(C::THREADS), 0, st, a, e);
+  };
+  if constexpr (std::is_same_v<E, Layer> && C::BM == 256) with_act(e.act, launch);
+  else launch(std::integral_constant<int, ANY>{});
   PT_LAUNCH_CHECK(nullptr, "k_linear_product");
   if (!a.split.tail) return PT_OK;
   hipLaunchKernelGGL((k_linear_join<DT, C, E>), dim3(joiners<C>(a.split.tail)), dim3(256), 0, st, a, e);
