@@ -569,7 +569,7 @@ typedef struct {
 
 /* Bytes of workspace of the two calls (for arrays as they are given: operands that do not begin at multiples of 16 bytes, lie at odd strides
  * or have widths that are no multiple of 64 are copied into it first); either pointer may be NULL.  Host only.  PT_ERR_UNSUPPORTED: more than
- * 2^25 rows, 2^21 outs or a width over 2^20, or more than 2^30 tiles of 128 x 128 in a product. */
+ * 2^25 rows, 2^21 outs or a width over 2^20, or 2^24 tiles of 128 x 128 or more in a product. */
 int pt_linear_workspace(const pt_linear* layer, uint64_t* out_bytes, uint64_t* grads_bytes);
 
 /* workspace: device, 256-byte aligned, of at least those bytes (else PT_ERR_NOMEM); its contents are of no use afterwards; may be NULL where
@@ -582,7 +582,8 @@ int pt_linear_grads(const pt_linear* layer, void* workspace, uint64_t workspace_
  * in fp32, s unrounded.  Gradients, from sum (x where there is no residual), rstd, gain, d_y and d_sum, the gradient that reaches the sum
  * on its other ways:
  *     t = d_y gain     d_x = d_sum + rstd (t - sum rstd^2 mean_k(t sum))  (x's and residual's)     d_gain_k = sum_r d_y sum rstd
- * An output in 8 bits has the gradient of one in 16. */
+ * An output in 8 bits has the gradient of one in 16.  Squares are in fp32's range up to magnitudes of 1e19 / sqrt(width); a row of zeros needs an
+ * eps above 0, else its y is NaN. */
 typedef struct {
   const void* x;         /* device, [rows, width] 16-bit elements                                      */
   const void* residual;  /* device, [rows, width], or NULL: 0                                          */
@@ -628,7 +629,7 @@ typedef struct {
   void* out;                 /* device, [rows, width], written                               */
   uint64_t x_stride, residual_stride, out_stride;
   pt_drop drop;
-  uint32_t rows, width;      /* rows times ceil(width / 8) up to 2^32 - 1                    */
+  uint32_t rows, width;      /* rows times ceil(width / 8) up to 2^32 - 1024                 */
   int32_t dtype;
   int32_t reserved;
 } pt_dropped;

@@ -75,7 +75,8 @@ extern "C" int pt_dropout(const pt_dropped* d, void* stream) {
   if (((uintptr_t)d->x | (uintptr_t)d->out | (uintptr_t)d->residual) % 2 != 0 || (uintptr_t)d->drop.step % 8 != 0)
     return pt_fail(nullptr, PT_ERR_ALIGNMENT, "pt_dropout: an array is not aligned to its elements");
   const uint64_t pieces = (uint64_t(d->width) + 7) / 8;
-  if (d->rows * pieces > 0xffffffffull) return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "pt_dropout: more than 2^32 - 1 pieces of eight elements");
+  if (d->rows * pieces > 0xfffffc00ull)     // a lane each, of which a grid has less than 2^32
+    return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "pt_dropout: more than 2^32 - 1024 pieces of eight elements");
   if (!d->rows) return PT_OK;
   DropArgs a = {(const uint16_t*)d->x, (const uint16_t*)d->residual, (uint16_t*)d->out, d->x_stride, d->residual_stride, d->out_stride,
                 pt_random::make(d->drop), d->rows * pieces, d->width, uint32_t(pieces), 0};

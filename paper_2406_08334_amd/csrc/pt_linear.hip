@@ -670,9 +670,9 @@ int check(const pt_linear* l, const char* who) {
   if (!l->x_scale) a |= (uintptr_t)l->x | (uintptr_t)l->weight;
   if (a % 2 != 0 || ((uintptr_t)l->x_scale | (uintptr_t)l->weight_scale) % 4 != 0 || (uintptr_t)l->drop.step % 8 != 0)
     return pt_fail(nullptr, PT_ERR_ALIGNMENT, "%s: an array is not aligned to its elements", who);
-  const auto tiles = [](uint64_t m, uint64_t n) { return ((m + 127) / 128) * ((n + 63) / 64); };
+  const auto tiles = [](uint64_t m, uint64_t n) { return ((m + 127) / 128) * ((n + 127) / 128); };
   if (l->rows > (1u << 25) || l->outs > (1u << 21) || l->width > (1u << 20) ||
-      std::max({tiles(l->outs, l->rows), tiles(l->width, l->rows), tiles(l->width, l->outs)}) > (1u << 30))
+      std::max({tiles(l->outs, l->rows), tiles(l->width, l->rows), tiles(l->width, l->outs)}) >= (1u << 24))
     return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "%s: more than 2^25 rows, 2^21 outs, a width over 2^20 or too many tiles", who);
   return PT_OK;
 }

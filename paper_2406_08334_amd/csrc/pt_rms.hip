@@ -16,6 +16,7 @@ using namespace pt_rows_ops;
 namespace {
 
 constexpr uint32_t MOST_WIDTH = 32768;
+constexpr uint32_t MOST_ROWS = 1u << 21;   // of a launch: 2^32 lanes are more than a grid may have
 
 // Sum of x, and largest of `big`, over the lanes that share a row.
 template <int WAVES>
@@ -328,6 +329,23 @@ uint64_t grads_bytes(const pt_rms& n) {
   return bytes;
 }
 
+template <int DT> int norm_rows(const NormArgs& a, hipStream_t st) {
+  return by_width(a.width, [&](auto w, auto p) {
+    constexpr uint32_t TWO_A_UNIT = 512;
+    const uint32_t grid = grid_of<w()>(a.rows);
+    if constexpr (w() == 4) {
+      if (a.y_scale && grid >= 8 * TWO_A_UNIT) {
+        hipLaunchKernelGGL((k_rms<DT, w(), p(), true>), dim3(TWO_A_UNIT), dim3(Rows<w()>::THREADS), 0, st, a);
+        PT_LAUNCH_CHECK(nullptr, "k_rms");
+        return int(PT_OK);
+      }
+    }
+    hipLaunchKernelGGL((k_rms<DT, w(), p(), false>), dim3(grid), dim3(Rows<w()>::THREADS), 0, st, a);
+    PT_LAUNCH_CHECK(nullptr, "k_rms");
+    return int(PT_OK);
+  });
+}
+
 int check(const pt_rms* n, const char* who) {
   if (!n) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: norm is NULL", who);
   if (n->dtype != PT_BF16 && n->dtype != PT_FP16) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: dtype %d is neither PT_BF16 nor PT_FP16", who, n->dtype);
@@ -356,27 +374,15 @@ extern "C" int pt_rms_norm(const pt_rms* n, void* stream) {
   if (int rc = check(n, "pt_rms_norm"); rc != PT_OK) return rc;
   if (!n->rows) return PT_OK;
   if (!n->x || !n->y) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_rms_norm: NULL array");
-  const NormArgs a = {(const uint16_t*)n->x, (const uint16_t*)n->residual, (const uint16_t*)n->gain, (uint16_t*)n->sum, n->rstd, n->y, n->y_scale,
-                      n->x_stride, n->residual_stride, n->sum_stride, n->y_stride, float(n->eps), 1.0f / float(n->width), n->rows, n->width};
-  return by_width(n->width, [&](auto w, auto p) {
-    constexpr uint32_t TWO_A_UNIT = 512;
-    const uint32_t grid = grid_of<w()>(n->rows);
-    const bool ahead = w() == 4 && n->y_scale && grid >= 8 * TWO_A_UNIT;
-    const dim3 block(Rows<w()>::THREADS);
-    const auto launch = [&](auto dt) {
-      if constexpr (w() == 4) {
-        if (ahead) {
-          hipLaunchKernelGGL((k_rms<dt(), w(), p(), true>), dim3(TWO_A_UNIT), block, 0, (hipStream_t)stream, a);
-          return;
-        }
-      }
-      hipLaunchKernelGGL((k_rms<dt(), w(), p(), false>), dim3(grid), block, 0, (hipStream_t)stream, a);
-    };
-    if (n->dtype == PT_BF16) launch(std::integral_constant<int, PT_BF16>{});
-    else launch(std::integral_constant<int, PT_FP16>{});
-    PT_LAUNCH_CHECK(nullptr, "k_rms");
-    return int(PT_OK);
-  });
+  for (uint64_t r = 0; r < n->rows; r += MOST_ROWS) {
+    const auto row = [&](const void* x, uint64_t stride) { return x ? (uint16_t*)x + r * stride : nullptr; };
+    const NormArgs a = {row(n->x, n->x_stride), row(n->residual, n->residual_stride), (const uint16_t*)n->gain, row(n->sum, n->sum_stride),
+                        n->rstd ? n->rstd + r : nullptr, n->y_scale ? (void*)((uint8_t*)n->y + r * n->y_stride) : row(n->y, n->y_stride),
+                        n->y_scale ? n->y_scale + r : nullptr, n->x_stride, n->residual_stride, n->sum_stride, n->y_stride, float(n->eps),
+                        1.0f / float(n->width), uint32_t(std::min<uint64_t>(MOST_ROWS, n->rows - r)), n->width};
+    if (int rc = n->dtype == PT_BF16 ? norm_rows<PT_BF16>(a, (hipStream_t)stream) : norm_rows<PT_FP16>(a, (hipStream_t)stream); rc != PT_OK) return rc;
+  }
+  return PT_OK;
 }
 
 extern "C" int pt_rms_grads(const pt_rms* n, void* workspace, uint64_t workspace_bytes, void* stream) {
@@ -424,13 +430,18 @@ extern "C" int pt_rows8(const pt_rows* d, void* stream) {
     return pt_fail(nullptr, PT_ERR_ALIGNMENT, "pt_rows8: an array is not aligned to its elements");
   if (d->width > MOST_WIDTH || d->rows > (1u << 30)) return pt_fail(nullptr, PT_ERR_UNSUPPORTED, "pt_rows8: a width over %u or more than 2^30 rows", MOST_WIDTH);
   if (!d->rows) return PT_OK;
-  const Rows8Args a = {d->x, (uint8_t*)d->codes, d->scale, d->x_stride, d->codes_stride, d->rows, d->width};
-  return by_width(d->width, [&](auto w, auto p) {
-    const dim3 grid(grid_of<w()>(d->rows)), block(Rows<w()>::THREADS);
-    if (d->type == PT_BF16) hipLaunchKernelGGL((k_rows8<PT_BF16, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
-    else if (d->type == PT_FP16) hipLaunchKernelGGL((k_rows8<PT_FP16, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((k_rows8<PT_FP32, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
-    PT_LAUNCH_CHECK(nullptr, "k_rows8");
-    return int(PT_OK);
-  });
+  for (uint64_t r = 0; r < d->rows; r += MOST_ROWS) {
+    const Rows8Args a = {(const char*)d->x + r * d->x_stride * (d->type == PT_FP32 ? 4 : 2), (uint8_t*)d->codes + r * d->codes_stride, d->scale + r, d->x_stride,
+                         d->codes_stride, uint32_t(std::min<uint64_t>(MOST_ROWS, d->rows - r)), d->width};
+    const int rc = by_width(d->width, [&](auto w, auto p) {
+      const dim3 grid(grid_of<w()>(a.rows)), block(Rows<w()>::THREADS);
+      if (d->type == PT_BF16) hipLaunchKernelGGL((k_rows8<PT_BF16, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
+      else if (d->type == PT_FP16) hipLaunchKernelGGL((k_rows8<PT_FP16, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
+      else hipLaunchKernelGGL((k_rows8<PT_FP32, w(), p()>), grid, block, 0, (hipStream_t)stream, a);
+      PT_LAUNCH_CHECK(nullptr, "k_rows8");
+      return int(PT_OK);
+    });
+    if (rc != PT_OK) return rc;
+  }
+  return PT_OK;
 }

@@ -213,3 +213,23 @@ def test_no_rows():
     B.pt_rms_grads(d, torch.empty(max(1, B.pt_rms_workspace(d)), dtype=torch.uint8, device="cuda"))
     torch.cuda.synchronize()
     assert not bool(dg.any())
+
+
+def test_more_rows_than_a_launch_takes():
+    """The rows behind the first 2^21, in their places."""
+    rows, width = (1 << 21) + 77, 9
+    x = torch.randn(rows, width, device="cuda").bfloat16()
+    y, rstd = torch.empty_like(x), torch.empty(rows, device="cuda")
+    y8, codes = (torch.empty(rows, width, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ys, scale = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    s = torch.empty_like(x)
+    B.pt_rms_norm(B.rms(x, y, residual=x, sum=s, rstd=rstd))
+    B.pt_rms_norm(B.rms(x, y8, residual=x, y_scale=ys))
+    B.pt_rows8(B.rows8(x, codes, scale))
+    torch.cuda.synchronize()
+    want_s, want_r, want, err = ref.rms(x, x, None, 1e-5)
+    ref.within("rstd", rstd, want_r, err * want_r)
+    ref.within("sum", s, want_s, ref.rounding(want_s, x.dtype) * 1.001)
+    ref.within("y", y, want, err * want.abs() + ref.rounding(want, x.dtype) * 1.001)
+    ref.codes_within("y8", y8, ys, want, err * want.abs())
+    ref.codes_within("codes", codes, scale, x.double(), torch.zeros_like(want))

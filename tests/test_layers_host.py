@@ -27,7 +27,7 @@ def refused(status, *calls):
         assert str(e.value)
 
 
-LINEAR = dict(x=0x1000, weight=0x2000, out=0x3000, pre=0x4000, gate=0x5000, d_out=0x6000, d_x=0x7000, d_weight=0x8000, d_bias=0x9000, d_gate=0xa000, rows=10,
+LINEAR = dict(x=0x1000, weight=0x2000, out=0x3000, pre=0x4000, gate=0x5000, d_out=0x6000, d_x=0x7000, d_weight=0x8000, d_bias=0x9000, d_gate=0xa000, rows=100,
               outs=100, width=60, x_stride=64, weight_stride=64, gate_stride=100, residual_stride=100, pre_stride=100, out_stride=100, d_out_stride=100,
               d_x_stride=64, d_weight_stride=64, d_gate_stride=100, act=B.PT_ACT["silu"])
 
@@ -48,7 +48,7 @@ def test_a_layer_that_is_refused(change, status):
 
 def test_what_each_call_of_a_layer_needs():
     out, grads = B.pt_linear_workspace(made(B.pt_linear, LINEAR, {}))
-    assert out > 0 and grads > 0
+    assert out > 0 and grads > 0 and B.pt_linear_workspace(made(B.pt_linear, LINEAR, dict(rows=16)))[0] == 0      # few rows: none is needed
     room = torch.empty(1 << 20, dtype=torch.uint8)
     for change in (dict(x=0), dict(weight=0), dict(out=0)):
         refused(ARG, lambda: B.pt_linear_out(made(B.pt_linear, LINEAR, change), room, 0))
