@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(256) k_linear_join(const ProductArgs a, const 
   join_product<DT, C>(a, e, blockIdx.x, gridDim.x);
 }
 
-// Both gradients in one launch, where neither fills the chip for long: 1531 x 771 x 3083 in 24 us, one after the other 20 + 21.  C: the tiles of d_x.
+// Both gradients in one launch, where neither fills the chip for long: 1531 x 771 x 3083 in 29 us, one after the other 21 + 22 and a gap.  C: the tiles of d_x.
 template <int DT, class C>
 __global__ void __launch_bounds__(256) k_linear_both(const ProductArgs x, const Plain ex, const ProductArgs w, const Plain ew, uint32_t blocks_x) {
   static_assert(C::THREADS == 256 && Mid::THREADS == 256, "one launch");
@@ -528,10 +528,13 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a, const C
         if (a.gate) qg = fetch8((const PT_GLOBAL uint16_t*)a.gate + r * a.gate_stride, c, a.outs);
         float e[8], z[8], g[8], slope[8];
         decode8<DT>(place8(qe, c, a.outs), e);
-        if (a.drop.off) {
+        // last of all, so that what is dropped adds nothing, whatever pre and gate hold there
+        const uint64_t z0 = a.drop.off ? pt_random::mix64(from + r * row_step) : 0, z1 = a.drop.off ? pt_random::mix64(from + r * row_step + pt_random::PHI) : 0;
+        const auto drop = [&](float (&x)[8]) {
+          if (!a.drop.off) return;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) a.drop.apply(from + r * row_step + h * pt_random::PHI, e + 4 * h);
-        }
+          for (int j = 0; j < 8; ++j) x[j] = a.drop.of(j < 4 ? z0 : z1, j & 3, x[j]);
+        };
         if (a.pre) {
           decode8<DT>(place8(qz, c, a.outs), z);
 #pragma unroll
@@ -539,6 +542,7 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a, const C
           if (a.d_gate) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) z[j] *= e[j];
+            drop(z);
             store8((PT_GLOBAL uint16_t*)a.d_gate + r * a.d_gate_stride, c, a.outs, encode8<DT>(z));
           }
 #pragma unroll
@@ -549,6 +553,7 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a, const C
 #pragma unroll
           for (int j = 0; j < 8; ++j) e[j] *= g[j];
         }
+        drop(e);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (c + j >= a.outs) e[j] = 0.0f;

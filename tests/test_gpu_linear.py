@@ -203,6 +203,8 @@ def test_what_a_dropped_element_holds_reaches_nothing():
         g = case(rows, 64, 96, act="silu", gate=True, drop=0.5, grads=True)
         want = ref.linear_grads(g)
         g["d_out"][off] = float("inf")
+        g["pre"][off] = float("nan")
+        g["gate"][off] = float("-inf")
         call(g, True)
         for name, (v, b) in want.items():
             ref.within(name, g[name], v, b)
