@@ -114,6 +114,7 @@ struct Layer {
   int act;
   pt_random::Drop drop;
   uint64_t words;            // of random numbers in a row
+  bool direct;               // whole tiles on their sums where they are
 
   // z of N outs of row n from their sums: scales in 8 bits and bias, of the outs m on.
   template <int DT, int N> struct Columns {
@@ -169,7 +170,8 @@ struct Layer {
 
   // A tile all of which there is, on its sums where they are: four of consecutive outs of a row and of the 16 outs behind, exchanged for eight as arrays are read and
   // written.  For one activation: five of 64 sums each do not fit the instruction cache.  (Through LDS, as at the edges: 8192 x 1600 x 6144 167.7 us instead of
-  // 149.4, of which the products 127; 8192 x 4096 x 8192 434, 410; but with a gate, which is read in pieces of lines then, 8192 x 4096 x 11008 671, 690.)
+  // 149.4, of which the products 127; 8192 x 4096 x 8192 434, 410; but with a gate, which is read in
+  // pieces of lines then, 8192 x 4096 x 11008 671, 690; rows at odd addresses 8192 x 1600 x 6401 174, 188, with a residual 8192 x 768 x 3083 68, 83.)
   template <int DT, int ACT, class T>
   __device__ __forceinline__ void whole(const T& t, uint32_t m0, uint32_t n0) const {
     constexpr int PAIRS = T::FM / 2, PARTS = PAIRS * T::FN;
@@ -226,7 +228,7 @@ struct Layer {
   template <int DT, int ACT, class C, class T>
   __device__ __forceinline__ void tile(T& t, uint32_t m0, uint32_t n0, lds_char* even, lds_char* odd) const {
     if constexpr (ACT != ANY && T::TM * C::WM == C::BM) {  // not a narrower one
-      if (!gate && m0 + C::BM <= extent_m && n0 + C::BN <= extent_n) return whole<DT, ACT>(t, m0, n0);
+      if (direct && m0 + C::BM <= extent_m && n0 + C::BN <= extent_n) return whole<DT, ACT>(t, m0, n0);
     }
     constexpr uint32_t TM = T::TM, ROW = TM * 4, LANES = TM / 8, STEP = 64 / LANES, TURNS = 16 / STEP, G = TURNS < 2 ? 1 : 2, WAVES = T::THREADS / 64;
     static_assert(TM >= 32 && (WAVES + 1) / 2 * 16 * ROW <= T::BYTES, "the waves' parts fit the buffers");
@@ -744,8 +746,11 @@ template <int MUL, int DT> int run_thin(const ThinArgs& a, const Layer& e, hipSt
 
 template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
   const bool b8 = in8(l);
+  // where a gate is not read and rows begin at multiples of 16 bytes (in pieces of lines: whole)
+  const bool direct = !l.gate && ((uintptr_t)l.out | (uintptr_t)l.pre | (uintptr_t)l.residual) % 16 == 0 &&
+                      ((l.out_stride | (l.pre ? l.pre_stride : 0) | (l.residual ? l.residual_stride : 0)) % 8 == 0);
   const Layer e = {(const uint16_t*)l.bias, (const uint16_t*)l.gate, (const uint16_t*)l.residual, (uint16_t*)l.pre, (uint16_t*)l.out, l.x_scale, l.weight_scale,
-                   l.gate_stride, l.residual_stride, l.pre_stride, l.out_stride, l.outs, l.rows, l.act, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4};
+                   l.gate_stride, l.residual_stride, l.pre_stride, l.out_stride, l.outs, l.rows, l.act, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4, direct};
   const uint32_t bytes = b8 ? 1 : 2;
   if (thin(l.rows, l.outs, uint64_t(l.width) * bytes)) {
     const ThinArgs a = {(const char*)l.x, (const char*)l.weight, l.x_stride * bytes, l.weight_stride * bytes, l.rows, l.outs, l.width * bytes};

@@ -114,6 +114,23 @@ def test_large_tiles(rows, width, outs):
     check(c)
 
 
+# one round of 256 x 256 tiles and a few of 64 x 256 at the end of the outs; rows at multiples of 16 bytes (stored from the sums) or not (through LDS)
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("dtype,pad,shift,more", [("bf16", 4, 0, dict(residual=True, drop=0.1)), ("fp16", 4, 8, dict()), ("bf16", 4, 0, dict(gate=True)),
+                                                  ("fp16", 0, 1, dict(residual=True, drop=0.5, gate=True))])
+def test_every_epilogue_of_the_largest_tiles(dtype, pad, shift, more, act):
+    c = case(4096, 1024, 4100, dtype, act=act, bias=True, pad=pad, shift=shift, **more)
+    call(c)
+    check(c)
+
+
+@pytest.mark.parametrize("act,dtype,more", [("none", "bf16", dict(pad=4)), ("gelu", "fp16", dict(pad=4, residual=True, drop=0.1)), ("silu", "bf16", dict(gate=True))])
+def test_8_bits_in_the_largest_tiles(act, dtype, more):
+    c = case(4096, 2048, 4100, dtype, act=act, bias=True, bits=8, **more)
+    call(c)
+    check(c)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("rows,width,outs", SIZES)
 def test_grads_against_64_bits(rows, width, outs, dtype):
