@@ -313,7 +313,14 @@ struct ProductArgs {
   uint32_t extent_m, extent_n, twos;
   float* sums;
   Split split;
+  bool low;                  // of d_x: rows LOW on are what rounding the rows LOW before has left
 };
+
+// Up to LOW rows what rounding dz leaves is multiplied as rows of its own, which lie LOW behind, in tiles that have room for them.  It is of few rows and outs that single
+// roundings show: gradients of one row and 64 outs would have up to 2.1 times the error of rounding the result alone (of many rows 1.4).  1 x 4096 x 11008 56.5 -> 60.2
+// us, 16 x 4096 x 11008 59.1 -> 61.1, as x is copied and dz twice as long.
+constexpr uint32_t LOW = 32;
+static_assert(Few::BN == 2 * LOW, "both in a tile");
 
 // MUL: PT_BF16, PT_FP16 or PT_E4M3, what is multiplied; DT: what the epilogue reads and writes.
 template <int MUL, int DT, int ACT, class C, bool PK, bool QK, class E>
@@ -325,6 +332,14 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, const E& e, l
   with_tile<MUL, C, PK, QK>(a.extent_m - tm * C::BM, [&](auto t) {
     typedef decltype(t) T;
     t.run(even, odd, a.p, a.q, tm * C::BM, tn * C::BN, t0 * TWO, t1 - t0);
+    if constexpr (C::BN == 2 * LOW && !PK) {
+      if (a.low) {
+#pragma unroll
+        for (int j = 0; j < T::FN / 2; ++j)
+#pragma unroll
+          for (int i = 0; i < T::FM; ++i) t.acc[i][j] += t.acc[i][j + T::FN / 2];
+      }
+    }
     if (left) {
 #pragma unroll
       for (int j = 0; j < T::FN; ++j) leave<C>(t, j, left);
@@ -467,6 +482,7 @@ struct CopyArgs {
   uint64_t stride;
   uint32_t rows, width, pitch;             // elements; pitch: of a copied row, which is zero behind its end
   void* to;
+  uint32_t low;                            // 0, or how many rows there are: they go to rows 0 on and to rows LOW on, zero up to LOW and 2 LOW (rows is that then)
 };
 inline uint32_t copy_blocks(const CopyArgs& a) { return (a.rows + 3) / 4; }
 // Of one or two bytes an element, four rows by a workgroup of 256.
@@ -475,7 +491,8 @@ __device__ __forceinline__ void copy_rows(const CopyArgs& a, uint32_t block) {
   const uint32_t r = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
   if (r >= a.rows) return;
   if constexpr (BYTES == 2) {
-    copy_row((const PT_GLOBAL uint16_t*)a.from + r * a.stride, (PT_GLOBAL uint16_t*)a.to + size_t(r) * a.pitch, a.width, a.pitch, lane, 64);
+    const uint32_t from = a.low ? r % LOW : r;
+    copy_row((const PT_GLOBAL uint16_t*)a.from + from * a.stride, (PT_GLOBAL uint16_t*)a.to + size_t(r) * a.pitch, a.low && from >= a.low ? 0 : a.width, a.pitch, lane, 64);
   } else {
     const PT_GLOBAL char* row = (const PT_GLOBAL char*)a.from + r * a.stride;
     PT_GLOBAL char* to = (PT_GLOBAL char*)a.to + size_t(r) * a.pitch;
@@ -503,6 +520,7 @@ struct SlopeArgs {
   uint64_t words;
   uint32_t rows, outs, pitch, rows_each, strips;       // strips of 512 columns
   int act;
+  bool low;                  // 2 LOW rows of dz
 };
 
 // 512 columns, eight a lane, of rows_each rows, a quarter of which is a wave's.  Bound by memory.  The last workgroups copy what has to be copied of the
@@ -518,13 +536,18 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a, const C
   __shared__ float s_part[4][512];
   const uint32_t by = blockIdx.x / a.strips, bx = blockIdx.x - by * a.strips;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = bx * 512 + lane * 8;
-  const uint32_t first = by * a.rows_each, end = min(a.rows, first + a.rows_each);
+  const uint32_t first = by * a.rows_each, end = min(a.low ? LOW : a.rows, first + a.rows_each);
   const uint64_t from = a.drop.key() + (c / 4 + 1) * pt_random::PHI, row_step = a.words * pt_random::PHI;
   float sum[8] = {};
   if (c < a.pitch)
     with_act(a.act, [&](auto act) {
       for (uint32_t r = first + wave; r < end; r += 4) {
         u32x4 qe = {0, 0, 0, 0}, qz = qe, qg = qe;
+        if (r >= a.rows) {                                 // of 2 LOW
+          *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.dz + size_t(r) * a.pitch + c) = qe;
+          *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.dz + size_t(r + LOW) * a.pitch + c) = qe;
+          continue;
+        }
         qe = fetch8((const PT_GLOBAL uint16_t*)a.d_out + r * a.d_out_stride, c, a.outs);
         if (a.pre) qz = fetch8((const PT_GLOBAL uint16_t*)a.pre + r * a.pre_stride, c, a.outs);
         if (a.gate) qg = fetch8((const PT_GLOBAL uint16_t*)a.gate + r * a.gate_stride, c, a.outs);
@@ -561,7 +584,17 @@ __global__ void __launch_bounds__(256) k_linear_slope(const SlopeArgs a, const C
           if (c + j >= a.outs) e[j] = 0.0f;
           sum[j] += e[j];
         }
-        if (a.dz) *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.dz + size_t(r) * a.pitch + c) = encode8<DT>(e);
+        if (a.dz) {
+          const u32x4 w = encode8<DT>(e);
+          *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.dz + size_t(r) * a.pitch + c) = w;
+          if (a.low) {
+            float y[8];
+            decode8<DT>(w, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = __builtin_fabsf(y[j]) < __builtin_inff() ? e[j] - y[j] : 0.0f;       // inf stays inf
+            *(PT_GLOBAL u32x4*)((PT_GLOBAL uint16_t*)a.dz + size_t(r + LOW) * a.pitch + c) = encode8<DT>(y);
+          }
+        }
       }
     });
   if (!a.part) return;
@@ -605,6 +638,8 @@ bool direct(const void* at, uint64_t stride, uint32_t width, uint32_t bytes) {
 struct Plan {
   bool x_direct, w_direct, slope;          // slope: dz is not d_out
   bool both;                               // gradients in one launch
+  bool low;                                // as in ProductArgs
+  uint32_t rows;                           // of dz and the x that is multiplied with it
   uint32_t Kd, Np;                         // width and outs rounded up to whole steps (Kd in 16-bit words)
   Choice c, c_x, c_w;
   uint32_t rows_each, row_blocks;
@@ -639,19 +674,22 @@ Plan plan_grads(const pt_linear& l) {
   Taker take;
   p.Kd = uint32_t(up(l.width, TWO));
   p.Np = uint32_t(up(l.outs, TWO));
-  p.x_direct = !l.d_weight || direct(l.x, l.x_stride, l.width, 2);
+  const bool rounds = l.act != PT_ACT_NONE || l.gate || l.drop.p > 0.0;
+  p.low = rounds && l.rows <= LOW && (l.d_x || l.d_weight);
+  p.rows = p.low ? 2 * LOW : l.rows;
+  p.x_direct = !l.d_weight || (!p.low && direct(l.x, l.x_stride, l.width, 2));
   p.w_direct = !l.d_x || direct(l.weight, l.weight_stride, l.width, 2);
-  p.slope = l.act != PT_ACT_NONE || l.gate || l.drop.p > 0.0 || !direct(l.d_out, l.d_out_stride, l.outs, 2);
-  p.x = take(p.x_direct ? 0 : 2ull * l.rows * p.Kd);
+  p.slope = rounds || !direct(l.d_out, l.d_out_stride, l.outs, 2);
+  p.x = take(p.x_direct ? 0 : 2ull * p.rows * p.Kd);
   p.w = take(p.w_direct ? 0 : 2ull * l.outs * p.Kd);
-  p.dz = take(p.slope ? 2ull * l.rows * p.Np : 0);
+  p.dz = take(p.slope ? 2ull * p.rows * p.Np : 0);
   const uint32_t strips = (p.Np + 511) / 512;
   p.rows_each = std::max(16u, std::min(256u, uint32_t(uint64_t(l.rows) * strips / 2048)));
   p.rows_each = std::max(p.rows_each, (l.rows + 65534) / 65535);
-  p.row_blocks = (l.rows + p.rows_each - 1) / p.rows_each;
+  p.row_blocks = ((p.low ? LOW : l.rows) + p.rows_each - 1) / p.rows_each;
   p.part = take(l.d_bias ? 4ull * p.row_blocks * p.Np : 0);
-  if (l.d_x) p.c_x = choose(l.width, l.rows, p.Np / TWO, false);
-  if (l.d_weight) p.c_w = choose(l.width, l.outs, (l.rows + TWO - 1) / TWO, false);
+  if (l.d_x) p.c_x = choose(l.width, p.rows, p.Np / TWO, false);
+  if (l.d_weight) p.c_w = choose(l.width, l.outs, (p.rows + TWO - 1) / TWO, false);
   // of few rows both are a matter of reading the weight or writing its gradient: side by side (16 x 4096 x 11008 61.0 -> 53.6 us, 3 x 12796 x 2624 84.8 -> 66.2)
   if (l.d_x && l.d_weight && p.c_x.kind == FEW && p.c_w.kind == BIG)
     p.c_w = {MID, {(l.width + Mid::BM - 1) / Mid::BM * ((l.outs + Mid::BN - 1) / Mid::BN), 0, 1, 0}, 0};
@@ -760,23 +798,24 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
     return b8 ? run_thin<PT_E4M3, DT>(a, e, st) : run_thin<DT, DT>(a, e, st);
   }
   const uint32_t pitch = 2 * p.Kd / bytes;
-  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, pitch, ws + p.x}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, pitch, ws + p.w};
+  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, pitch, ws + p.x, 0}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, pitch, ws + p.w, 0};
   if (int rc = b8 ? copy<1>(cx, cw, st) : copy<2>(cx, cw, st); rc != PT_OK) return rc;
   const uint32_t per = b8 ? 2 : 1;         // elements in a 16-bit word
   const ProductArgs a = {rows_of(p.w_direct, l.weight, l.weight_stride / per, l.width / per, ws + p.w, p.Kd, l.outs),
                          rows_of(p.x_direct, l.x, l.x_stride / per, l.width / per, ws + p.x, p.Kd, l.rows), l.outs, l.rows, p.Kd / TWO, (float*)(ws + p.sums),
-                         p.c.split};
+                         p.c.split, false};
   return b8 ? product<PT_E4M3, DT, true, true>(p.c.kind, a, e, st) : product<DT, DT, true, true>(p.c.kind, a, e, st);
 }
 
 template <int DT> int run_grads(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
-  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, p.Kd, ws + p.x}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, p.Kd, ws + p.w};
+  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : p.rows, l.width, p.Kd, ws + p.x, p.low ? l.rows : 0};
+  const CopyArgs cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, p.Kd, ws + p.w, 0};
   const bool dz_wanted = p.slope && (l.d_x || l.d_weight);
   if (dz_wanted || l.d_bias || l.d_gate) {
     const SlopeArgs a = {(const uint16_t*)l.d_out, l.act != PT_ACT_NONE || l.gate ? (const uint16_t*)l.pre : nullptr, (const uint16_t*)l.gate,
                          dz_wanted ? (uint16_t*)(ws + p.dz) : nullptr, (uint16_t*)l.d_gate, l.d_bias ? (float*)(ws + p.part) : nullptr, l.d_out_stride,
                          l.pre_stride, l.gate_stride, l.d_gate_stride, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4, l.rows, l.outs, p.Np, p.rows_each,
-                         (p.Np + 511) / 512, l.act};
+                         (p.Np + 511) / 512, l.act, p.low};
     const uint32_t blocks = a.strips * p.row_blocks;
     hipLaunchKernelGGL(k_linear_slope<DT>, dim3(blocks + copy_blocks(cx) + copy_blocks(cw)), dim3(256), 0, st, a, cx, cw, blocks);
     PT_LAUNCH_CHECK(nullptr, "k_linear_slope");
@@ -793,10 +832,10 @@ template <int DT> int run_grads(const pt_linear& l, const Plan& p, char* ws, hip
   const uint32_t dz_width = p.slope ? p.Np : l.outs;
   // of weight and x, k are their rows
   const auto across = [](Operand o, uint32_t rows) { return Operand{o.at, o.pitch, o.k, rows}; };
-  const ProductArgs ax = {across(rows_of(p.w_direct, l.weight, l.weight_stride, l.width, ws + p.w, p.Kd, 0), l.outs), {dz.at, dz.pitch, l.rows, dz_width}, l.width, l.rows,
-                          p.Np / TWO, (float*)(ws + p.sums), p.c_x.split};
-  const ProductArgs aw = {across(rows_of(p.x_direct, l.x, l.x_stride, l.width, ws + p.x, p.Kd, 0), l.rows), {dz.at, dz.pitch, dz_width, l.rows}, l.width, l.outs,
-                          (l.rows + TWO - 1) / TWO, (float*)(ws + p.sums_w), p.c_w.split};
+  const ProductArgs ax = {across(rows_of(p.w_direct, l.weight, l.weight_stride, l.width, ws + p.w, p.Kd, 0), l.outs), {dz.at, dz.pitch, p.rows, dz_width}, l.width, p.rows,
+                          p.Np / TWO, (float*)(ws + p.sums), p.c_x.split, p.low};
+  const ProductArgs aw = {across(rows_of(p.x_direct, l.x, l.x_stride, l.width, ws + p.x, p.Kd, 0), p.rows), {dz.at, dz.pitch, dz_width, p.rows}, l.width, l.outs,
+                          (p.rows + TWO - 1) / TWO, (float*)(ws + p.sums_w), p.c_w.split, false};
   const Plain ex = {(uint16_t*)l.d_x, l.d_x_stride, l.width, l.rows}, ew = {(uint16_t*)l.d_weight, l.d_weight_stride, l.width, l.outs};
   if (p.both) return p.c_x.kind == FEW ? both<DT, Few>(ax, ex, aw, ew, bias, bias_blocks, st) : both<DT, Mid>(ax, ex, aw, ew, bias, bias_blocks, st);
   if (l.d_x)

@@ -133,7 +133,8 @@ def linear_grads(c):
     out["d_bias"] = (dz.sum(0), None)
     bound = ddz.sum(0) + (R + 64) * E * dz.abs().sum(0)
     out["d_bias"] = (dz.sum(0), bound + rounding(dz.sum(0), dt) * 1.001)
-    ddz = ddz + rounding(dz, dt)
+    # up to 32 rows what rounding dz leaves is multiplied as well, and rounded itself
+    ddz = ddz + rounding(dz, dt) * (unit(dt)[0] if R <= 32 else 1.0) + unit(dt)[1] * unit(dt)[0]
     for name, a, b, da, n in (("d_x", dz, w, ddz, N), ("d_weight", dz.t(), x, ddz.t(), R)):
         v = a @ b
         bound = da @ b.abs() + (n + 64) * E * (a.abs() @ b.abs())

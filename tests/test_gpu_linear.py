@@ -147,6 +147,25 @@ def test_grads_of_large_tiles(rows, width, outs):
     check(c, True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,outs", [(1, 64, 64), (2, 96, 64), (31, 200, 130), (32, 64, 1000), (7, 4096, 65), (16, 77, 2048), (33, 64, 64)])
+def test_grads_of_few_rows_have_one_rounding(rows, width, outs, dtype):
+    """Up to 32 rows the bound has no term for rounding dz but its square."""
+    for k in range(3):
+        c = case(rows, width, outs, dtype, act=("gelu", "silu", "none")[k], gate=k != 0, drop=0.2 * k, grads=True, seed=k)
+        call(c, True)
+        check(c, True)
+
+
+def test_grads_beyond_the_type_stay_infinite():
+    for rows in (3, 40):
+        c = case(rows, 64, 96, "fp16", gate=True, grads=True)
+        c["d_out"][1, 5], c["gate"][1, 5] = 60000.0, 8.0
+        call(c, True)
+        assert bool(c["d_bias"][5].isinf()) and bool(c["d_x"][1].float().abs().isinf().all())
+        assert bool(c["d_x"][[0, 2]].isfinite().all()) and bool(c["d_weight"][[4, 6]].isfinite().all())
+
+
 @pytest.mark.parametrize("what", ["d_x", "d_weight", "d_bias", "d_gate"])
 def test_one_gradient_alone(what):
     c = case(130, 96, 140, act="gelu", gate=True, drop=0.2, grads=True)
