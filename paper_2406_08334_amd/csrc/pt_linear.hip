@@ -1,9 +1,13 @@
 // Matrix product with bias, activation, gate, dropout and residual in its epilogue, and its gradients.
 //
 //   out       z = x W^T + bias, out = residual + D(act(z) gate), z in 16 bits if it is to be kept: one product, the rest on its sums in registers
-//   slope     dz = D(d_out) gate act'(pre) in 16 bits, d_gate, and sums of dz's columns for the bias
+//   slope     dz = D(d_out gate act'(pre)) in 16 bits, d_gate, and sums of dz's columns for the bias; copies of operands that the products cannot take
 //   d_x       = dz W,  d_weight = dz^T x
 //
+// Up to 32 rows out is a matter of reading the weight (k_linear_thin); beyond, and for the gradients, tiles of pt_mfma.h.
+// Products bound the large ones: 8192 x 4096 x 8192 bf16 410 us, 1340 TFLOP/s, where a large library product reaches 1473 at best and 1410 here; 8192 x 1600 x 6400 with
+// bias, gelu and z kept 191 (a round of tiles 39 of products, 17 of epilogue, which nothing else of its compute unit hides); e4m3 8192 x 4096 x 11008 344 us,
+// 2150 TFLOP/s (library, without scales of rows: 324).  Gradients of 8192 x 4096 x 11008 1247 us: 511 + 537 at 1440 and 1380 TFLOP/s, slope 167 at 5.4 TB/s.
 #include "pt_random.h"
 #include "pt_rows.h"
 
