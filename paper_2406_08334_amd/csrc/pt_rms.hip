@@ -294,8 +294,8 @@ __global__ void __launch_bounds__(Rows<WAVES>::THREADS) k_rows8(const Rows8Args 
 
 // ---- host -----------------------------------------------------------------------------------------------
 
-// f: called with the waves that share a row of `width` and a lane's pieces of it, as constants: as few waves as 32 elements a lane allow (no more than 16 where
-// sums over the rows are kept too), and no more idle lanes than that makes.
+// f: called with the waves that share a row of `width` and a lane's pieces of it, as constants: as few waves as 32 elements a lane allow (by_width_grads, where
+// sums over the rows are kept too: as the registers do), and no more idle lanes than that makes.
 template <int W, int P, class F> int with(F&& f) { return f(std::integral_constant<int, W>{}, std::integral_constant<int, P>{}); }
 template <class F> int by_width(uint32_t width, F&& f) {
   if (width <= 512) return with<1, 1>(f);

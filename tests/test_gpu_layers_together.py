@@ -96,6 +96,33 @@ def test_a_norm_in_8_bits_before_a_product_in_8_bits(rows):
     ref.within("out", out, *ref.linear(c)["out"])
 
 
+def test_two_streams_at_once():
+    """The same block on two streams with a workspace each, call behind call without waiting: the results of one after the other."""
+    blocks, want = [], []
+    for seed in (1, 2):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        h = torch.randn(700, 192, generator=gen, device="cuda").bfloat16()
+        b = train_head.Block(h, 640, 0.25, seed, gen)
+        b.d_out.copy_(torch.randn(700, 192, generator=gen, device="cuda"))
+        b.forward(), b.backward()
+        blocks.append(b)
+        want.append([x.clone() for x in [b.out, b.d_hidden] + b.grads])
+        b.step.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for _ in range(5):
+        for b, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                b.forward()
+        for b, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                b.backward()
+                b.step.zero_()
+    torch.cuda.synchronize()
+    for b, w in zip(blocks, want):
+        assert all(torch.equal(x, y) for x, y in zip([b.out, b.d_hidden] + b.grads, w))
+
+
 @pytest.mark.parametrize("bits,dtype", [(8, "bf16"), (32, "fp16")])
 def test_the_example_runs_with_a_block(bits, dtype):
     losses = train_head.train(steps=30, vocab=256, width=64, rows=512, bits=bits, dtype=dtype, mlp=128, drop=0.1)
