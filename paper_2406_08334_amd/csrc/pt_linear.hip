@@ -628,7 +628,16 @@ Choice choose(uint32_t m, uint32_t n, uint32_t twos, bool layer) {
     const Split s = split<C>((m + C::BM - 1) / C::BM * ((n + C::BN - 1) / C::BN), twos, !layer ? 3000 : C::BM == 256 ? 12000 : 5000);
     return Choice{kind, s, 4ull * s.tail * s.n * C::BM * C::BN};
   };
-  if (n <= uint32_t(Few::BN)) return of(Few{}, FEW);
+  if (n <= uint32_t(Few::BN)) {
+    Choice c = of(Few{}, FEW);
+    // shared by so few workgroups that a quarter of the chip idles: by twice as many, two of which fit a compute unit (64 x 4096 x 11008, 172: 33.9 -> 28.2 us; where 200
+    // or more run already, twice as many cost their sums: 64 x 1600 x 6400 13.8, 14.5)
+    if (layer && c.split.tail && !c.split.whole && c.split.tail * c.split.n <= 192 && c.split.n * 4 <= twos) {
+      c.split.n *= 2;
+      c.bytes *= 2;
+    }
+    return c;
+  }
   const Choice big = of(Big{}, BIG), mid = of(Mid{}, MID);
   const uint32_t left = m % 256, tenths = m / 256 * 10 + (left == 0 ? 0 : left <= 64 ? 4 : left <= 128 ? 6 : 10);
   return mid.split.ns < big.split.ns * tenths / ((m + 255) / 256 * 10) ? mid : big;
