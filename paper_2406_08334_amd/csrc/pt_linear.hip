@@ -322,7 +322,8 @@ struct ProductArgs {
 
 // Up to LOW rows what rounding dz leaves is multiplied as rows of its own, which lie LOW behind, in tiles that have room for them.  It is of few rows and outs that single
 // roundings show: gradients of one row and 64 outs would have up to 2.1 times the error of rounding the result alone (of many rows 1.4).  1 x 4096 x 11008 56.5 -> 60.2
-// us, 16 x 4096 x 11008 59.1 -> 61.1, as x is copied and dz twice as long.
+// us, 16 x 4096 x 11008 59.1 -> 61.1, as x is copied and dz twice as long.  An infinite operand is no matter of what is left (0 inf is NaN): in d_x it adds to finite sums
+// only, which have no such operand, and for d_weight x is copied without them.
 constexpr uint32_t LOW = 32;
 static_assert(Few::BN == 2 * LOW, "both in a tile");
 
@@ -341,7 +342,12 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, const E& e, l
 #pragma unroll
         for (int j = 0; j < T::FN / 2; ++j)
 #pragma unroll
-          for (int i = 0; i < T::FM; ++i) t.acc[i][j] += t.acc[i][j + T::FN / 2];
+          for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float x = t.acc[i][j][q];
+            t.acc[i][j][q] = __builtin_fabsf(x) < __builtin_inff() ? x + t.acc[i][j + T::FN / 2][q] : x;
+          }
       }
     }
     if (left) {
@@ -486,7 +492,9 @@ struct CopyArgs {
   uint64_t stride;
   uint32_t rows, width, pitch;             // elements; pitch: of a copied row, which is zero behind its end
   void* to;
-  uint32_t low;                            // 0, or how many rows there are: they go to rows 0 on and to rows LOW on, zero up to LOW and 2 LOW (rows is that then)
+  uint32_t low;                            // 0, or how many rows there are: they go to rows 0 on and, but for infinities and NaN, to rows LOW on, zero up to LOW and 2 LOW
+                                           // (rows is that then)
+  uint32_t exponent;                       // of infinities and NaN
 };
 inline uint32_t copy_blocks(const CopyArgs& a) { return (a.rows + 3) / 4; }
 // Of one or two bytes an element, four rows by a workgroup of 256.
@@ -495,8 +503,11 @@ __device__ __forceinline__ void copy_rows(const CopyArgs& a, uint32_t block) {
   const uint32_t r = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
   if (r >= a.rows) return;
   if constexpr (BYTES == 2) {
-    const uint32_t from = a.low ? r % LOW : r;
-    copy_row((const PT_GLOBAL uint16_t*)a.from + from * a.stride, (PT_GLOBAL uint16_t*)a.to + size_t(r) * a.pitch, a.low && from >= a.low ? 0 : a.width, a.pitch, lane, 64);
+    const uint32_t from = a.low ? r % LOW : r, width = a.low && from >= a.low ? 0 : a.width;
+    const PT_GLOBAL uint16_t* row = (const PT_GLOBAL uint16_t*)a.from + from * a.stride;
+    PT_GLOBAL uint16_t* to = (PT_GLOBAL uint16_t*)a.to + size_t(r) * a.pitch;
+    if (a.low && r >= LOW) copy_row<true>(row, to, width, a.pitch, lane, 64, a.exponent);
+    else copy_row(row, to, width, a.pitch, lane, 64);
   } else {
     const PT_GLOBAL char* row = (const PT_GLOBAL char*)a.from + r * a.stride;
     PT_GLOBAL char* to = (PT_GLOBAL char*)a.to + size_t(r) * a.pitch;
@@ -811,7 +822,7 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
     return b8 ? run_thin<PT_E4M3, DT>(a, e, st) : run_thin<DT, DT>(a, e, st);
   }
   const uint32_t pitch = 2 * p.Kd / bytes;
-  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, pitch, ws + p.x, 0}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, pitch, ws + p.w, 0};
+  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : l.rows, l.width, pitch, ws + p.x, 0, 0}, cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, pitch, ws + p.w, 0, 0};
   if (int rc = b8 ? copy<1>(cx, cw, st) : copy<2>(cx, cw, st); rc != PT_OK) return rc;
   const uint32_t per = b8 ? 2 : 1;         // elements in a 16-bit word
   const ProductArgs a = {rows_of(p.w_direct, l.weight, l.weight_stride / per, l.width / per, ws + p.w, p.Kd, l.outs),
@@ -821,8 +832,8 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
 }
 
 template <int DT> int run_grads(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
-  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : p.rows, l.width, p.Kd, ws + p.x, p.low ? l.rows : 0};
-  const CopyArgs cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, p.Kd, ws + p.w, 0};
+  const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : p.rows, l.width, p.Kd, ws + p.x, p.low ? l.rows : 0, DT == PT_BF16 ? 0x7f80u : 0x7c00u};
+  const CopyArgs cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, p.Kd, ws + p.w, 0, 0};
   const bool dz_wanted = p.slope && (l.d_x || l.d_weight);
   if (dz_wanted || l.d_bias || l.d_gate) {
     const SlopeArgs a = {(const uint16_t*)l.d_out, l.act != PT_ACT_NONE || l.gate ? (const uint16_t*)l.pre : nullptr, (const uint16_t*)l.gate,

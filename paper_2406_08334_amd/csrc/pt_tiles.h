@@ -13,8 +13,11 @@ typedef u32x2 u32x2_a __attribute__((aligned(2)));
 
 inline uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 
-// One row of 16-bit words, at any address, into one of Kd words that begins at a multiple of 16 bytes; zero behind its end.
-__device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOBAL uint16_t* to, uint32_t d, uint32_t Kd, uint32_t lane, uint32_t lanes) {
+// One row of 16-bit words, at any address, into one of Kd words that begins at a multiple of 16 bytes; zero behind its end.  FINITE: and where all bits of `exponent`
+// are set, infinities and NaN.
+template <bool FINITE = false>
+__device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOBAL uint16_t* to, uint32_t d, uint32_t Kd, uint32_t lane, uint32_t lanes,
+                                         uint32_t exponent = 0) {
 #pragma unroll 4
   for (uint32_t c = lane * 8; c < Kd; c += lanes * 8) {
     u32x4 q = {0, 0, 0, 0};
@@ -23,6 +26,10 @@ __device__ __forceinline__ void copy_row(const PT_GLOBAL uint16_t* from, PT_GLOB
 #pragma unroll
       for (uint32_t j = 0; j < 8; ++j)
         if (c + j < d) q[j / 2] |= uint32_t(from[c + j]) << (16 * (j & 1));
+    if constexpr (FINITE) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] &= ((q[j] & exponent) == exponent ? 0u : 0xffffu) | ((q[j] >> 16 & exponent) == exponent ? 0u : 0xffff0000u);
+    }
     *(PT_GLOBAL u32x4*)(to + c) = q;
   }
 }
