@@ -544,10 +544,10 @@ typedef enum { PT_ACT_NONE = 0, PT_ACT_RELU = 1, PT_ACT_GELU = 2 /* by erf */, P
  *     z_rn = sum_k x_rk W_nk + bias_n         pre = z        out = residual + D(act(z) gate)
  * computed in fp32 from exact products, each output rounded once.  (Of codes in 8 bits the matrix cores add the products of every eight next to each other, 8 i on, as
  * multiples of 2^-13 of the largest one's power of two, cut towards zero; the sums of eight in fp32, which has to hold a sum times x_scale.)  Gradients, from d_out, x, W,
- * pre (as rounded) and gate:
+ * pre (as rounded, +-inf beyond the type) and gate:
  *     e = D(d_out)    d_gate = e act(pre)    dz = e gate act'(pre)    d_bias = sum_r dz    d_x = dz W    d_weight = dz^T x
  * dz is rounded to the 16-bit type between the products (d_bias is not of rounded ones; of up to 32 rows what that leaves is multiplied as
- * well); d_residual is d_out itself. */
+ * well); d_residual is d_out itself.  At -inf relu, both gelus and silu are their limit, 0, and so is the derivative; at +inf they are inf, and it is 1. */
 typedef struct {
   const void* x;             /* device, [rows, width] 16-bit elements; with x_scale e4m3 codes            */
   const void* weight;        /* device, [outs, width], as x                                               */

@@ -35,12 +35,16 @@ __device__ __forceinline__ float normal(float z, float& e) {
   return z < 0.0f ? q : 1.0f - q;
 }
 
+// z f, where f is 0 below -FAR, for -inf too, of which it is the limit; NaN comes from f.
+constexpr float FAR = 128.0f;
+__device__ __forceinline__ float times(float z, float f) { return __builtin_fmaxf(z, -FAR) * f; }
+
 template <int ACT>
 __device__ __forceinline__ float act(float z) {
   if constexpr (ACT == PT_ACT_RELU) return z < 0.0f ? 0.0f : z;
-  else if constexpr (ACT == PT_ACT_SILU) return z * sigmoid(z);
-  else if constexpr (ACT == PT_ACT_GELU_TANH) return z * sigmoid(TANH_2A * __builtin_fmaf(TANH_B * z, z * z, z));     // (1 + tanh(u)) / 2 = sigmoid(2 u)
-  else if constexpr (ACT == PT_ACT_GELU) { float e; return z * normal(z, e); }
+  else if constexpr (ACT == PT_ACT_SILU) return times(z, sigmoid(z));
+  else if constexpr (ACT == PT_ACT_GELU_TANH) return times(z, sigmoid(TANH_2A * __builtin_fmaf(TANH_B * z, z * z, z)));     // (1 + tanh(u)) / 2 = sigmoid(2 u)
+  else if constexpr (ACT == PT_ACT_GELU) { float e; return times(z, normal(z, e)); }
   else return z;
 }
 // act(z) and its derivative, which beyond 32 is 0 or 1 (its terms there would be products of 0 and inf), as are the factors of z.
@@ -53,16 +57,16 @@ __device__ __forceinline__ float act(float z, float& slope) {
   } else if constexpr (ACT == PT_ACT_SILU) {
     const float f = sigmoid(z);
     slope = f * __builtin_fmaf(c, 1.0f - f, 1.0f);
-    return z * f;
+    return times(z, f);
   } else if constexpr (ACT == PT_ACT_GELU_TANH) {
     const float f = sigmoid(TANH_2A * __builtin_fmaf(TANH_B * c, c * c, c));
     slope = __builtin_fmaf(c * f * (1.0f - f), TANH_2A * __builtin_fmaf(3.0f * TANH_B * c, c, 1.0f), f);
-    return z * f;
+    return times(z, f);
   } else if constexpr (ACT == PT_ACT_GELU) {
     float e;
     const float f = normal(c, e);
     slope = __builtin_fmaf(c * 0.39894228040143267794f, e, f);
-    return z * f;
+    return times(z, f);
   }
   slope = 1.0f;
   return z;

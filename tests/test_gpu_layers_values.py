@@ -53,3 +53,53 @@ def test_infinite_operands_of_gradients(rows, outs, dtype, exact):
     got = gradients(c, x=x, weight=w)
     assert bool(got["d_weight"][:, k].isnan().all()) and bool(got["d_x"][:, k].isnan().all())
     assert torch.equal(got["d_weight"][:, rest], want["d_weight"][:, rest]) and torch.equal(got["d_x"][:, rest], want["d_x"][:, rest])
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [3, 100])
+def test_gradients_of_a_saturated_z(rows, dtype, act):
+    """z beyond the type's range is kept as +-inf: there an activation is its limit, 0 or z, and its derivative 0 or 1."""
+    c = case(rows, 64, 96, dtype, act=act, gate=True, grads=True)
+    e, g = c["d_out"].double(), c["gate"].double()
+    want = gradients(c)
+    pre = c["pre"].clone()
+    pre[1, 5], pre[2, 7] = -INF, INF
+    got = gradients(c, pre=pre)
+    assert bool(got["d_x"].isfinite().all()) and bool(got["d_weight"].isfinite().all())
+    assert float(got["d_gate"][1, 5]) == (-INF * float(e[1, 5].sign()) if act == "none" else 0.0)
+    assert float(got["d_gate"][2, 7]) == INF * float(e[2, 7].sign())
+    for where, slope in (((1, 5), 1.0 if act == "none" else 0.0), ((2, 7), 1.0)):
+        rest = [r for r in range(rows) if r != where[0]]
+        bias = (e[rest, where[1]] * g[rest, where[1]] * ref.act(act, c["pre"][rest, where[1]].double())[1])
+        v = bias.sum() + slope * e[where] * g[where]
+        # as in ref.linear_grads: the activation's derivative, the sum, one rounding
+        bound = (ref.ACT_ERR + (rows + 64) * ref.E) * (e[:, where[1]] * g[:, where[1]]).abs().sum() * 1.2 + 1.001 * ref.rounding(v, c["pre"].dtype)
+        assert abs(float(got["d_bias"][where[1]]) - float(v)) <= float(bound)
+    same = torch.ones(rows, 96, dtype=torch.bool, device="cuda")
+    same[1, 5], same[2, 7] = False, False
+    assert torch.equal(got["d_gate"][same], want["d_gate"][same])
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,outs", [(16, 64, 32), (48, 64, 40), (200, 64, 136), (2048, 1024, 4104)])
+def test_activations_of_infinite_z(rows, width, outs, dtype, act):
+    """Through every kind of product and epilogue: +inf stays, -inf becomes the activation's limit, NaN stays NaN, other rows keep their bits."""
+    dt = ref.TYPES[dtype][0]
+    for gate in (None, torch.full((rows, outs), 2.0, dtype=dt, device="cuda")):
+        x, w = torch.zeros(rows, width, dtype=dt, device="cuda"), torch.zeros(outs, width, dtype=dt, device="cuda")
+        x[:, 0] = torch.linspace(-4.0, 4.0, rows, device="cuda")
+        w[:, 0] = 1.0
+        outs_ = []
+        for bad in (None, INF, -INF, NAN):
+            if bad is not None:
+                x[rows // 3, 0] = bad
+            c = dict(x=x, weight=w, act=act, gate=gate, out=torch.full((rows, outs), 7.0, dtype=dt, device="cuda"), buffers={})
+            call(c)
+            outs_.append(c["out"])
+        for bad, out in zip((INF, -INF, NAN), outs_[1:]):
+            f = out[rows // 3].float()
+            assert bool(f.isnan().all() if bad != bad else (f == (bad if bad > 0 or act == "none" else 0.0)).all()), bad
+            out[rows // 3] = outs_[0][rows // 3]
+            assert torch.equal(out, outs_[0])
