@@ -547,7 +547,8 @@ typedef enum { PT_ACT_NONE = 0, PT_ACT_RELU = 1, PT_ACT_GELU = 2 /* by erf */, P
  * pre (as rounded, +-inf beyond the type) and gate:
  *     e = D(d_out)    d_gate = e act(pre)    dz = e gate act'(pre)    d_bias = sum_r dz    d_x = dz W    d_weight = dz^T x
  * dz is rounded to the 16-bit type between the products (d_bias is not of rounded ones; of up to 32 rows what that leaves is multiplied as
- * well); d_residual is d_out itself.  At -inf relu, both gelus and silu are their limit, 0, and so is the derivative; at +inf they are inf, and it is 1. */
+ * well); d_residual is d_out itself.  A pre of -inf has activation and derivative 0, but for PT_ACT_NONE, one of +inf inf and 1; a sum
+ * that is -inf itself makes an out of NaN with gelu, gelu_tanh and silu. */
 typedef struct {
   const void* x;             /* device, [rows, width] 16-bit elements; with x_scale e4m3 codes            */
   const void* weight;        /* device, [outs, width], as x                                               */
