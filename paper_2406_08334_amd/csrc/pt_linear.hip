@@ -47,10 +47,10 @@ __device__ __forceinline__ float act(float z) {
 // -inf, and its product with 0 NaN: 8192 x 1600 x 6400 with gelu 204.5 -> 207.7 us, 8192 x 4096 x 11008 with silu 578 -> 584.)
 constexpr float FAR = 128.0f;
 __device__ __forceinline__ float times(float z, float f) { return __builtin_fmaxf(z, -FAR) * f; }
-// act(z) and its derivative, which beyond 32 is 0 or 1 (its terms there would be products of 0 and inf), as are the factors of z.
+// act(z) and its derivative, which beyond FAR is 0 or 1 in fp32 (its terms there would be products of 0 and inf), as are the factors of z.
 template <int ACT>
 __device__ __forceinline__ float act(float z, float& slope) {
-  const float c = z < -32.0f ? -32.0f : z > 32.0f ? 32.0f : z;
+  const float c = z < -FAR ? -FAR : z > FAR ? FAR : z;
   if constexpr (ACT == PT_ACT_RELU) {
     slope = z > 0.0f ? 1.0f : 0.0f;
     return act<ACT>(z);

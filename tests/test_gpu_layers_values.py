@@ -106,3 +106,19 @@ def test_activations_of_infinite_z(rows, width, outs, dtype, act):
                 assert bool((f == (0.0 if bad < 0 and act == "relu" else bad)).all()), bad
             out[rows // 3] = outs_[0][rows // 3]
             assert torch.equal(out, outs_[0])
+
+
+def test_silu_derivative_far_below_zero():
+    """(1 + z) sigmoid(z) to fp32's accuracy as far as it is a normal number: the exponential's argument counts up to 123, each unit E twice over, and the factors
+    a few E; one rounding to bf16."""
+    z = torch.tensor([-20.0, -31.0, -32.0, -33.0, -40.0, -48.5, -57.0, -64.0, -71.0, -80.0, -84.0], dtype=torch.bfloat16, device="cuda")
+    n = z.numel()
+    for rows in (1, 40):
+        dt, dev = torch.bfloat16, "cuda"
+        pre, d_out = z.expand(rows, n).contiguous(), torch.zeros(rows, n, dtype=dt, device=dev)
+        d_out[rows - 1] = 1.0
+        d_bias = torch.empty(n, dtype=dt, device=dev)
+        c = dict(x=torch.zeros(rows, 8, dtype=dt, device=dev), weight=torch.zeros(n, 8, dtype=dt, device=dev), act="silu", pre=pre, d_out=d_out, d_bias=d_bias, buffers={})
+        call(c, True)
+        want = (1 + z.double()) * torch.sigmoid(z.double())
+        ref.within("d_bias", d_bias, want, 300 * ref.E * want.abs() + 1.001 * ref.rounding(want, dt))
