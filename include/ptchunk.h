@@ -601,7 +601,7 @@ typedef struct {
   void* d_x;             /* device, [rows, width] 16-bit, or NULL                                      */
   void* d_gain;          /* device, [width] 16-bit, or NULL                                            */
   uint64_t x_stride, residual_stride, sum_stride, y_stride, d_y_stride, d_sum_stride, d_x_stride;
-  double eps;            /* >= 0                                                                       */
+  double eps;            /* >= 0 and in fp32's range; above 0 it is fp32's least at least               */
   uint32_t rows, width;  /* width up to 32768                                                          */
   int32_t dtype;         /* pt_dtype                                                                   */
   int32_t reserved;

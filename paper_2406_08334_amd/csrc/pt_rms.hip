@@ -10,6 +10,7 @@
 // rows8 of 13824 x 5120 in fp32 61 us, 5.8.
 #include "pt_rows.h"
 
+#include <cfloat>
 #include <cmath>
 
 using namespace pt_rows_ops;
@@ -351,7 +352,7 @@ int check(const pt_rms* n, const char* who) {
   if (!n) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: norm is NULL", who);
   if (n->dtype != PT_BF16 && n->dtype != PT_FP16) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: dtype %d is neither PT_BF16 nor PT_FP16", who, n->dtype);
   if (!n->width) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: width must be > 0", who);
-  if (!(n->eps >= 0.0)) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: eps must be >= 0", who);
+  if (!(n->eps >= 0.0 && n->eps <= double(FLT_MAX))) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "%s: eps is not >= 0 and in fp32's range", who);
   const struct { const void* at; uint64_t stride; } rows[] = {{n->x, n->x_stride}, {n->residual, n->residual_stride}, {n->sum, n->sum_stride},
     {n->y, n->y_stride}, {n->d_y, n->d_y_stride}, {n->d_sum, n->d_sum_stride}, {n->d_x, n->d_x_stride}};
   for (const auto& x : rows)
@@ -375,11 +376,12 @@ extern "C" int pt_rms_norm(const pt_rms* n, void* stream) {
   if (int rc = check(n, "pt_rms_norm"); rc != PT_OK) return rc;
   if (!n->rows) return PT_OK;
   if (!n->x || !n->y) return pt_fail(nullptr, PT_ERR_INVALID_ARG, "pt_rms_norm: NULL array");
+  const float eps = n->eps > 0.0 ? std::max(float(n->eps), FLT_TRUE_MIN) : 0.0f;       // above 0 stays above 0: rows of zeros
   for (uint64_t r = 0; r < n->rows; r += MOST_ROWS) {
     const auto row = [&](const void* x, uint64_t stride) { return x ? (uint16_t*)x + r * stride : nullptr; };
     const NormArgs a = {row(n->x, n->x_stride), row(n->residual, n->residual_stride), (const uint16_t*)n->gain, row(n->sum, n->sum_stride),
                         n->rstd ? n->rstd + r : nullptr, n->y_scale ? (void*)((uint8_t*)n->y + r * n->y_stride) : row(n->y, n->y_stride),
-                        n->y_scale ? n->y_scale + r : nullptr, n->x_stride, n->residual_stride, n->sum_stride, n->y_stride, float(n->eps),
+                        n->y_scale ? n->y_scale + r : nullptr, n->x_stride, n->residual_stride, n->sum_stride, n->y_stride, eps,
                         1.0f / float(n->width), uint32_t(std::min<uint64_t>(MOST_ROWS, n->rows - r)), n->width};
     if (int rc = n->dtype == PT_BF16 ? norm_rows<PT_BF16>(a, (hipStream_t)stream) : norm_rows<PT_FP16>(a, (hipStream_t)stream); rc != PT_OK) return rc;
   }

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import layers_reference as ref
+from paper_2406_08334_amd import binding as B
 from test_gpu_linear import call, case
 
 pytestmark = pytest.mark.gpu
@@ -122,3 +123,18 @@ def test_silu_derivative_far_below_zero():
         call(c, True)
         want = (1 + z.double()) * torch.sigmoid(z.double())
         ref.within("d_bias", d_bias, want, 300 * ref.E * want.abs() + 1.001 * ref.rounding(want, dt))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_an_eps_that_fp32_has_not(bits):
+    """Above 0, and so a row of zeros stays zero; its rstd is a number."""
+    x = torch.randn(4, 100).bfloat16().cuda()
+    x[2] = 0
+    y = torch.empty(4, 100, dtype=torch.uint8 if bits == 8 else torch.bfloat16, device="cuda")
+    y_scale, rstd = torch.empty(4, device="cuda") if bits == 8 else None, torch.empty(4, device="cuda")
+    B.pt_rms_norm(B.rms(x, y, rstd=rstd, y_scale=y_scale, eps=1e-60))
+    torch.cuda.synchronize()
+    v = y.float() if bits == 16 else y.view(torch.float8_e4m3fn).float() * y_scale[:, None]
+    assert bool(rstd.isfinite().all()) and bool((v[2] == 0).all()) and bool(v.isfinite().all())
+    _, want_r, want, err = ref.rms(x[[0, 1, 3]], None, None, 0.0)
+    ref.within("rstd", rstd[[0, 1, 3]], want_r, err * want_r)
