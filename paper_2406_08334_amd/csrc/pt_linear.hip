@@ -664,7 +664,7 @@ bool direct(const void* at, uint64_t stride, uint32_t width, uint32_t bytes) {
 
 // Where everything lies in the workspace.
 struct Plan {
-  bool x_direct, w_direct, slope;          // slope: dz is not d_out
+  bool x_direct, w_direct, slope;          // slope: the products need a dz that is not d_out
   bool both;                               // gradients in one launch
   bool low;                                // as in ProductArgs
   uint32_t rows;                           // of dz and the x that is multiplied with it
@@ -707,7 +707,7 @@ Plan plan_grads(const pt_linear& l) {
   p.rows = p.low ? 2 * LOW : l.rows;
   p.x_direct = !l.d_weight || (!p.low && direct(l.x, l.x_stride, l.width, 2));
   p.w_direct = !l.d_x || direct(l.weight, l.weight_stride, l.width, 2);
-  p.slope = rounds || !direct(l.d_out, l.d_out_stride, l.outs, 2);
+  p.slope = (l.d_x || l.d_weight) && (rounds || !direct(l.d_out, l.d_out_stride, l.outs, 2));
   p.x = take(p.x_direct ? 0 : 2ull * p.rows * p.Kd);
   p.w = take(p.w_direct ? 0 : 2ull * l.outs * p.Kd);
   p.dz = take(p.slope ? 2ull * p.rows * p.Np : 0);
@@ -838,10 +838,9 @@ template <int DT> int run_out(const pt_linear& l, const Plan& p, char* ws, hipSt
 template <int DT> int run_grads(const pt_linear& l, const Plan& p, char* ws, hipStream_t st) {
   const CopyArgs cx = {l.x, l.x_stride, p.x_direct ? 0 : p.rows, l.width, p.Kd, ws + p.x, p.low ? l.rows : 0, DT == PT_BF16 ? 0x7f80u : 0x7c00u};
   const CopyArgs cw = {l.weight, l.weight_stride, p.w_direct ? 0 : l.outs, l.width, p.Kd, ws + p.w, 0, 0};
-  const bool dz_wanted = p.slope && (l.d_x || l.d_weight);
-  if (dz_wanted || l.d_bias || l.d_gate) {
+  if (p.slope || l.d_bias || l.d_gate) {
     const SlopeArgs a = {(const uint16_t*)l.d_out, l.act != PT_ACT_NONE || l.gate ? (const uint16_t*)l.pre : nullptr, (const uint16_t*)l.gate,
-                         dz_wanted ? (uint16_t*)(ws + p.dz) : nullptr, (uint16_t*)l.d_gate, l.d_bias ? (float*)(ws + p.part) : nullptr, l.d_out_stride,
+                         p.slope ? (uint16_t*)(ws + p.dz) : nullptr, (uint16_t*)l.d_gate, l.d_bias ? (float*)(ws + p.part) : nullptr, l.d_out_stride,
                          l.pre_stride, l.gate_stride, l.d_gate_stride, pt_random::make(l.drop), (uint64_t(l.outs) + 3) / 4, l.rows, l.outs, p.Np, p.rows_each,
                          (p.Np + 511) / 512, l.act, p.low};
     const uint32_t blocks = a.strips * p.row_blocks;
