@@ -645,8 +645,10 @@ Choice choose(uint32_t m, uint32_t n, uint32_t twos, bool layer) {
   };
   if (n <= uint32_t(Few::BN)) {
     Choice c = of(Few{}, FEW);
-    // shared by so few workgroups that a quarter of the chip idles: by twice as many, two of which fit a compute unit (64 x 4096 x 11008, 172: 33.9 -> 28.2 us; where 200
-    // or more run already, twice as many cost their sums: 64 x 1600 x 6400 13.8, 14.5)
+    // shared by so few workgroups that a quarter of the chip idles: by twice as many, two of which fit a compute unit (64 rows, once and twice as many: 4096 x 11008, 172,
+    // 36.0 and 29.2 us; 4096 x 12288, 192, 37.3 and 30.9).  Where more run, twice as many cost their sums if the weight is short (1600 x 6400, 250, 13.7 and 13.7; 4096 x 5120,
+    // 240, 16.8 and 17.9; 4096 x 4096, 15.5 and 17.0; 2048 x 8192, 15.6 and 17.1); of a long one they would pay too, which this rule leaves (5120 x 13824, 216, 51.9 and 45.6;
+    // 4096 x 14336, 224, 41.7 and 34.5; 8192 x 8192, 44.0 and 38.8).
     if (layer && c.split.tail && !c.split.whole && c.split.tail * c.split.n <= 192 && c.split.n * 4 <= twos) {
       c.split.n *= 2;
       c.bytes *= 2;
